@@ -75,7 +75,8 @@ typedef enum {
   OCC_E_ALIAS = 7,     /* two buffers overlap (only err_new == err_prev may) */
   OCC_E_WORKSPACE = 8, /* workspace NULL, too small, or not 256-byte aligned */
   OCC_E_HIP = 9,       /* a HIP runtime call or kernel launch failed */
-  OCC_E_FLAGS = 10     /* unknown bit in the flags argument */
+  OCC_E_FLAGS = 10,    /* unknown bit in the flags argument */
+  OCC_E_VALUE = 11     /* an activation, hyperparameter or state form outside its range */
 } occ_status_t;
 
 typedef enum { OCC_F32 = 0, OCC_BF16 = 1 } occ_dtype_t;
@@ -274,6 +275,166 @@ occ_status_t occ_sc_select(const occ_stage_t* stages, int n_stages, int max_comp
 /* Read (and optionally clear) the sticky numeric flags of a workspace.
  * Synchronises `stream`. */
 occ_status_t occ_get_flags(void* ws, uint32_t* flags_out, int clear, occ_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Stage operators: what a pipeline stage runs right before and right after
+ * the compressor.  The backward pass of a layer takes the activation gradient
+ * that occ_decompress_ex rebuilt and makes the weight gradients that
+ * occ_step_batched compresses; AdamW takes the decompressed gradients, or the
+ * factors themselves.  The conventions above hold: device pointers, row-major
+ * matrices with leading dimensions, any alignment (rows that start on 16 bytes
+ * and hold whole 16-byte pieces select the fastest forms), host-side checks,
+ * work enqueued on `stream`.  Results are deterministic: no atomics, and sums
+ * in an order that sizes and alignment alone decide.
+ * ------------------------------------------------------------------------- */
+
+/* Activation functions: z; max(z, 0); z Phi(z); the tanh form
+ * z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2; z / (1 + e^-z). */
+typedef enum {
+  OCC_ACT_NONE = 0,
+  OCC_ACT_RELU = 1,
+  OCC_ACT_GELU = 2,
+  OCC_ACT_GELU_TANH = 3,
+  OCC_ACT_SILU = 4
+} occ_act_t;
+
+/* Forward pass of a layer (all matrices of type `dtype`, products and sums in
+ * fp32, one rounding at each store):
+ *   occ_linear_fwd   Z = X W^T + bias, Y = act(Z) + R
+ *                    W is out x in, bias holds `out` values, Z is tokens x out
+ *   occ_gated_fwd    [G U] = X W^T + bias, Y = act(G) * U + R
+ *                    W is 2 out x in (the gate's rows, then the other
+ *                    projection's), bias holds 2 out values, Z = [G U] is
+ *                    tokens x 2 out
+ * X is tokens x in, Y and R tokens x out.  bias (fp32), R and Z may be NULL;
+ * R may be Y (the residual is replaced in place).  Z is what the backward pass
+ * needs: leave it out when serving.  tokens may be 0 (nothing is done).
+ * in and out at most 2^24. */
+typedef struct {
+  int32_t dtype; /* occ_dtype_t */
+  int32_t act;   /* occ_act_t */
+  int64_t tokens, in, out;
+  const void* X;
+  int64_t ldx;
+  const void* W;
+  int64_t ldw;
+  const float* bias;
+  const void* R;
+  int64_t ldr;
+  void* Z;
+  int64_t ldz;
+  void* Y;
+  int64_t ldy;
+} occ_linear_t;
+
+/* Backward pass.  With dZ the gradient at the pre-activation,
+ *   linear: dZ = dY act'(Z)           gated: dZ = [dY U act'(G), dY act(G)]
+ *   dX = dZ W      dW = dZ^T X      dbias = sum of dZ over the tokens
+ * dX, dW and dbias may each be NULL (not wanted; at least one is given).  X is
+ * needed for dW, W for dX, Z unless the layer is linear with OCC_ACT_NONE.
+ * dW has type dw_dtype: `dtype`, or OCC_F32 for a bf16 layer.  With
+ * OCC_GRAD_ACCUMULATE dW and dbias are added to (micro-batches), dX is not.
+ * dZ is rounded to `dtype` before the products when it is not dY itself; dbias
+ * is summed from it before that rounding.  With no tokens dW and dbias are set
+ * to zero (or left, when accumulating). */
+typedef struct {
+  int32_t dtype;    /* occ_dtype_t */
+  int32_t dw_dtype; /* occ_dtype_t */
+  int32_t act;      /* occ_act_t */
+  int32_t reserved;
+  int64_t tokens, in, out;
+  const void* dY;
+  int64_t lddy;
+  const void* X;
+  int64_t ldx;
+  const void* W;
+  int64_t ldw;
+  const void* Z;
+  int64_t ldz;
+  void* dX;
+  int64_t lddx;
+  void* dW;
+  int64_t lddw;
+  float* dbias;
+} occ_linear_grad_t;
+
+enum { OCC_GRAD_ACCUMULATE = 1u };
+
+/* Workspace bytes of the calls below for these arguments (sizes, leading
+ * dimensions, alignment and which outputs are asked for).  0: none is needed
+ * and ws may be NULL, or the arguments are invalid.  The workspace needs no
+ * initialisation; its first 256 bytes (the numeric flags of the compressor)
+ * are left alone, so one workspace can serve every call of a stage. */
+size_t occ_linear_fwd_workspace_bytes(const occ_linear_t* l);
+size_t occ_gated_fwd_workspace_bytes(const occ_linear_t* l);
+size_t occ_linear_bwd_workspace_bytes(const occ_linear_grad_t* l);
+size_t occ_gated_bwd_workspace_bytes(const occ_linear_grad_t* l);
+
+occ_status_t occ_linear_fwd(const occ_linear_t* l, void* ws, size_t ws_bytes, occ_stream_t stream);
+occ_status_t occ_gated_fwd(const occ_linear_t* l, void* ws, size_t ws_bytes, occ_stream_t stream);
+occ_status_t occ_linear_bwd(const occ_linear_grad_t* l, unsigned flags, void* ws, size_t ws_bytes,
+                            occ_stream_t stream);
+occ_status_t occ_gated_bwd(const occ_linear_grad_t* l, unsigned flags, void* ws, size_t ws_bytes,
+                           occ_stream_t stream);
+
+/* One tensor of occ_adamw_step.  W, W16, m and v are contiguous rows x cols
+ * (a vector: rows = 1).
+ *   W        fp32 weights, updated
+ *   W16      bf16 copy of the new weights (nearest even), or NULL
+ *   G        gradient of type g_dtype, leading dimension ldg, or NULL: then
+ *   P, Q     the gradient is P Q^T (P rows x rank, Q cols x rank, contiguous,
+ *            fp32: the compressor's factors); it is not written anywhere
+ *   m, v     state_bits 32: the fp32 moments.
+ *            state_bits 8: m and sqrt(v) as OCP e4m3 codes (one byte each),
+ *            with m_scale and v_scale (fp32, rows x ceil(cols / 256)) holding
+ *            a factor for each run of 256 columns of a row.  All zero bytes
+ *            and scales are the state before the first step.
+ *   decay    weight decay (decoupled) of this tensor */
+typedef struct {
+  int64_t rows, cols;
+  float* W;
+  void* W16;
+  const void* G;
+  int64_t ldg;
+  int32_t g_dtype; /* occ_dtype_t */
+  int32_t rank;
+  const float* P;
+  const float* Q;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  int32_t state_bits; /* 32 or 8 */
+  float decay;
+} occ_param_t;
+
+/* Hyperparameters of a step.  step counts from 1.  seed selects the random
+ * bits that the 8-bit codes are rounded with: another one each step, the same
+ * one on every data-parallel rank; a code depends on seed, the tensor's place
+ * in the list and the element's place in the tensor only.
+ *   grad_scale  device scalar that multiplies every gradient (a clipping
+ *               coefficient, 1 / loss scale), or NULL
+ *   flags       device word, e.g. flags_out of occ_step_batched_noalloc, or
+ *               NULL: when it holds OCC_F_NONFINITE the call changes nothing */
+typedef struct {
+  double lr, beta1, beta2, eps;
+  int64_t step;
+  uint32_t seed;
+  uint32_t reserved;
+  const float* grad_scale;
+  const uint32_t* flags;
+} occ_adamw_t;
+
+/* AdamW over `count` tensors (any mix of gradient and state forms):
+ *   g = grad_scale G, m = beta1 m + (1 - beta1) g, v = beta2 v + (1 - beta2) g^2
+ *   W = W (1 - lr decay) - lr / (1 - beta1^step) m / (sqrt(v / (1 - beta2^step)) + eps)
+ * in fp32.  8-bit moments enter at their stored values, the step uses the new
+ * moments before they are rounded again.  Codes are rounded up with the
+ * probability of the part cut off; a positive v keeps a positive code.  A
+ * non-finite gradient reaches W and the moments of its element (8-bit: of its
+ * run of 256).  No workspace; nothing is copied to the device by itself. */
+occ_status_t occ_adamw_step(const occ_param_t* params, int count, const occ_adamw_t* h,
+                            occ_stream_t stream);
 
 /* Per-kernel timing with HIP events, for benchmarks.  Between
  * occ_profile_begin and occ_profile_end every kernel the library launches is

@@ -2,8 +2,10 @@
 
     python -m paper_2301_09830_amd.build        # or build() from Python
 
-The library is a single translation unit (csrc/api.hip includes the kernel
-templates).  Packed-fp32 VALU instructions are disabled for the device code.
+The library has two translation units: csrc/api.hip (the compressor) and
+csrc/stage_ops.hip (the operators a pipeline stage runs beside it), compiled
+side by side and linked.  Packed-fp32 VALU instructions are disabled for the
+device code.
 """
 
 from __future__ import annotations
@@ -28,14 +30,18 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found (ROCm is required to build liboptcc)")
 
 
-def compile_command(out: str = LIB) -> list:
+SOURCES = ("api.hip", "stage_ops.hip")
+
+
+def compile_command(out: str = LIB, source: str = SOURCES[0]) -> list:
+    """hipcc's command for one translation unit, as a shared library."""
     return [
         hipcc(), f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-shared",
         "-ffp-contract=off",
         "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
         "-Wno-unused-result",
         "-I", INCLUDE, "-I", CSRC,
-        os.path.join(CSRC, "api.hip"),
+        os.path.join(CSRC, source),
         "-o", out,
     ]
 
@@ -43,16 +49,32 @@ def compile_command(out: str = LIB) -> list:
 def build(verbose: bool = False) -> str:
     """Compile liboptcc.so for gfx950 next to this file; returns its path."""
     tmp = LIB + ".tmp"
-    cmd = compile_command(tmp)
-    proc = subprocess.run(cmd, capture_output=True, text=True)
-    noise = "is not a recognized feature for this target"
-    errlines = [ln for ln in proc.stderr.splitlines() if noise not in ln]
-    if proc.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + " ".join(cmd) + "\n" + "\n".join(errlines))
-    if verbose and errlines:
-        print("\n".join(errlines), file=sys.stderr)
+    objects = [LIB + f".{i}.o" for i in range(len(SOURCES))]
+    steps = [[c for c in compile_command(o, src) if c != "-shared"] + ["-c"]
+             for o, src in zip(objects, SOURCES)]
+    try:
+        procs = [subprocess.Popen(cmd, stdout=subprocess.DEVNULL, stderr=subprocess.PIPE, text=True)
+                 for cmd in steps]
+        for proc, cmd, err in [(p, c, p.communicate()[1]) for p, c in zip(procs, steps)]:
+            _report(proc.returncode, cmd, err, verbose)
+        link = [hipcc(), f"--offload-arch={ARCH}", "-fPIC", "-shared", *objects, "-o", tmp]
+        proc = subprocess.run(link, capture_output=True, text=True)
+        _report(proc.returncode, link, proc.stderr, verbose)
+    finally:
+        for o in objects:
+            if os.path.exists(o):
+                os.remove(o)
     os.replace(tmp, LIB)
     return LIB
+
+
+def _report(code: int, cmd: list, err: str, verbose: bool) -> None:
+    noise = "is not a recognized feature for this target"
+    lines = [ln for ln in err.splitlines() if noise not in ln]
+    if code != 0:
+        raise RuntimeError("hipcc failed:\n" + " ".join(cmd) + "\n" + "\n".join(lines))
+    if verbose and lines:
+        print("\n".join(lines), file=sys.stderr)
 
 
 if __name__ == "__main__":

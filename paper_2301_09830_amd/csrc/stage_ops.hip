@@ -1,0 +1,650 @@
+// liboptcc C ABI of the stage operators: linear and gated layers, AdamW.
+// Argument validation, workspace carving and launch sequencing, on the host.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+#include <vector>
+
+#include "host.hpp"
+#include "kernels_adamw.hpp"
+#include "kernels_layer.hpp"
+#include "optcc.h"
+
+using namespace occ;
+
+namespace {
+
+constexpr size_t kWsAlign = 256;        // of the workspace and of each region in it
+constexpr size_t kWsHeader = 256;       // the compressor's numeric flags, left alone
+constexpr int64_t kMaxTokens = (int64_t)1 << 30;
+constexpr int64_t kMaxWidth = (int64_t)1 << 24;   // of in and out
+constexpr int64_t kMaxRowBytes = (int64_t)1 << 26;  // 32 rows are addressed in 31 bits
+
+int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
+int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Regions of a workspace, in order.
+struct Carve {
+  size_t end = kWsHeader;
+  size_t take(size_t bytes) {
+    const size_t at = end;
+    end += (size_t)up((int64_t)bytes, kWsAlign);
+    return at;
+  }
+  size_t total() const { return end == kWsHeader ? 0 : end; }
+};
+
+struct Spans {
+  Span v[12];
+  int n = 0;
+  void add(const void* p, int64_t rows, int64_t cols, int64_t ld, size_t es, bool w) {
+    if (p && rows > 0) v[n++] = span2d(p, rows, cols, ld, es, w);
+  }
+  bool clash() const {
+    for (int i = 0; i < n; ++i)
+      for (int j = i + 1; j < n; ++j)
+        if ((v[i].writable || v[j].writable) && v[i].lo < v[j].hi && v[j].lo < v[i].hi) return true;
+    return false;
+  }
+};
+
+bool ld_ok(int64_t cols, int64_t ld) { return ld >= cols && ld < kMaxDim; }
+
+// ----------------------------------------------------------------------------
+// plan of one tiled product
+// ----------------------------------------------------------------------------
+// Two tiles.  256 x 256 on eight waves (one block a CU) moves the fewest
+// bytes through LDS per product; 128 x 128 on four waves (two blocks a CU)
+// leaves fewer CUs idle when the result is small.  K is split, and the parts
+// joined by a second kernel, where even the small tiles do not fill the chip.
+// The cost of a choice is the rounds of blocks it takes times their length in
+// clocks of one CU.
+struct ProductPlan {
+  bool big = false;
+  int bm = 0, bn = 0;
+  int64_t tiles_m = 0, tiles_n = 0, tiles_k = 0;
+  int splits = 1, k_per_split = 1;
+  size_t part_bytes = 0;
+};
+
+constexpr int kCUs = 256;
+
+ProductPlan plan_product(int64_t m, int64_t width, int64_t k, size_t es) {
+  ProductPlan best;
+  double best_cost = INFINITY;
+  const int64_t tk = div_up(k, kRowBytes / (int64_t)es);
+  for (int big = 0; big < 2; ++big) {
+    const int side = big ? 256 : 128;
+    const int64_t tm = div_up(m, side), tn = div_up(width, side);
+    const int64_t slots = big ? kCUs : 2 * kCUs;
+    const double per_k = (es == 2 ? (big ? 2600.0 : 1700.0) : (big ? 17000.0 : 8600.0));
+    for (int s = 1; s <= 16; s *= 2) {
+      if (s > 1 && tk < 4 * s) break;
+      const int64_t kps = div_up(tk, s), sp = div_up(tk, kps);
+      const double rounds = (double)div_up(tm * tn * sp, slots);
+      double cost = rounds * ((double)kps * per_k + 8000.0);
+      const double part = (double)sp * (double)m * (double)width * 4.0;
+      if (sp > 1) {
+        if (part > 512e6) break;
+        cost += 2.0 * part / 2000.0 + 8000.0;   // bytes a clock of the whole chip; a launch
+      }
+      if (cost < best_cost) {
+        best_cost = cost;
+        best.big = big != 0;
+        best.bm = best.bn = side;
+        best.tiles_m = tm;
+        best.tiles_n = tn;
+        best.tiles_k = tk;
+        best.splits = (int)sp;
+        best.k_per_split = (int)kps;
+        best.part_bytes = sp > 1 ? (size_t)part : 0;
+      }
+    }
+  }
+  return best;
+}
+
+bool grid_fits(const ProductPlan& p) {
+  return p.tiles_m * p.tiles_n < ((int64_t)1 << 26) && p.tiles_k < ((int64_t)1 << 24);
+}
+
+template <class T, bool AKS, bool BKS, int EP>
+occ_status_t run_product(const char* name, const ProductPlan& p, GemmArgs g, char* ws, size_t part_off, hipStream_t s) {
+  g.tiles_m = (int32_t)p.tiles_m;
+  g.tiles_n = (int32_t)p.tiles_n;
+  g.tiles_k = (int32_t)p.tiles_k;
+  g.splits = p.splits;
+  g.k_per_split = p.k_per_split;
+  g.part = p.splits > 1 ? (float*)(ws + part_off) : nullptr;
+  const unsigned grid = (unsigned)(p.tiles_m * p.tiles_n * p.splits);
+  OCC_TRY(launch(name, s, [&] {
+    if (p.big)
+      hipLaunchKernelGGL((k_gemm<T, 2, 4, 8, 4, AKS, BKS, EP, true>), dim3(grid), dim3(512), 0, s, g);
+    else
+      hipLaunchKernelGGL((k_gemm<T, 2, 2, 4, 4, AKS, BKS, EP, false>), dim3(grid), dim3(256), 0, s, g);
+  }));
+  if (p.splits == 1) return OCC_OK;
+  const int64_t quads = (int64_t)g.M * div_up(g.N, 4);
+  return launch("gemm_join", s, [&] {
+    hipLaunchKernelGGL((k_gemm_join<T, EP>), dim3((unsigned)std::min<int64_t>(div_up(quads, 256), 4096)), dim3(256), 0,
+                       s, g);
+  });
+}
+
+// An operand the tiled product cannot take in place: rows off 16 bytes, rows
+// that end inside a piece, or rows too far apart.
+bool needs_copy(const void* p, int64_t ld, int64_t cols, size_t es) {
+  return !aligned(p, 16) || (size_t)ld * es % 16 || (size_t)cols * es % 16 || ld * (int64_t)es >= kMaxRowBytes;
+}
+
+int64_t piece_ld(int64_t cols, size_t es) { return up(cols, 16 / (int64_t)es); }
+
+template <class T>
+occ_status_t copy_operand(const void* src, int64_t ld, int64_t rows, int64_t cols, char* dst, hipStream_t s) {
+  const int64_t pieces = piece_ld(cols, sizeof(T)) * (int64_t)sizeof(T) / 16;
+  const int64_t blocks = std::min<int64_t>(div_up(rows * pieces, 256), 8192);
+  return launch("align_rows", s, [&] {
+    hipLaunchKernelGGL((k_align_rows<T>), dim3((unsigned)blocks), dim3(256), 0, s, (const T*)src, ld, (T*)dst, rows,
+                       (int)cols, (int)pieces);
+  });
+}
+
+// ----------------------------------------------------------------------------
+// forward
+// ----------------------------------------------------------------------------
+// Up to this many tokens the weights are streamed through registers.
+constexpr int64_t kFewTokens = 64;
+
+struct FwdPlan {
+  bool few = false, copy_x = false, copy_w = false;
+  size_t x_off = 0, w_off = 0, part_off = 0, bytes = 0;
+  ProductPlan prod;
+};
+
+occ_status_t check_fwd(const occ_linear_t* l, bool gated) {
+  if (!l) return OCC_E_NULL;
+  if (l->dtype != OCC_F32 && l->dtype != OCC_BF16) return OCC_E_DTYPE;
+  if (l->act < OCC_ACT_NONE || l->act > OCC_ACT_SILU) return OCC_E_VALUE;
+  if (l->tokens < 0 || l->tokens >= kMaxTokens || l->in < 1 || l->in > kMaxWidth || l->out < 1 || l->out > kMaxWidth)
+    return OCC_E_SHAPE;
+  const int64_t wide = gated ? 2 * l->out : l->out;
+  if (!ld_ok(l->in, l->ldx) || !ld_ok(l->in, l->ldw) || !ld_ok(l->out, l->ldy)) return OCC_E_SHAPE;
+  if ((l->R && !ld_ok(l->out, l->ldr)) || (l->Z && !ld_ok(wide, l->ldz))) return OCC_E_SHAPE;
+  return OCC_OK;
+}
+
+occ_status_t plan_fwd(const occ_linear_t& l, bool gated, FwdPlan& f) {
+  if (l.tokens == 0) return OCC_OK;
+  f.few = l.tokens <= kFewTokens;
+  if (f.few) return OCC_OK;
+  const size_t es = elem_size(l.dtype);
+  const int64_t wide = gated ? 2 * l.out : l.out;
+  f.copy_x = needs_copy(l.X, l.ldx, l.in, es);
+  f.copy_w = needs_copy(l.W, l.ldw, l.in, es);
+  f.prod = plan_product(l.tokens, wide, l.in, es);
+  if (gated) f.prod.tiles_n = div_up(l.out, f.prod.bn / 2);
+  if (!grid_fits(f.prod)) return OCC_E_SHAPE;
+  Carve c;
+  const size_t row = (size_t)piece_ld(l.in, es) * es;
+  if (f.copy_x) f.x_off = c.take((size_t)l.tokens * row);
+  if (f.copy_w) f.w_off = c.take((size_t)wide * row);
+  if (f.prod.splits > 1) f.part_off = c.take(f.prod.part_bytes);
+  f.bytes = c.total();
+  return OCC_OK;
+}
+
+template <class T, bool GATED>
+occ_status_t run_fwd(const occ_linear_t& l, const FwdPlan& f, char* ws, hipStream_t s) {
+  FwdEpi e{};
+  e.Y = l.Y;
+  e.ldy = l.ldy;
+  e.Z = l.Z;
+  e.ldz = l.ldz;
+  e.R = l.R;
+  e.ldr = l.ldr;
+  e.bias = l.bias;
+  e.act = l.act;
+  e.out = (int32_t)l.out;
+  if (f.few) {
+    SkinnyArgs g{};
+    g.X = l.X;
+    g.W = l.W;
+    g.ldx = l.ldx;
+    g.ldw = l.ldw;
+    g.tokens = (int32_t)l.tokens;
+    g.in = (int32_t)l.in;
+    g.fwd = e;
+    const dim3 grid((unsigned)div_up(l.out, 16)), block(SK_WAVES * 64);
+    return launch(GATED ? "gated_few" : "linear_few", s, [&] {
+      if (l.tokens <= 16) hipLaunchKernelGGL((k_skinny<T, 1, GATED>), grid, block, 0, s, g);
+      else if (l.tokens <= 32) hipLaunchKernelGGL((k_skinny<T, 2, GATED>), grid, block, 0, s, g);
+      else hipLaunchKernelGGL((k_skinny<T, 4, GATED>), grid, block, 0, s, g);
+    });
+  }
+  GemmArgs g{};
+  g.A = l.X;
+  g.lda = l.ldx;
+  g.B = l.W;
+  g.ldb = l.ldw;
+  const int64_t wide = GATED ? 2 * l.out : l.out;
+  if (f.copy_x) {
+    OCC_TRY(copy_operand<T>(l.X, l.ldx, l.tokens, l.in, ws + f.x_off, s));
+    g.A = ws + f.x_off;
+    g.lda = piece_ld(l.in, sizeof(T));
+  }
+  if (f.copy_w) {
+    OCC_TRY(copy_operand<T>(l.W, l.ldw, wide, l.in, ws + f.w_off, s));
+    g.B = ws + f.w_off;
+    g.ldb = piece_ld(l.in, sizeof(T));
+  }
+  g.M = (int32_t)l.tokens;
+  g.N = (int32_t)l.out;
+  g.ka = g.kb = (int32_t)piece_ld(l.in, sizeof(T));
+  g.fwd = e;
+  return run_product<T, false, false, GATED ? EP_GATED : EP_FWD>(GATED ? "gated_fwd" : "linear_fwd", f.prod, g, ws,
+                                                                 f.part_off, s);
+}
+
+occ_status_t check_ws(const void* ws, size_t ws_bytes, size_t need) {
+  if (!need) return OCC_OK;
+  return !ws || !aligned(ws, kWsAlign) || ws_bytes < need ? OCC_E_WORKSPACE : OCC_OK;
+}
+
+template <bool GATED>
+occ_status_t forward(const occ_linear_t* lp, void* ws, size_t ws_bytes, occ_stream_t stream) {
+  OCC_TRY(check_fwd(lp, GATED));
+  const occ_linear_t& l = *lp;
+  if (l.tokens == 0) return OCC_OK;
+  if (!l.X || !l.W || !l.Y) return OCC_E_NULL;
+  const size_t es = elem_size(l.dtype);
+  if (!aligned(l.X, es) || !aligned(l.W, es) || !aligned(l.Y, es) || !aligned(l.R, es) || !aligned(l.Z, es) ||
+      !aligned(l.bias, 4))
+    return OCC_E_ALIGN;
+  FwdPlan f;
+  OCC_TRY(plan_fwd(l, GATED, f));
+  OCC_TRY(check_ws(ws, ws_bytes, f.bytes));
+  const int64_t wide = GATED ? 2 * l.out : l.out;
+  Spans sp;
+  sp.add(l.X, l.tokens, l.in, l.ldx, es, false);
+  sp.add(l.W, wide, l.in, l.ldw, es, false);
+  sp.add(l.bias, 1, wide, wide, 4, false);
+  sp.add(l.Y, l.tokens, l.out, l.ldy, es, true);
+  sp.add(l.Z, l.tokens, wide, l.ldz, es, true);
+  if (l.R && (l.R != l.Y || l.ldr != l.ldy)) sp.add(l.R, l.tokens, l.out, l.ldr, es, false);
+  if (f.bytes) sp.add(ws, 1, (int64_t)f.bytes, (int64_t)f.bytes, 1, true);
+  if (sp.clash()) return OCC_E_ALIAS;
+  hipStream_t s = (hipStream_t)stream;
+  return l.dtype == OCC_BF16 ? run_fwd<uint16_t, GATED>(l, f, (char*)ws, s) : run_fwd<float, GATED>(l, f, (char*)ws, s);
+}
+
+// ----------------------------------------------------------------------------
+// backward
+// ----------------------------------------------------------------------------
+struct BwdPlan {
+  bool has_dz = false;    // dZ is made (else it is dY)
+  bool copy_dy = false, copy_x = false, copy_w = false;
+  int64_t strip = 0, strips = 0;
+  size_t dz_off = 0, bias_off = 0, x_off = 0, w_off = 0, part_off = 0, bytes = 0;
+  int64_t ldd = 0;
+  ProductPlan dx, dw;
+};
+
+occ_status_t check_bwd(const occ_linear_grad_t* l, bool gated) {
+  if (!l) return OCC_E_NULL;
+  if (l->dtype != OCC_F32 && l->dtype != OCC_BF16) return OCC_E_DTYPE;
+  if (l->dw_dtype != l->dtype && l->dw_dtype != OCC_F32) return OCC_E_DTYPE;
+  if (l->act < OCC_ACT_NONE || l->act > OCC_ACT_SILU) return OCC_E_VALUE;
+  if (l->tokens < 0 || l->tokens >= kMaxTokens || l->in < 1 || l->in > kMaxWidth || l->out < 1 || l->out > kMaxWidth)
+    return OCC_E_SHAPE;
+  const int64_t wide = gated ? 2 * l->out : l->out;
+  const bool z = gated || l->act != OCC_ACT_NONE;
+  if (!l->dX && !l->dW && !l->dbias) return OCC_E_NULL;
+  if (!ld_ok(l->out, l->lddy) || (z && !ld_ok(wide, l->ldz))) return OCC_E_SHAPE;
+  if (l->dX && (!ld_ok(l->in, l->lddx) || !ld_ok(l->in, l->ldw))) return OCC_E_SHAPE;
+  if (l->dW && (!ld_ok(l->in, l->lddw) || !ld_ok(l->in, l->ldx))) return OCC_E_SHAPE;
+  return OCC_OK;
+}
+
+occ_status_t plan_bwd(const occ_linear_grad_t& l, bool gated, BwdPlan& f) {
+  if (l.tokens == 0) return OCC_OK;
+  const size_t es = elem_size(l.dtype);
+  const int64_t wide = gated ? 2 * l.out : l.out;
+  const bool prod = l.dX || l.dW;
+  const bool act = gated || l.act != OCC_ACT_NONE;
+  f.has_dz = act && prod;
+  f.ldd = piece_ld(wide, es);
+  Carve c;
+  if (f.has_dz) {
+    f.dz_off = c.take((size_t)l.tokens * f.ldd * es);
+  } else if (prod && needs_copy(l.dY, l.lddy, l.out, es)) {
+    f.copy_dy = true;
+    f.dz_off = c.take((size_t)l.tokens * f.ldd * es);
+  }
+  if (f.has_dz || l.dbias) {
+    // enough blocks to fill the chip several times, whole groups of rows in each
+    const int64_t across = div_up(l.out, DZ_LANES * 4);
+    const int64_t down = std::max<int64_t>(1, std::min<int64_t>(div_up(4096, across), div_up(l.tokens, DZ_ROWS)));
+    f.strip = up(div_up(l.tokens, down), DZ_ROWS);
+    f.strips = div_up(l.tokens, f.strip);
+    if (l.dbias) f.bias_off = c.take((size_t)f.strips * wide * 4);
+  }
+  size_t part = 0;
+  if (l.dX) {
+    f.copy_w = needs_copy(l.W, l.ldw, l.in, es);
+    if (f.copy_w) f.w_off = c.take((size_t)wide * piece_ld(l.in, es) * es);
+    f.dx = plan_product(l.tokens, l.in, wide, es);
+    if (!grid_fits(f.dx)) return OCC_E_SHAPE;
+    part = f.dx.part_bytes;
+  }
+  if (l.dW) {
+    f.copy_x = needs_copy(l.X, l.ldx, l.in, es);
+    if (f.copy_x) f.x_off = c.take((size_t)l.tokens * piece_ld(l.in, es) * es);
+    f.dw = plan_product(wide, l.in, l.tokens, es);
+    if (!grid_fits(f.dw)) return OCC_E_SHAPE;
+    part = std::max(part, f.dw.part_bytes);
+  }
+  if (part) f.part_off = c.take(part);   // one product after the other
+  f.bytes = c.total();
+  return OCC_OK;
+}
+
+template <class T, bool GATED>
+occ_status_t run_bwd(const occ_linear_grad_t& l, const BwdPlan& f, bool accumulate, char* ws, hipStream_t s) {
+  const int64_t wide = GATED ? 2 * l.out : l.out;
+  const bool act = GATED || l.act != OCC_ACT_NONE;
+  if (f.strips) {
+    DzArgs d{};
+    d.dY = l.dY;
+    d.ldy = l.lddy;
+    d.Z = act ? l.Z : nullptr;
+    d.ldz = l.ldz;
+    d.dZ = f.has_dz ? ws + f.dz_off : nullptr;
+    d.ldd = f.ldd;
+    d.bias_part = l.dbias ? (float*)(ws + f.bias_off) : nullptr;
+    d.tokens = (int32_t)l.tokens;
+    d.out = (int32_t)l.out;
+    d.act = l.act;
+    d.strip = (int32_t)f.strip;
+    OCC_TRY(launch("dz", s, [&] {
+      hipLaunchKernelGGL((k_dz<T, GATED>), dim3((unsigned)div_up(l.out, DZ_LANES * 4), (unsigned)f.strips), dim3(256),
+                         0, s, d);
+    }));
+    if (l.dbias)
+      OCC_TRY(launch("dz_bias", s, [&] {
+        hipLaunchKernelGGL(k_dz_bias, dim3((unsigned)div_up(wide, 256)), dim3(256), 0, s, (const float*)d.bias_part,
+                           (int)f.strips, wide, l.dbias, accumulate ? 1 : 0);
+      }));
+  }
+  const void* dz = l.dY;
+  int64_t ldd = l.lddy;
+  if (f.has_dz || f.copy_dy) {
+    dz = ws + f.dz_off;
+    ldd = f.ldd;
+  }
+  if (f.copy_dy) OCC_TRY(copy_operand<T>(l.dY, l.lddy, l.tokens, l.out, ws + f.dz_off, s));
+  if (l.dX) {
+    GemmArgs g{};
+    g.A = dz;
+    g.lda = ldd;
+    g.B = l.W;
+    g.ldb = l.ldw;
+    if (f.copy_w) {
+      OCC_TRY(copy_operand<T>(l.W, l.ldw, wide, l.in, ws + f.w_off, s));
+      g.B = ws + f.w_off;
+      g.ldb = piece_ld(l.in, sizeof(T));
+    }
+    g.M = (int32_t)l.tokens;
+    g.N = (int32_t)l.in;
+    g.ka = (int32_t)f.ldd;
+    g.kb = (int32_t)wide;
+    g.C = l.dX;
+    g.ldc = l.lddx;
+    OCC_TRY((run_product<T, false, true, EP_STORE>("dgrad", f.dx, g, ws, f.part_off, s)));
+  }
+  if (l.dW) {
+    GemmArgs g{};
+    g.A = dz;
+    g.lda = ldd;
+    g.B = l.X;
+    g.ldb = l.ldx;
+    if (f.copy_x) {
+      OCC_TRY(copy_operand<T>(l.X, l.ldx, l.tokens, l.in, ws + f.x_off, s));
+      g.B = ws + f.x_off;
+      g.ldb = piece_ld(l.in, sizeof(T));
+    }
+    g.M = (int32_t)wide;
+    g.N = (int32_t)l.in;
+    g.ka = g.kb = (int32_t)l.tokens;
+    g.C = l.dW;
+    g.ldc = l.lddw;
+    g.c_f32 = l.dw_dtype == OCC_F32;
+    g.accumulate = accumulate;
+    OCC_TRY((run_product<T, true, true, EP_STORE>("wgrad", f.dw, g, ws, f.part_off, s)));
+  }
+  return OCC_OK;
+}
+
+template <class T>
+occ_status_t zero_rows(void* p, int64_t rows, int64_t cols, int64_t ld, hipStream_t s) {
+  return launch("zero_grad", s, [&] {
+    hipLaunchKernelGGL((k_zero_rows<T>), dim3((unsigned)std::min<int64_t>(div_up(rows * cols, 256), 8192)), dim3(256),
+                       0, s, (T*)p, rows, (int)cols, ld);
+  });
+}
+
+template <bool GATED>
+occ_status_t backward(const occ_linear_grad_t* lp, unsigned flags, void* ws, size_t ws_bytes, occ_stream_t stream) {
+  OCC_TRY(check_bwd(lp, GATED));
+  if (flags & ~(unsigned)OCC_GRAD_ACCUMULATE) return OCC_E_FLAGS;
+  const occ_linear_grad_t& l = *lp;
+  const bool accumulate = flags & OCC_GRAD_ACCUMULATE;
+  const size_t es = elem_size(l.dtype), ws_es = elem_size(l.dw_dtype);
+  const int64_t wide = GATED ? 2 * l.out : l.out;
+  const bool act = GATED || l.act != OCC_ACT_NONE;
+  if (!aligned(l.dY, es) || !aligned(l.X, es) || !aligned(l.W, es) || !aligned(l.Z, es) || !aligned(l.dX, es) ||
+      !aligned(l.dW, ws_es) || !aligned(l.dbias, 4))
+    return OCC_E_ALIGN;
+  hipStream_t s = (hipStream_t)stream;
+  BwdPlan f;
+  if (l.tokens > 0) {
+    if (!l.dY || (act && !l.Z) || (l.dX && !l.W) || (l.dW && !l.X)) return OCC_E_NULL;
+    OCC_TRY(plan_bwd(l, GATED, f));
+    OCC_TRY(check_ws(ws, ws_bytes, f.bytes));
+  }
+  Spans sp;
+  sp.add(l.dY, l.tokens, l.out, l.lddy, es, false);
+  if (act) sp.add(l.Z, l.tokens, wide, l.ldz, es, false);
+  if (l.dW) sp.add(l.X, l.tokens, l.in, l.ldx, es, false);
+  if (l.dX) sp.add(l.W, wide, l.in, l.ldw, es, false);
+  sp.add(l.dX, l.tokens, l.in, l.lddx, es, true);
+  sp.add(l.dW, wide, l.in, l.lddw, ws_es, true);
+  sp.add(l.dbias, 1, wide, wide, 4, true);
+  if (f.bytes) sp.add(ws, 1, (int64_t)f.bytes, (int64_t)f.bytes, 1, true);
+  if (sp.clash()) return OCC_E_ALIAS;
+  if (l.tokens == 0) {
+    if (accumulate) return OCC_OK;
+    if (l.dW) OCC_TRY(ws_es == 2 ? zero_rows<uint16_t>(l.dW, wide, l.in, l.lddw, s)
+                                 : zero_rows<float>(l.dW, wide, l.in, l.lddw, s));
+    return l.dbias ? zero_rows<float>(l.dbias, 1, wide, wide, s) : OCC_OK;
+  }
+  return l.dtype == OCC_BF16 ? run_bwd<uint16_t, GATED>(l, f, accumulate, (char*)ws, s)
+                             : run_bwd<float, GATED>(l, f, accumulate, (char*)ws, s);
+}
+
+// ----------------------------------------------------------------------------
+// AdamW
+// ----------------------------------------------------------------------------
+enum AdamKind { AK_F32_32, AK_BF16_32, AK_F32_8, AK_BF16_8, AK_FACTORS_32, AK_FACTORS_8, AK_NUM };
+
+AdamKind kind_of(const occ_param_t& p) {
+  if (!p.G) return p.state_bits == 32 ? AK_FACTORS_32 : AK_FACTORS_8;
+  if (p.state_bits == 32) return p.g_dtype == OCC_BF16 ? AK_BF16_32 : AK_F32_32;
+  return p.g_dtype == OCC_BF16 ? AK_BF16_8 : AK_F32_8;
+}
+
+int64_t adam_blocks(const occ_param_t& p) {
+  const int64_t per_row = div_up(p.cols, kRun);
+  if (!p.G) return div_up(p.rows, ADF_ROWS) * per_row;
+  return p.state_bits == 32 ? div_up(p.rows * p.cols, AD_BLOCK) : div_up(p.rows * per_row, AD8_BLOCK);
+}
+
+occ_status_t check_param(const occ_param_t& p, std::vector<Span>& spans) {
+  if (p.rows < 1 || p.cols < 1 || p.rows >= kMaxTokens || p.cols >= kMaxTokens ||
+      p.rows * p.cols >= ((int64_t)1 << 42) || adam_blocks(p) >= kMaxTokens)
+    return OCC_E_SHAPE;
+  if (p.state_bits != 32 && p.state_bits != 8) return OCC_E_VALUE;
+  if (!std::isfinite(p.decay)) return OCC_E_VALUE;
+  if (!p.W || !p.m || !p.v || (p.state_bits == 8 && (!p.m_scale || !p.v_scale))) return OCC_E_NULL;
+  const size_t ss = p.state_bits == 32 ? 4 : 1;
+  const int64_t per_row = div_up(p.cols, kRun);
+  if (!aligned(p.W, 4) || !aligned(p.W16, 2) || !aligned(p.m, ss) || !aligned(p.v, ss)) return OCC_E_ALIGN;
+  if (p.G) {
+    if (p.g_dtype != OCC_F32 && p.g_dtype != OCC_BF16) return OCC_E_DTYPE;
+    if (!ld_ok(p.cols, p.ldg)) return OCC_E_SHAPE;
+    if (!aligned(p.G, elem_size(p.g_dtype))) return OCC_E_ALIGN;
+    spans.push_back(span2d(p.G, p.rows, p.cols, p.ldg, elem_size(p.g_dtype), false));
+  } else {
+    if (!p.P || !p.Q) return OCC_E_NULL;
+    if (p.rank < 1 || p.rank > OCC_MAX_RANK) return OCC_E_RANK;
+    if (!aligned(p.P, 4) || !aligned(p.Q, 4)) return OCC_E_ALIGN;
+    spans.push_back(span2d(p.P, p.rows, p.rank, p.rank, 4, false));
+    spans.push_back(span2d(p.Q, p.cols, p.rank, p.rank, 4, false));
+  }
+  spans.push_back(span2d(p.W, p.rows, p.cols, p.cols, 4, true));
+  if (p.W16) spans.push_back(span2d(p.W16, p.rows, p.cols, p.cols, 2, true));
+  spans.push_back(span2d(p.m, p.rows, p.cols, p.cols, ss, true));
+  spans.push_back(span2d(p.v, p.rows, p.cols, p.cols, ss, true));
+  if (p.state_bits == 8) {
+    if (!aligned(p.m_scale, 4) || !aligned(p.v_scale, 4)) return OCC_E_ALIGN;
+    spans.push_back(span2d(p.m_scale, p.rows, per_row, per_row, 4, true));
+    spans.push_back(span2d(p.v_scale, p.rows, per_row, per_row, 4, true));
+  }
+  return OCC_OK;
+}
+
+occ_status_t launch_adam(AdamKind kind, const AdamArgs& a, int64_t blocks, hipStream_t s) {
+  const dim3 grid((unsigned)blocks), block(256);
+  return launch("adamw", s, [&] {
+    switch (kind) {
+      case AK_F32_32: hipLaunchKernelGGL((k_adamw32<float>), grid, block, 0, s, a); break;
+      case AK_BF16_32: hipLaunchKernelGGL((k_adamw32<uint16_t>), grid, block, 0, s, a); break;
+      case AK_F32_8: hipLaunchKernelGGL((k_adamw8<float>), grid, block, 0, s, a); break;
+      case AK_BF16_8: hipLaunchKernelGGL((k_adamw8<uint16_t>), grid, block, 0, s, a); break;
+      case AK_FACTORS_32: hipLaunchKernelGGL((k_adamw_factors<32>), grid, block, 0, s, a); break;
+      default: hipLaunchKernelGGL((k_adamw_factors<8>), grid, block, 0, s, a); break;
+    }
+  });
+}
+
+occ_status_t adamw(const occ_param_t* params, int count, const occ_adamw_t* h, hipStream_t s) {
+  if (count < 1) return OCC_E_SHAPE;
+  if (!params || !h) return OCC_E_NULL;
+  if (!std::isfinite(h->lr) || !(h->beta1 >= 0.0 && h->beta1 < 1.0) || !(h->beta2 >= 0.0 && h->beta2 < 1.0) ||
+      !(h->eps >= 0.0 && std::isfinite(h->eps)) || h->step < 1)
+    return OCC_E_VALUE;
+  if (!aligned(h->grad_scale, 4) || !aligned(h->flags, 4)) return OCC_E_ALIGN;
+  std::vector<Span> spans;
+  spans.reserve((size_t)count * 8 + 2);
+  for (int j = 0; j < count; ++j) OCC_TRY(check_param(params[j], spans));
+  if (h->grad_scale) spans.push_back({(uintptr_t)h->grad_scale, (uintptr_t)h->grad_scale + 4, false});
+  if (h->flags) spans.push_back({(uintptr_t)h->flags, (uintptr_t)h->flags + 4, false});
+  if (overlaps(std::move(spans))) return OCC_E_ALIAS;
+  AdamArgs a{};
+  a.b1 = (float)h->beta1;
+  a.c1 = (float)(1.0 - h->beta1);
+  a.b2 = (float)h->beta2;
+  a.c2 = (float)(1.0 - h->beta2);
+  a.a = (float)(h->lr / (1.0 - std::pow(h->beta1, (double)h->step)));
+  a.c = (float)(1.0 / std::sqrt(1.0 - std::pow(h->beta2, (double)h->step)));
+  a.eps = (float)h->eps;
+  a.grad_scale = h->grad_scale;
+  a.flags = h->flags;
+  for (int kind = 0; kind < AK_NUM; ++kind) {
+    int64_t blocks = 0;
+    a.count = 0;
+    for (int j = 0; j < count; ++j) {
+      const occ_param_t& p = params[j];
+      if (kind_of(p) != kind) continue;
+      const int64_t nb = adam_blocks(p);
+      if (a.count == kAdamTensors || blocks + nb >= kMaxTokens) {
+        OCC_TRY(launch_adam((AdamKind)kind, a, blocks, s));
+        a.count = 0;
+        blocks = 0;
+      }
+      AdamTensor& t = a.t[a.count++];
+      t.W = p.W;
+      t.W16 = (uint16_t*)p.W16;
+      t.G = p.G;
+      t.P = p.P;
+      t.Q = p.Q;
+      t.m = p.m;
+      t.v = p.v;
+      t.m_scale = p.m_scale;
+      t.v_scale = p.v_scale;
+      t.ldg = p.ldg;
+      t.rows = (int32_t)p.rows;
+      t.cols = (int32_t)p.cols;
+      t.rank = p.rank;
+      t.block0 = (int32_t)blocks;
+      t.keep = (float)(1.0 - h->lr * (double)p.decay);
+      t.key = (h->seed + (uint32_t)j * 0x6A09E667u) * 0xBB67AE85u;
+      blocks += nb;
+    }
+    if (a.count) OCC_TRY(launch_adam((AdamKind)kind, a, blocks, s));
+  }
+  return OCC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t occ_linear_fwd_workspace_bytes(const occ_linear_t* l) {
+  FwdPlan f;
+  return check_fwd(l, false) == OCC_OK && plan_fwd(*l, false, f) == OCC_OK ? f.bytes : 0;
+}
+
+size_t occ_gated_fwd_workspace_bytes(const occ_linear_t* l) {
+  FwdPlan f;
+  return check_fwd(l, true) == OCC_OK && plan_fwd(*l, true, f) == OCC_OK ? f.bytes : 0;
+}
+
+size_t occ_linear_bwd_workspace_bytes(const occ_linear_grad_t* l) {
+  BwdPlan f;
+  return check_bwd(l, false) == OCC_OK && plan_bwd(*l, false, f) == OCC_OK ? f.bytes : 0;
+}
+
+size_t occ_gated_bwd_workspace_bytes(const occ_linear_grad_t* l) {
+  BwdPlan f;
+  return check_bwd(l, true) == OCC_OK && plan_bwd(*l, true, f) == OCC_OK ? f.bytes : 0;
+}
+
+occ_status_t occ_linear_fwd(const occ_linear_t* l, void* ws, size_t ws_bytes, occ_stream_t stream) {
+  return forward<false>(l, ws, ws_bytes, stream);
+}
+
+occ_status_t occ_gated_fwd(const occ_linear_t* l, void* ws, size_t ws_bytes, occ_stream_t stream) {
+  return forward<true>(l, ws, ws_bytes, stream);
+}
+
+occ_status_t occ_linear_bwd(const occ_linear_grad_t* l, unsigned flags, void* ws, size_t ws_bytes,
+                            occ_stream_t stream) {
+  return backward<false>(l, flags, ws, ws_bytes, stream);
+}
+
+occ_status_t occ_gated_bwd(const occ_linear_grad_t* l, unsigned flags, void* ws, size_t ws_bytes,
+                           occ_stream_t stream) {
+  return backward<true>(l, flags, ws, ws_bytes, stream);
+}
+
+occ_status_t occ_adamw_step(const occ_param_t* params, int count, const occ_adamw_t* h, occ_stream_t stream) {
+  try {
+    return adamw(params, count, h, (hipStream_t)stream);
+  } catch (...) {   // no memory for the list of spans
+    return OCC_E_HIP;
+  }
+}
+
+}  // extern "C"

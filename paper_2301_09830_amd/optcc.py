@@ -29,11 +29,14 @@ OCC_DEC_SPLIT_BF16, OCC_DEC_OUT_BF16 = 1, 2
 OCC_MAX_RANK = 128
 OCC_NOALLOC_MAX_BYTES = 64 << 20
 OCC_MAX_ITERS = 64
+OCC_ACT_NONE, OCC_ACT_RELU, OCC_ACT_GELU, OCC_ACT_GELU_TANH, OCC_ACT_SILU = range(5)
+OCC_GRAD_ACCUMULATE = 1
+OCC_SCALE_RUN = 256   # columns that share one scale of an 8-bit moment
 
 STATUS_NAMES = {
     0: "OCC_OK", 1: "OCC_E_NULL", 2: "OCC_E_SHAPE", 3: "OCC_E_RANK", 4: "OCC_E_ITERS",
     5: "OCC_E_DTYPE", 6: "OCC_E_ALIGN", 7: "OCC_E_ALIAS", 8: "OCC_E_WORKSPACE",
-    9: "OCC_E_HIP", 10: "OCC_E_FLAGS",
+    9: "OCC_E_HIP", 10: "OCC_E_FLAGS", 11: "OCC_E_VALUE",
 }
 
 
@@ -78,6 +81,87 @@ class occ_kernel_time_t(ctypes.Structure):
         ("launches", ctypes.c_int32),
         ("reserved", ctypes.c_int32),
         ("total_ms", ctypes.c_double),
+    ]
+
+
+class occ_linear_t(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("act", ctypes.c_int32),
+        ("tokens", ctypes.c_int64),
+        ("in_", ctypes.c_int64),
+        ("out", ctypes.c_int64),
+        ("X", ctypes.c_void_p),
+        ("ldx", ctypes.c_int64),
+        ("W", ctypes.c_void_p),
+        ("ldw", ctypes.c_int64),
+        ("bias", ctypes.c_void_p),
+        ("R", ctypes.c_void_p),
+        ("ldr", ctypes.c_int64),
+        ("Z", ctypes.c_void_p),
+        ("ldz", ctypes.c_int64),
+        ("Y", ctypes.c_void_p),
+        ("ldy", ctypes.c_int64),
+    ]
+
+
+class occ_linear_grad_t(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("dw_dtype", ctypes.c_int32),
+        ("act", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("tokens", ctypes.c_int64),
+        ("in_", ctypes.c_int64),
+        ("out", ctypes.c_int64),
+        ("dY", ctypes.c_void_p),
+        ("lddy", ctypes.c_int64),
+        ("X", ctypes.c_void_p),
+        ("ldx", ctypes.c_int64),
+        ("W", ctypes.c_void_p),
+        ("ldw", ctypes.c_int64),
+        ("Z", ctypes.c_void_p),
+        ("ldz", ctypes.c_int64),
+        ("dX", ctypes.c_void_p),
+        ("lddx", ctypes.c_int64),
+        ("dW", ctypes.c_void_p),
+        ("lddw", ctypes.c_int64),
+        ("dbias", ctypes.c_void_p),
+    ]
+
+
+class occ_param_t(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int64),
+        ("cols", ctypes.c_int64),
+        ("W", ctypes.c_void_p),
+        ("W16", ctypes.c_void_p),
+        ("G", ctypes.c_void_p),
+        ("ldg", ctypes.c_int64),
+        ("g_dtype", ctypes.c_int32),
+        ("rank", ctypes.c_int32),
+        ("P", ctypes.c_void_p),
+        ("Q", ctypes.c_void_p),
+        ("m", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("m_scale", ctypes.c_void_p),
+        ("v_scale", ctypes.c_void_p),
+        ("state_bits", ctypes.c_int32),
+        ("decay", ctypes.c_float),
+    ]
+
+
+class occ_adamw_t(ctypes.Structure):
+    _fields_ = [
+        ("lr", ctypes.c_double),
+        ("beta1", ctypes.c_double),
+        ("beta2", ctypes.c_double),
+        ("eps", ctypes.c_double),
+        ("step", ctypes.c_int64),
+        ("seed", ctypes.c_uint32),
+        ("reserved", ctypes.c_uint32),
+        ("grad_scale", ctypes.c_void_p),
+        ("flags", ctypes.c_void_p),
     ]
 
 
@@ -127,6 +211,20 @@ _SIGS = {
     "occ_sc_select": (ctypes.c_int, [ctypes.POINTER(occ_stage_t), ctypes.c_int, ctypes.c_int,
                                      ctypes.POINTER(ctypes.c_uint8), ctypes.POINTER(ctypes.c_int),
                                      ctypes.POINTER(ctypes.c_double)]),
+    "occ_linear_fwd_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(occ_linear_t)]),
+    "occ_gated_fwd_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(occ_linear_t)]),
+    "occ_linear_bwd_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(occ_linear_grad_t)]),
+    "occ_gated_bwd_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(occ_linear_grad_t)]),
+    "occ_linear_fwd": (ctypes.c_int, [ctypes.POINTER(occ_linear_t), ctypes.c_void_p,
+                                      ctypes.c_size_t, ctypes.c_void_p]),
+    "occ_gated_fwd": (ctypes.c_int, [ctypes.POINTER(occ_linear_t), ctypes.c_void_p,
+                                     ctypes.c_size_t, ctypes.c_void_p]),
+    "occ_linear_bwd": (ctypes.c_int, [ctypes.POINTER(occ_linear_grad_t), ctypes.c_uint,
+                                      ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "occ_gated_bwd": (ctypes.c_int, [ctypes.POINTER(occ_linear_grad_t), ctypes.c_uint,
+                                     ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "occ_adamw_step": (ctypes.c_int, [ctypes.POINTER(occ_param_t), ctypes.c_int,
+                                      ctypes.POINTER(occ_adamw_t), ctypes.c_void_p]),
     "occ_profile_begin": (ctypes.c_int, []),
     "occ_profile_end": (ctypes.c_int, [ctypes.POINTER(occ_kernel_time_t), ctypes.c_int,
                                        ctypes.POINTER(ctypes.c_int)]),
@@ -462,6 +560,204 @@ def occ_get_flags(ws, clear: bool = False, stream=None) -> int:
     _check("occ_get_flags", lib().occ_get_flags(_ptr(ws), ctypes.byref(out), int(clear),
                                                 _stream(stream)))
     return int(out.value)
+
+
+# ----------------------------------------------------------------------------
+# stage operators
+# ----------------------------------------------------------------------------
+def _mat(t, name: str, rows: int, cols: int, dtype):
+    """(pointer, leading dimension) of an optional rows x cols matrix."""
+    if t is None:
+        return None, 0
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    if tuple(t.shape) != (rows, cols):
+        raise ValueError(f"{name} must be {rows} x {cols}")
+    return t.data_ptr() if rows else None, _ld(t, name) if rows else cols
+
+
+def _vec(t, name: str, n: int):
+    if t is None:
+        return None
+    if t.dtype != _torch().float32:
+        raise TypeError(f"{name} must be float32")
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must hold {n} contiguous values")
+    return t.data_ptr()
+
+
+def _workspace(nbytes: int, ws, device):
+    """(tensor, pointer, bytes) of the caller's workspace or of a new one; the
+    stage operators need no initialised header."""
+    if not nbytes:
+        return None, None, 0
+    if ws is None:
+        ws = _torch().empty(nbytes + 256, dtype=_torch().uint8, device=device)
+        at = (ws.data_ptr() + 255) // 256 * 256
+        return ws, at, nbytes
+    return ws, ws.data_ptr(), ws.numel()
+
+
+def _layer_fwd(name: str, wide: int, X, W, bias, act, R, Y, Z, ws, stream):
+    torch = _torch()
+    tokens, n_in = X.shape
+    if W.shape[0] % wide:
+        raise ValueError("W must hold the rows of both projections")
+    out = W.shape[0] // wide
+    if Y is None:
+        Y = torch.empty((tokens, out), dtype=X.dtype, device=X.device)
+    a = occ_linear_t()
+    a.dtype, a.act = _mdtype(X), int(act)
+    a.tokens, a.in_, a.out = tokens, n_in, out
+    a.X, a.ldx = _mat(X, "X", tokens, n_in, X.dtype)
+    a.W, a.ldw = _mat(W, "W", wide * out, n_in, X.dtype)
+    a.bias = _vec(bias, "bias", wide * out)
+    a.R, a.ldr = _mat(R, "R", tokens, out, X.dtype)
+    a.Z, a.ldz = _mat(Z, "Z", tokens, wide * out, X.dtype)
+    a.Y, a.ldy = _mat(Y, "Y", tokens, out, X.dtype)
+    L = lib()
+    p = ctypes.byref(a)
+    keep, wp, wn = _workspace(getattr(L, name + "_workspace_bytes")(p), ws, X.device)
+    _check(name, getattr(L, name)(p, wp, wn, _stream(stream)))
+    return Y
+
+
+def occ_linear_fwd(X, W, bias=None, act: int = OCC_ACT_NONE, R=None, Y=None, Z=None, ws=None,
+                   stream=None):
+    """Y = act(X W^T + bias) + R; Z, if given, receives the pre-activation.
+
+    X tokens x in, W out x in, R, Y and Z tokens x out, all float32 or all
+    bfloat16; bias float32.  R may be Y.  Returns Y.
+    """
+    return _layer_fwd("occ_linear_fwd", 1, X, W, bias, act, R, Y, Z, ws, stream)
+
+
+def occ_gated_fwd(X, W, bias=None, act: int = OCC_ACT_SILU, R=None, Y=None, Z=None, ws=None,
+                  stream=None):
+    """[G U] = X W^T + bias; Y = act(G) * U + R; Z, if given, receives [G U].
+
+    W is 2 out x in: the gate's rows, then the other projection's.
+    """
+    return _layer_fwd("occ_gated_fwd", 2, X, W, bias, act, R, Y, Z, ws, stream)
+
+
+def _layer_bwd(name: str, wide: int, dY, X, W, Z, act, dX, dW, dbias, accumulate, ws, stream):
+    torch = _torch()
+    tokens, out = dY.shape
+    some = X if X is not None else W if W is not None else dX if dX is not None else dW
+    n_in = 1 if some is None else some.shape[1]
+    a = occ_linear_grad_t()
+    a.dtype = _mdtype(dY)
+    a.dw_dtype = a.dtype if dW is None else _mdtype(dW)
+    a.act = int(act)
+    a.tokens, a.in_, a.out = tokens, n_in, out
+    a.dY, a.lddy = _mat(dY, "dY", tokens, out, dY.dtype)
+    a.X, a.ldx = _mat(X, "X", tokens, n_in, dY.dtype)
+    a.W, a.ldw = _mat(W, "W", wide * out, n_in, dY.dtype)
+    a.Z, a.ldz = _mat(Z, "Z", tokens, wide * out, dY.dtype)
+    a.dX, a.lddx = _mat(dX, "dX", tokens, n_in, dY.dtype)
+    a.dW, a.lddw = _mat(dW, "dW", wide * out, n_in, torch.float32 if a.dw_dtype == OCC_F32
+                        else torch.bfloat16)
+    a.dbias = _vec(dbias, "dbias", wide * out)
+    if tokens == 0 and dX is not None and dW is None and dbias is None:
+        return      # an empty dX
+    L = lib()
+    p = ctypes.byref(a)
+    keep, wp, wn = _workspace(getattr(L, name + "_workspace_bytes")(p), ws, dY.device)
+    _check(name, getattr(L, name)(p, OCC_GRAD_ACCUMULATE if accumulate else 0, wp, wn,
+                                  _stream(stream)))
+
+
+def occ_linear_bwd(dY, X=None, W=None, Z=None, act: int = OCC_ACT_NONE, dX=None, dW=None,
+                   dbias=None, accumulate: bool = False, ws=None, stream=None) -> None:
+    """Gradients of occ_linear_fwd, each made if a tensor is given for it:
+    dX (needs W), dW (needs X; may be float32 for a bfloat16 layer), dbias.
+    Z is the stored pre-activation (not needed with OCC_ACT_NONE).  accumulate:
+    dW and dbias are added to.  The gradient of R is dY itself.
+    """
+    _layer_bwd("occ_linear_bwd", 1, dY, X, W, Z, act, dX, dW, dbias, accumulate, ws, stream)
+
+
+def occ_gated_bwd(dY, X=None, W=None, Z=None, act: int = OCC_ACT_SILU, dX=None, dW=None,
+                  dbias=None, accumulate: bool = False, ws=None, stream=None) -> None:
+    """Gradients of occ_gated_fwd (W, dW and dbias hold both projections); as
+    occ_linear_bwd, with Z = [G U] always needed."""
+    _layer_bwd("occ_gated_bwd", 2, dY, X, W, Z, act, dX, dW, dbias, accumulate, ws, stream)
+
+
+def make_param(W, m, v, G=None, P=None, Q=None, W16=None, m_scale=None, v_scale=None,
+               decay: float = 0.0) -> occ_param_t:
+    """One tensor of occ_adamw_step: float32 W (a matrix, or a vector), its
+    gradient G (float32 or bfloat16) or the factors P and Q of one, and its
+    moments: float32, or float8_e4m3fn / uint8 codes with their scales."""
+    torch = _torch()
+    shape = (1, W.shape[0]) if W.dim() == 1 else tuple(W.shape)
+    if len(shape) != 2:
+        raise ValueError("W must be 1-D or 2-D")
+    rows, cols = shape
+
+    def whole(t, name, n, *dtypes):
+        if t is None:
+            return None
+        if t.dtype not in dtypes:
+            raise TypeError(f"{name} must be {' or '.join(map(str, dtypes))}")
+        if t.numel() != n or not t.is_contiguous():
+            raise ValueError(f"{name} must hold {n} contiguous values")
+        return t.data_ptr()
+
+    a = occ_param_t()
+    a.rows, a.cols = rows, cols
+    a.W = whole(W, "W", rows * cols, torch.float32)
+    a.W16 = whole(W16, "W16", rows * cols, torch.bfloat16)
+    if G is not None:
+        if P is not None or Q is not None:
+            raise ValueError("give G, or P and Q")
+        G2 = G.reshape(1, -1) if G.dim() == 1 and G.is_contiguous() else G
+        if tuple(G2.shape) != shape:
+            raise ValueError(f"G must be {rows} x {cols}")
+        a.G, a.ldg, a.g_dtype = G2.data_ptr(), _ld(G2, "G"), _mdtype(G2)
+    elif P is not None and Q is not None:
+        a.rank = P.shape[1]
+        a.P = whole(P, "P", rows * a.rank, torch.float32)
+        a.Q = whole(Q, "Q", cols * a.rank, torch.float32)
+    else:
+        raise ValueError("give G, or P and Q")
+    codes = (torch.float8_e4m3fn, torch.uint8)
+    a.state_bits = 8 if m.dtype in codes else 32
+    kinds = codes if a.state_bits == 8 else (torch.float32,)
+    a.m, a.v = whole(m, "m", rows * cols, *kinds), whole(v, "v", rows * cols, *kinds)
+    if a.state_bits == 8:
+        if m_scale is None or v_scale is None:
+            raise ValueError("8-bit moments need m_scale and v_scale")
+        n = rows * (-(-cols // OCC_SCALE_RUN))
+        a.m_scale = whole(m_scale, "m_scale", n, torch.float32)
+        a.v_scale = whole(v_scale, "v_scale", n, torch.float32)
+    a.decay = float(decay)
+    return a
+
+
+def make_params(params):
+    """The array occ_adamw_step takes, made once and kept while the tensors live."""
+    items = list(params)
+    return (occ_param_t * len(items))(*items)
+
+
+def occ_adamw_step(params, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.95,
+                   eps: float = 1e-8, seed: int = 0, grad_scale=None, flags=None,
+                   stream=None) -> None:
+    """AdamW over every tensor of `params` (make_params, or a sequence of
+    make_param); see occ_adamw_step in include/optcc.h.  grad_scale: float32
+    CUDA tensor of one value; flags: int32 CUDA tensor of one value."""
+    if not isinstance(params, ctypes.Array):
+        params = make_params(params)
+    h = occ_adamw_t(lr, beta1, beta2, eps, step, seed & 0xFFFFFFFF, 0,
+                    _vec(grad_scale, "grad_scale", 1), None)
+    if flags is not None:
+        if flags.numel() != 1 or flags.element_size() != 4:
+            raise ValueError("flags must be one 32-bit word")
+        h.flags = flags.data_ptr()
+    _check("occ_adamw_step", lib().occ_adamw_step(params, len(params), ctypes.byref(h),
+                                                  _stream(stream)))
 
 
 def occ_profile_begin() -> None:

@@ -1,0 +1,310 @@
+"""AdamW over many tensors against float64 (tests/stage_ref.py)."""
+
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2301_09830_amd import optcc  # noqa: E402
+from stage_ref import adamw64, decode, e4m3_values, within  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+LR, B1, B2, EPS = 1e-3, 0.9, 0.95, 1e-8
+U = 2.0 ** -24
+
+
+class State:
+    """One tensor with random moments; `shift`: elements its buffers are off
+    their allocation (codes: bytes)."""
+
+    def __init__(self, rows, cols, bits, grads, seed, shift=0, pad=0, copy=True, rank=0, decay=0.1):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        n = rows * cols
+
+        def off(x):
+            buf = torch.empty(x.numel() + shift, dtype=x.dtype, device="cuda")
+            view = buf[shift:].view(x.shape)
+            view.copy_(x)
+            return view
+
+        def randn(*s):
+            return torch.randn(*s, generator=g, device="cuda")
+
+        self.rows, self.cols, self.bits, self.decay = rows, cols, bits, decay
+        self.W = off(randn(rows, cols) * 0.02)
+        self.W16 = off(torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")) if copy else None
+        self.G = self.P = self.Q = self.m_scale = self.v_scale = None
+        if grads == "factors":
+            self.P, self.Q = off(randn(rows, rank)), off(randn(cols, rank) * 1e-3)
+        else:
+            dt = torch.bfloat16 if grads == "bf16" else torch.float32
+            buf = torch.full((rows, cols + pad), float("nan"), dtype=dt, device="cuda")
+            self.G = buf[:, :cols]
+            self.G.copy_(randn(rows, cols) * 1e-3)
+        if bits == 32:
+            self.m = off(randn(rows, cols) * 3e-4)
+            self.v = off((randn(rows, cols) * 1e-3) ** 2)
+        else:
+            c = torch.randint(0, 127, (rows, cols), generator=g, device="cuda", dtype=torch.uint8)
+            s = torch.randint(0, 2, (rows, cols), generator=g, device="cuda", dtype=torch.uint8)
+            self.m = off(c | (s << 7))
+            self.v = off(torch.randint(1, 127, (rows, cols), generator=g, device="cuda",
+                                       dtype=torch.uint8))
+            per = -(-cols // 256)
+            self.m_scale = (torch.rand(rows, per, generator=g, device="cuda") + 0.5) * 2e-6
+            self.v_scale = (torch.rand(rows, per, generator=g, device="cuda") + 0.5) * 4e-6
+        assert self.W.numel() == n
+
+    def param(self):
+        return optcc.make_param(self.W, self.m, self.v, G=self.G, P=self.P, Q=self.Q, W16=self.W16,
+                                m_scale=self.m_scale, v_scale=self.v_scale, decay=self.decay)
+
+    def reference(self, step, scale=1.0):
+        """float64 results of a step from the present state, with the bounds of
+        the fp32 arithmetic: each of the few operations rounds by U."""
+        if self.G is not None:
+            g = self.G.double()
+            dg = U * g.abs() * abs(scale)
+        else:
+            p, q = self.P.double(), self.Q.double()
+            g = p @ q.t()
+            dg = 2 * (p.shape[1] + 2) * U * (p.abs() @ q.abs().t()) * abs(scale)
+        g = g * scale
+        if self.bits == 32:
+            m, v = self.m.double(), self.v.double()
+        else:
+            m = decode(self.m, self.m_scale, self.cols)
+            v = decode(self.v, self.v_scale, self.cols) ** 2
+        w0 = self.W.double()
+        w, m1, v1, root = adamw64(w0, m, v, g, LR, B1, B2, EPS, step, self.decay)
+        bm = 4 * U * (B1 * m.abs() + (1 - B1) * g.abs()) + (1 - B1) * dg
+        bv = 6 * U * v1 + (1 - B2) * (2 * g.abs() * dg + dg * dg)
+        den = root / math.sqrt(1 - B2 ** step) + EPS
+        a = LR / (1 - B1 ** step)
+        low = (v1 - bv).clamp_min(0).sqrt() / math.sqrt(1 - B2 ** step) + EPS
+        bw = 3 * U * w0.abs() + a * (8 * U * m1.abs() / den + bm / low + m1.abs() * (1 / low - 1 / den))
+        return {"W": (w, bw + U * w.abs()), "m": (m1, bm), "v": (v1, bv), "root": root}
+
+
+def check(s, ref, what):
+    within(s.W, *ref["W"], what + " W")
+    if s.W16 is not None:
+        assert torch.equal(s.W16, s.W.bfloat16()), what
+    if s.bits == 32:
+        within(s.m, *ref["m"], what + " m")
+        within(s.v, *ref["v"], what + " v")
+        return
+    # scales: the run's largest magnitude over 448; codes: one of the two
+    # neighbours of the value (a value within 1e-5 of a code may take that code's neighbours)
+    values = e4m3_values().to("cuda")
+    for x, codes, scale in ((ref["m"][0], s.m, s.m_scale), (ref["root"], s.v, s.v_scale)):
+        pad = -s.cols % 256
+        top = torch.nn.functional.pad(x, (0, pad)).view(s.rows, -1, 256).abs().amax(2)
+        top = top.clamp_min(2.0 ** -100) / 448
+        assert ((scale.double() - top).abs() <= 1e-5 * top).all(), what + " scale"
+        y = (x / scale.double().repeat_interleave(256, 1)[:, :s.cols]).abs()
+        c = codes.view(torch.uint8).long()
+        low = torch.searchsorted(values, y * (1 - 1e-5), right=True) - 1
+        high = torch.searchsorted(values, y * (1 + 1e-5) + 1e-12).clamp_max(126)
+        mag = c & 127
+        floor_one = (x > 0) & (mag == 1) if codes is s.v else torch.zeros_like(c, dtype=torch.bool)
+        assert (((mag >= low) & (mag <= high)) | floor_one).all(), what + " codes"
+        if codes is s.m:
+            assert ((c >= 128) == (x < 0))[mag > 0].all(), what + " signs"
+        else:
+            assert (mag[x > 0] > 0).all() and (c < 128).all(), what
+
+
+SHAPES = [(1, 1), (1, 3), (1, 255), (1, 256), (1, 257), (1, 4096), (1, 10001), (7, 1), (3, 5),
+          (16, 256), (17, 300), (64, 512), (65, 513), (200, 1023), (1000, 77)]
+
+
+@pytest.mark.parametrize("grads", ["f32", "bf16", "factors"])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_shapes(bits, grads):
+    for i, (rows, cols) in enumerate(SHAPES):
+        rank = 1 + (i * 13) % 128
+        s = State(rows, cols, bits, grads, seed=i, rank=rank, copy=i % 2 == 0)
+        ref = s.reference(step=3)
+        print(f"adamw {rows}x{cols} {bits} {grads} rank {rank}", flush=True)
+        optcc.occ_adamw_step([s.param()], LR, 3, B1, B2, EPS, seed=i)
+        torch.cuda.synchronize()
+        check(s, ref, f"{rows}x{cols}")
+
+
+@pytest.mark.parametrize("rank", [1, 2, 4, 15, 16, 17, 64, 127, 128])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_factor_ranks(bits, rank):
+    s = State(70, 300, bits, "factors", seed=rank, rank=rank)
+    ref = s.reference(step=10)
+    optcc.occ_adamw_step([s.param()], LR, 10, B1, B2, EPS)
+    check(s, ref, f"rank {rank}")
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("shift", [1, 2, 3])
+def test_any_alignment(bits, shift):
+    for grads in ("f32", "bf16", "factors"):
+        s = State(33, 301, bits, grads, seed=shift, shift=shift, pad=shift, rank=9)
+        ref = s.reference(step=2)
+        optcc.occ_adamw_step([s.param()], LR, 2, B1, B2, EPS)
+        check(s, ref, f"{grads} shift {shift}")
+
+
+def test_many_tensors_in_one_call():
+    """More tensors than one launch takes, every form among them."""
+    forms = [(b, g) for b in (32, 8) for g in ("f32", "bf16", "factors")]
+    states = []
+    for i in range(210):
+        bits, grads = forms[i % 6]
+        states.append(State(1 + i % 9, 1 + (i * 37) % 700, bits, grads, seed=i, rank=1 + i % 20,
+                            decay=0.1 * (i % 2)))
+    scale = torch.tensor([0.37], device="cuda")
+    refs = [s.reference(5, float(scale)) for s in states]
+    optcc.occ_adamw_step(optcc.make_params(s.param() for s in states), LR, 5, B1, B2, EPS, seed=77,
+                         grad_scale=scale)
+    for i, (s, r) in enumerate(zip(states, refs)):
+        check(s, r, f"tensor {i}")
+
+
+def test_several_steps_from_nothing():
+    """From zero moments, 32 and 8 bits side by side on the same gradients: the
+    8-bit weights follow within the codes' coarseness."""
+    a = State(40, 520, 32, "f32", seed=1)
+    b = State(40, 520, 8, "f32", seed=1)
+    b.W.copy_(a.W)
+    for s in (a, b):
+        for t in (s.m, s.v):
+            t.zero_()
+    b.m_scale.zero_()
+    b.v_scale.zero_()
+    start = a.W.clone()
+    pa, pb = [a.param()], [b.param()]
+    for step in range(1, 31):
+        g = torch.randn(40, 520, device="cuda") * 1e-3 + 5e-4
+        a.G.copy_(g)
+        b.G.copy_(g)
+        ref = b.reference(step)
+        optcc.occ_adamw_step(pa, LR, step, B1, B2, EPS)
+        optcc.occ_adamw_step(pb, LR, step, B1, B2, EPS, seed=step)
+        check(b, ref, f"step {step}")
+    moved = (a.W - start).norm()
+    assert (a.W - b.W).norm() < 0.1 * moved
+
+
+def test_rounding_is_unbiased():
+    """A value a part p above a code rounds up in a share p of the elements
+    (200000 of them: 5 standard deviations are 0.0056), for m and for sqrt(v)
+    independently, and each seed rounds others."""
+    n = 200000
+    for p in (0.1, 0.5, 0.77):
+        y = 1.0 + p / 8        # between the codes of 1 and 1.125
+        s = State(1, n, 8, "f32", seed=0, decay=0.0, copy=False)
+        # beta = 0: m = g and v = g^2; one element of 448 in each run sets its scale to 1
+        s.G.fill_(y)
+        s.G[0, ::256] = 448.0
+        ups = []
+        for seed in (1, 2):
+            optcc.occ_adamw_step([s.param()], 0.0, 1, 0.0, 0.0, EPS, seed=seed)
+            rest = torch.arange(n, device="cuda") % 256 != 0
+            one, up = 56, 57   # codes of 1 and of 1.125
+            for c in (s.m.view(torch.uint8)[0][rest], s.v.view(torch.uint8)[0][rest]):
+                assert ((c == one) | (c == up)).all()
+                share = float((c == up).double().mean())
+                assert abs(share - p) < 0.0062, (p, share)
+                ups.append(c == up)
+        for i in range(4):
+            for j in range(i):
+                both = float((ups[i] & ups[j]).double().mean())
+                assert abs(both - p * p) < 0.007
+
+
+def test_grad_scale_and_flags():
+    for bits in (32, 8):
+        for grads in ("f32", "bf16", "factors"):
+            s = State(20, 300, bits, grads, seed=4, rank=8)
+            before = [t.clone() for t in (s.W, s.W16, s.m, s.v)]
+            flags = torch.tensor([optcc.OCC_F_NONFINITE], dtype=torch.int32, device="cuda")
+            scale = torch.tensor([0.25], device="cuda")
+            optcc.occ_adamw_step([s.param()], LR, 2, B1, B2, EPS, flags=flags, grad_scale=scale)
+            assert all(torch.equal(x, y) for x, y in zip(before, (s.W, s.W16, s.m, s.v)))
+            ref = s.reference(2, 0.25)
+            flags.fill_(optcc.OCC_F_RANK_DEFICIENT)      # no reason to skip a step
+            optcc.occ_adamw_step([s.param()], LR, 2, B1, B2, EPS, flags=flags, grad_scale=scale)
+            check(s, ref, f"{bits} {grads}")
+
+
+def test_nonfinite_gradients_stay_in_their_run():
+    for bits in (32, 8):
+        s = State(3, 600, bits, "f32", seed=6, copy=False)
+        clean = State(3, 600, bits, "f32", seed=6, copy=False)
+        s.G[1, 300] = float("nan")
+        s.G[2, 10] = float("inf")
+        optcc.occ_adamw_step([s.param()], LR, 2, B1, B2, EPS)
+        optcc.occ_adamw_step([clean.param()], LR, 2, B1, B2, EPS)
+        same = torch.ones(3, 600, dtype=torch.bool, device="cuda")
+        same[1, 300] = same[2, 10] = False
+        assert torch.equal(s.W[same], clean.W[same])
+        assert torch.isnan(s.W[1, 300])
+        if bits == 8:
+            same[1, 256:512] = same[2, :256] = False
+            assert (s.m[1, 300] & 127) == 127 and torch.isinf(s.m_scale[2, 0])
+        else:
+            assert torch.isnan(s.m[1, 300]) and torch.isinf(s.v[2, 10])
+        assert torch.equal(s.m[same], clean.m[same]) and torch.equal(s.v[same], clean.v[same])
+
+
+def test_zero_gradients_and_zero_moments():
+    for bits in (32, 8):
+        s = State(2, 300, bits, "f32", seed=7, decay=0.5)
+        s.G.zero_(), s.m.zero_(), s.v.zero_()
+        w = s.W.clone()
+        optcc.occ_adamw_step([s.param()], LR, 1, B1, B2, EPS)
+        assert torch.allclose(s.W, w * (1 - LR * 0.5), rtol=1e-6)
+        assert (s.m.view(torch.uint8) == 0).all() and (s.v.view(torch.uint8) == 0).all()
+
+
+def test_elements_beyond_32_bits():
+    """2^31 + elements in one tensor: its last rows against float64."""
+    rows, cols = 33000, 65600
+    s = State(8, cols, 8, "bf16", seed=8, copy=False)
+    big = {k: torch.zeros(rows, getattr(s, k).shape[1], dtype=getattr(s, k).dtype, device="cuda")
+           for k in ("W", "G", "m", "v", "m_scale", "v_scale")}
+    for k, t in big.items():
+        t[-8:].copy_(getattr(s, k))
+    ref = s.reference(2)
+    p = optcc.make_param(big["W"], big["m"], big["v"], G=big["G"], m_scale=big["m_scale"],
+                         v_scale=big["v_scale"], decay=s.decay)
+    optcc.occ_adamw_step([p], LR, 2, B1, B2, EPS)
+    for k, t in big.items():
+        if k != "G":
+            getattr(s, k).copy_(t[-8:])
+    check(s, ref, "last rows")
+    assert (big["W"][:-8] == 0).all()
+
+
+def test_repeats_streams_and_graphs():
+    def fresh():
+        return [State(50, 300, b, g, seed=i, rank=8)
+                for i, (b, g) in enumerate([(32, "f32"), (8, "bf16"), (8, "factors")])]
+
+    def buffers(states):
+        return [t for s in states for t in (s.W, s.W16, s.m, s.v)]
+
+    a, b, c = fresh(), fresh(), fresh()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    pa, pb, pc = ([s.param() for s in x] for x in (a, b, c))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        optcc.occ_adamw_step(pc, LR, 2, B1, B2, EPS, seed=5)
+    for _ in range(3):
+        optcc.occ_adamw_step(pa, LR, 2, B1, B2, EPS, seed=5)
+        with torch.cuda.stream(side):
+            optcc.occ_adamw_step(pb, LR, 2, B1, B2, EPS, seed=5)
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y, z in zip(buffers(a), buffers(b), buffers(c)):
+            assert torch.equal(x, y) and torch.equal(x, z)
