@@ -59,17 +59,30 @@ __device__ __forceinline__ float normal_cdf(float z, float& e) {
 constexpr float kGeluC = 0.79788456080286536f;   // sqrt(2 / pi)
 constexpr float kGeluA = 0.044715f;
 
-__device__ __forceinline__ float act_f(int act, float z) {
+__device__ __forceinline__ f32x4_t act_quad(int act, f32x4_t z) {
+  f32x4_t y = z;
   float e;
-  switch (act) {
-    case ACT_RELU: return z > 0.0f || z != z ? z : 0.0f;
-    case ACT_GELU: return z * normal_cdf(z, e);
-    // (1 + tanh q) / 2 = sigmoid(2 q)
-    case ACT_GELU_TANH:
-      return z * sigmoid_f(2.0f * kGeluC * z * __builtin_fmaf(kGeluA, z * z, 1.0f));
-    case ACT_SILU: return z * sigmoid_f(z);
-    default: return z;
+  switch (act) {   // the same for all lanes
+    case ACT_RELU:
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = z[i] > 0.0f || z[i] != z[i] ? z[i] : 0.0f;
+      break;
+    case ACT_GELU:
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = z[i] * normal_cdf(z[i], e);
+      break;
+    case ACT_GELU_TANH:   // (1 + tanh q) / 2 = sigmoid(2 q)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        y[i] = z[i] * sigmoid_f(z[i] * __builtin_fmaf(2.0f * kGeluC * kGeluA, z[i] * z[i], 2.0f * kGeluC));
+      break;
+    case ACT_SILU:
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = z[i] * sigmoid_f(z[i]);
+      break;
+    default: break;
   }
+  return y;
 }
 
 // act(z) and act'(z)
@@ -161,23 +174,22 @@ struct FwdEpi {
   int32_t out;         // columns of Y; gated: W, bias and Z hold the gate's rows, then the others'
 };
 
+// bias[n .. n + 3], zeros without one
+__device__ __forceinline__ f32x4_t bias_quad(const FwdEpi& e, int n, int left) {
+  return e.bias ? ld_quad<float>(e.bias + n, left) : f32x4_t{};
+}
+
 // Columns n .. n + 3 of token m: z (and u, the other projection, when gated)
-// are sums of products in fp32.
+// are sums of products in fp32, the bias added.
 template <class T, bool GATED>
 __device__ __forceinline__ void fwd_epilogue(const FwdEpi& e, int64_t m, int n, f32x4_t z, f32x4_t u) {
   const int left = e.out - n;
   if (left <= 0) return;
-  if (e.bias) {
-    z += ld_quad<float>(e.bias + n, left);
-    if constexpr (GATED) u += ld_quad<float>(e.bias + e.out + n, left);
-  }
   if (e.Z) {
     st_quad((T*)e.Z + m * e.ldz + n, z, left);
     if constexpr (GATED) st_quad((T*)e.Z + m * e.ldz + e.out + n, u, left);
   }
-  f32x4_t y;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) y[i] = act_f(e.act, z[i]);
+  f32x4_t y = act_quad(e.act, z);
   if constexpr (GATED) y *= u;
   if (e.R) y += ld_quad<T>((const T*)e.R + m * e.ldr + n, left);
   st_quad((T*)e.Y + m * e.ldy + n, y, left);
@@ -376,6 +388,24 @@ __device__ __forceinline__ void band_tile(int t, int tiles_m, int tiles_n, int& 
   tm = band * kBand + in - tn * h;
 }
 
+// Passes that the results of a tile take through the LDS of its two stages.
+template <int BM, int BN, int STAGE>
+constexpr int PR_PASSES = BM * BN * 4 / (2 * STAGE) > 0 ? BM * BN * 4 / (2 * STAGE) : 1;
+
+// Four results of a gradient: stored, or added to what is there.
+template <class T>
+__device__ __forceinline__ void store_result(const GemmArgs& g, int64_t m, int n, f32x4_t v, int left) {
+  if (sizeof(T) == 4 || g.c_f32) {
+    float* const p = (float*)g.C + m * g.ldc + n;
+    if (g.accumulate) v += ld_quad<float>(p, left);
+    st_quad(p, v, left);
+  } else {
+    uint16_t* const p = (uint16_t*)g.C + m * g.ldc + n;
+    if (g.accumulate) v += ld_quad<uint16_t>(p, left);
+    st_quad(p, v, left);
+  }
+}
+
 // WM x WN waves, each 16 FA x 16 FB results.  PP: the waves form two groups
 // (one wave of each on every SIMD) that alternate between matrix
 // instructions and LDS reads; see the loop.
@@ -507,50 +537,53 @@ __global__ __launch_bounds__(WM * WN * 64, PP ? 2 : 2) void k_gemm(GemmArgs g) {
     if (wave < NW / 2) asm volatile("s_barrier" ::: "memory");
   }
 
-  // lane: token (row) lane % 16 and 4 columns of each 16 x 16 block
-  const int64_t mrow = m0 + wm * FA * 16 + (lane & 15);
-  const int ncol = n0 + wn * (BNC / WN) + (lane >> 4) * 4;
-  if (g.splits > 1) {
-    const int width = EP == EP_GATED ? 2 * g.N : g.N;
-    float* const dst = g.part + (int64_t)split * g.M * width;
-#pragma unroll
-    for (int a = 0; a < FA; ++a)
-#pragma unroll
-      for (int b = 0; b < FB; ++b) {
-        const int64_t m = mrow + a * 16;
-        const bool up = EP == EP_GATED && b >= FB / 2;
-        const int n = ncol + (up ? b - FB / 2 : b) * 16;
-        if (m < g.M && n < g.N) st_quad(dst + m * width + (up ? g.N : 0) + n, acc[a][b], g.N - n);
-      }
-    return;
+  // The results go through LDS, so that the epilogue runs along whole rows of
+  // the tile: a wave's stores then cover 512 (256) consecutive bytes instead
+  // of 32 in each of 16 rows, which lie in one memory channel when the row
+  // length is a power of two (8192 x 16384 results: 229 us at K = 64 that way).
+  // Pieces of 16 bytes are exchanged within a row by the row's number: a
+  // lane holds 4 columns of row lane % 16 of each 16 x 16 block.
+  constexpr int NP = PR_PASSES<BM, BN, STAGE>;
+  constexpr int WR = FA / NP * 16, PR = WM * WR;   // rows of a wave and of a pass
+  constexpr int QPR = BNC / 4, RPI = 64 / QPR;     // quads of a row; rows at a time
+  const int li = lane & 15, lg = lane >> 4;
+  const int q = lane % QPR, n = n0 + q * 4, left = g.N - n;
+  const bool split_k = g.splits > 1;
+  f32x4_t bz = {}, bu = {};
+  if (EP != EP_STORE && !split_k && left > 0) {
+    bz = bias_quad(g.fwd, n, left);
+    if constexpr (EP == EP_GATED) bu = bias_quad(g.fwd, g.N + n, left);
   }
+  const int64_t width = EP == EP_GATED ? 2 * (int64_t)g.N : g.N;
+  typedef __attribute__((address_space(3))) f32x4_t lds_f4;
 #pragma unroll
-  for (int a = 0; a < FA; ++a) {
-    const int64_t m = mrow + a * 16;
-    if (m >= g.M) continue;
-    if constexpr (EP == EP_GATED) {
+  for (int p = 0; p < NP; ++p) {
+    // (the stores of the pass before need not have ended)
+    if (p) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
-      for (int b = 0; b < FB / 2; ++b)
-        fwd_epilogue<T, true>(g.fwd, m, ncol + b * 16, acc[a][b], acc[a][b + FB / 2]);
-    } else if constexpr (EP == EP_FWD) {
-#pragma unroll
-      for (int b = 0; b < FB; ++b)
-        fwd_epilogue<T, false>(g.fwd, m, ncol + b * 16, acc[a][b], f32x4_t{});
-    } else {
+    for (int a = 0; a < FA / NP; ++a)
 #pragma unroll
       for (int b = 0; b < FB; ++b) {
-        const int n = ncol + b * 16, l = g.N - n;
-        if (l <= 0) continue;
-        f32x4_t v = acc[a][b];
-        if (sizeof(T) == 4 || g.c_f32) {
-          float* const p = (float*)g.C + m * g.ldc + n;
-          if (g.accumulate) v += ld_quad<float>(p, l);
-          st_quad(p, v, l);
-        } else {
-          uint16_t* const p = (uint16_t*)g.C + m * g.ldc + n;
-          if (g.accumulate) v += ld_quad<uint16_t>(p, l);
-          st_quad(p, v, l);
-        }
+        const int c = EP == EP_GATED ? (b >= FB / 2 ? QPR : 0) + (wn * (FB / 2) + b % (FB / 2)) * 4 + lg
+                                     : (wn * FB + b) * 4 + lg;
+        *(lds_f4*)(lds + (wm * WR + a * 16 + li) * BN * 4 + ((c ^ li) << 4)) = acc[p * (FA / NP) + a][b];
+      }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll 4
+    for (int r = 0; r < PR / NW / RPI; ++r) {
+      const int row = wave * (PR / NW) + r * RPI + lane / QPR;
+      const int64_t m = m0 + row / WR * (FA * 16) + p * WR + row % WR;
+      if (m >= g.M || left <= 0) continue;
+      f32x4_t z = *(const lds_f4*)(lds + row * BN * 4 + ((q ^ (row & 15)) << 4)), u = {};
+      if constexpr (EP == EP_GATED) u = *(const lds_f4*)(lds + row * BN * 4 + (((QPR + q) ^ (row & 15)) << 4));
+      if (split_k) {
+        float* const dst = g.part + ((int64_t)split * g.M + m) * width + n;
+        st_quad(dst, z, left);
+        if constexpr (EP == EP_GATED) st_quad(dst + g.N, u, left);
+      } else if constexpr (EP == EP_STORE) {
+        store_result<T>(g, m, n, z, left);
+      } else {
+        fwd_epilogue<T, EP == EP_GATED>(g.fwd, m, n, z + bz, u + bu);
       }
     }
   }
@@ -571,18 +604,12 @@ __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs g) {
       z += ld_quad<float>(p, left);
       if constexpr (EP == EP_GATED) u += ld_quad<float>(p + g.N, left);
     }
-    if constexpr (EP == EP_GATED) {
-      fwd_epilogue<T, true>(g.fwd, m, n, z, u);
-    } else if constexpr (EP == EP_FWD) {
-      fwd_epilogue<T, false>(g.fwd, m, n, z, u);
-    } else if (sizeof(T) == 4 || g.c_f32) {
-      float* const c = (float*)g.C + m * g.ldc + n;
-      if (g.accumulate) z += ld_quad<float>(c, left);
-      st_quad(c, z, left);
+    if constexpr (EP == EP_STORE) {
+      store_result<T>(g, m, n, z, left);
     } else {
-      uint16_t* const c = (uint16_t*)g.C + m * g.ldc + n;
-      if (g.accumulate) z += ld_quad<uint16_t>(c, left);
-      st_quad(c, z, left);
+      z += bias_quad(g.fwd, n, left);
+      if constexpr (EP == EP_GATED) u += bias_quad(g.fwd, g.N + n, left);
+      fwd_epilogue<T, EP == EP_GATED>(g.fwd, m, n, z, u);
     }
   }
 }

@@ -113,7 +113,12 @@ __global__ __launch_bounds__(SK_WAVES * 64) void k_skinny(SkinnyArgs g) {
       z += sums[v][t][lane];
       if constexpr (GATED) u += sums[v][NT + t][lane];
     }
-    if (m < g.tokens) fwd_epilogue<T, GATED>(g.fwd, m, n0 + q * 4, z, u);
+    const int n = n0 + q * 4, left = g.fwd.out - n;
+    if (m < g.tokens && left > 0) {
+      z += bias_quad(g.fwd, n, left);
+      if constexpr (GATED) u += bias_quad(g.fwd, g.fwd.out + n, left);
+      fwd_epilogue<T, GATED>(g.fwd, m, n, z, u);
+    }
   }
 }
 
