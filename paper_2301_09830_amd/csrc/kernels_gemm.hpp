@@ -465,10 +465,12 @@ __global__ __launch_bounds__(WM * WN * 64, PP ? 2 : 2) void k_gemm(GemmArgs g) {
 
   constexpr int HA = FA / 2, HB = FB / 2;
   Frag<ES> a0[HA], a1[HA], b0[HB], b1[HB];
-  auto read_a = [&](Frag<ES>* f, int stage, int half) {
+  // fragments i0 .. i1 - 1 of a half
+  auto read_a = [&](Frag<ES>* f, int stage, int half, int i0, int i1) {
     const lds_char* p = lds + stage * STAGE;
 #pragma unroll
-    for (int i = 0; i < HA; ++i) f[i] = ra.template read<OA::KROW>(p, half * HA + i);
+    for (int i = 0; i < HA; ++i)
+      if (i >= i0 && i < i1) f[i] = ra.template read<OA::KROW>(p, half * HA + i);
   };
   auto read_b = [&](Frag<ES>* f, int stage, int half) {
     const lds_char* p = lds + stage * STAGE + OA::BYTES;
@@ -500,34 +502,43 @@ __global__ __launch_bounds__(WM * WN * 64, PP ? 2 : 2) void k_gemm(GemmArgs g) {
   load_a(0);
   load_b(0);
   asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-  if (nk > 1) load_a(1);
-  read_a(a0, 0, 0);
+  if (nk > 1) {
+    load_b(1);
+    load_a(1);
+  }
+  read_a(a0, 0, 0, 0, HA);
   if constexpr (PP) {
     if (wave >= NW / 2) asm volatile("s_barrier" ::: "memory");
   }
   // The quarters of the wave's results, in an order that needs one new half
-  // operand each.  Loads of tile t + 1 end before its first read (the wait
-  // before the third quarter, and a barrier after it); the stage of tile t is
-  // loaded again only after every wave's last read of it (A: before that same
-  // barrier, B: earlier).
+  // operand each; the reads are spread so that each run of matrix
+  // instructions covers the same number of them.  Loads of tile t + 1 end
+  // before its first read (the wait before the second quarter, and a barrier
+  // after it); the stage of tile t is loaded again only after every wave's
+  // last read of it: B from the third quarter on, A from the fourth.
+  constexpr int Q1 = HA / 4, Q2 = HA / 2;
   for (int kt = 0; kt < nk; ++kt) {
     const int st = kt & 1;
     read_b(b0, st, 0);
-    if (kt + 1 < nk) load_b(st ^ 1);
+    read_a(a1, st, 1, 0, Q1);
     before();
     multiply(a0, b0, 0, 0);
     after();
     read_b(b1, st, 1);
+    read_a(a1, st, 1, Q1, Q2);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if constexpr (!PP) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     before();
     multiply(a0, b1, 0, 1);
     after();
-    read_a(a1, st, 1);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    read_a(a1, st, 1, Q2, HA);
+    if (kt + 1 < nk) read_a(a0, st ^ 1, 0, 0, Q1);
+    if (kt + 2 < nk) load_b(st);
     if constexpr (!PP) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     before();
     multiply(a1, b1, 1, 1);
     after();
-    if (kt + 1 < nk) read_a(a0, st ^ 1, 0);
+    if (kt + 1 < nk) read_a(a0, st ^ 1, 0, Q1, HA);
     if (kt + 2 < nk) load_a(st);
     before();
     multiply(a1, b0, 1, 0);
