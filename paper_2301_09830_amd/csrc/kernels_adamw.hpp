@@ -72,14 +72,15 @@ __device__ __forceinline__ void adam_quad(const AdamArgs& g, float keep, float s
     m[i] = m[i] * g.b1 + gr * g.c1;
     v[i] = v[i] * g.b2 + (gr * gr) * g.c2;
     root[i] = __builtin_sqrtf(v[i]);
-    w[i] = w[i] * keep - (m[i] / (root[i] * g.c + g.eps)) * g.a;
+    // the reciprocal's last bit is 2^-23 of the step, not of W
+    w[i] = w[i] * keep - (m[i] * __builtin_amdgcn_rcpf(root[i] * g.c + g.eps)) * g.a;
   }
 }
 
-// 32 random bits for element `index` of the tensor with this key: 16 for m
-// (low), 16 for v.  Two rounds of an odd multiplier and a shifted exclusive or.
-__device__ __forceinline__ uint32_t adam_bits(uint64_t index, uint32_t key) {
-  uint32_t x = (uint32_t)index * 0x9E3779B1u + key + (uint32_t)(index >> 32) * 0xBB67AE85u;
+// 32 random bits for an element, 16 for m (low) and 16 for v: two rounds of an
+// odd multiplier and a shifted exclusive or on x = index * 0x9E3779B1 + key +
+// (index >> 32) * 0xBB67AE85 (mod 2^32).
+__device__ __forceinline__ uint32_t adam_bits(uint32_t x) {
   x = (x ^ (x >> 16)) * 0x6A09E667u;
   x = (x ^ (x >> 15)) * 0xBB67AE85u;
   return x ^ (x >> 16);
@@ -137,9 +138,10 @@ __device__ __forceinline__ float run_top(float x) { return fmaxf(x, 7.8886090522
 __device__ __forceinline__ void encode_quad(f32x4_t m, f32x4_t root, float inv_m, float inv_v, uint64_t index,
                                             uint32_t key, uint32_t& cm, uint32_t& cv) {
   cm = cv = 0;
+  const uint32_t start = (uint32_t)index * 0x9E3779B1u + key;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint32_t r = adam_bits(index + i, key);
+    const uint32_t r = adam_bits(start + i * 0x9E3779B1u + (uint32_t)((index + i) >> 32) * 0xBB67AE85u);
     const float y = m[i] * inv_m;
     cm |= (e4m3_code(y, r & 0xffffu) | (__float_as_uint(y) >> 31 << 7)) << (8 * i);
     uint32_t c = e4m3_code(root[i] * inv_v, r >> 16);
@@ -271,105 +273,182 @@ __global__ __launch_bounds__(256) void k_adamw8(AdamArgs g) {
 // ----------------------------------------------------------------------------
 // gradients as factors: G = P Q^T is made in registers and never stored
 // ----------------------------------------------------------------------------
-// A wave takes 16 rows x 256 columns (one run of each row), a block 64 rows.
-// The products are fp32 on v_mfma_f32_16x16x4_f32 with Q as the first
-// operand: a lane then holds four consecutive columns of row lane % 16 of
-// each 16 x 16 block.  The order of the rank within the products is that of
-// the 16-byte pieces both operands are loaded in.
-constexpr int ADF_ROWS = 64;
+// A block takes 128 rows x 256 columns (one run of each row), a wave 16 of the
+// rows.  The products are fp32 on v_mfma_f32_16x16x4_f32; Q, which all waves
+// share, passes through LDS 32 ranks at a time, P goes straight to registers.
+// A lane's results are four columns of row lane % 16 of each 16 x 16 block;
+// 64 columns at a time they are turned through LDS, so that W and the moments
+// are read and written in runs of 256 bytes of a row (16 runs of 64 bytes at a
+// power of two apart meet in one memory channel: 2.8 ms for the 403M elements
+// of eight layers of width 2048 at rank 32, 2.1 ms this way).  The first
+// columns' W and moments are asked for before the products, each next 64
+// columns' while the present ones are worked on.
+constexpr int ADF_WAVES = 8;
+constexpr int ADF_ROWS = 16 * ADF_WAVES;
+constexpr int ADF_RANKS = 32;
 
 template <int BITS>
-__global__ __launch_bounds__(256) void k_adamw_factors(AdamArgs g) {
+struct AdamPiece {   // 4 rows x 4 columns of a lane, 4 rows apart
+  f32x4_t w[4], m[BITS == 32 ? 4 : 1], v[BITS == 32 ? 4 : 1];
+  uint32_t cm[4], cv[4];
+};
+
+template <int BITS>
+__global__ __launch_bounds__(ADF_WAVES * 64) void k_adamw_factors(AdamArgs g) {
   if (g.flags && (*g.flags & 1u)) return;
+  __shared__ f32x4_t qs[kRun * ADF_RANKS / 4];
+  __shared__ f32x4_t turn[ADF_WAVES][16 * 16];
   const AdamTensor& t = g.t[adam_tensor(g, blockIdx.x)];
   const float scale = g.grad_scale ? *g.grad_scale : 1.0f;
-  const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
+  const int wave = wave_id(), lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
   const int per_row = (t.cols + kRun - 1) / kRun;
   const int b = (int)blockIdx.x - t.block0;
   const int rb = b / per_row, run = b - rb * per_row;
-  const int row = rb * ADF_ROWS + wave_id() * 16 + i;
-  const bool mine = row < t.rows;
+  const int row0 = rb * ADF_ROWS + wave * 16;
   const int c0 = run * kRun;
-  const int nf = min(16, (t.cols - c0 + 15) / 16);
+  const int cols_left = t.cols - c0;
+
+  // rows row0 + 4 k + q, columns c0 + 64 j + 4 i of piece j
+  AdamPiece<BITS> now, next;
+  auto load = [&](AdamPiece<BITS>& p, int j) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int row = row0 + 4 * k + q;
+      const int64_t e = (int64_t)row * t.cols + c0 + 64 * j + 4 * i;
+      const int left = row < t.rows ? cols_left - 64 * j - 4 * i : 0;
+      p.w[k] = ld_quad<float>(t.W + e, left);
+      if constexpr (BITS == 32) {
+        p.m[k] = ld_quad<float>((const float*)t.m + e, left);
+        p.v[k] = ld_quad<float>((const float*)t.v + e, left);
+      } else {
+        p.cm[k] = ld_codes((const uint8_t*)t.m + e, left);
+        p.cv[k] = ld_codes((const uint8_t*)t.v + e, left);
+      }
+    }
+  };
+  load(now, 0);
+  float sm[4], sv[4];   // scales of the four rows
+  if constexpr (BITS == 8) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int64_t sr = (int64_t)min(row0 + 4 * k + q, t.rows - 1) * per_row + run;
+      sm[k] = t.m_scale[sr];
+      sv[k] = t.v_scale[sr];
+    }
+  }
+
   f32x4_t acc[16];
 #pragma unroll
   for (int f = 0; f < 16; ++f) acc[f] = f32x4_t{};
-  const float* const p = t.P + (int64_t)min(row, t.rows - 1) * t.rank + 4 * q;
-  const float* const qp = t.Q + 4 * q;
-  for (int k = 0; k < t.rank; k += 16) {
-    const int left = t.rank - k - 4 * q;
-    const f32x4_t pv = ld_quad<float>(p + k, left);
+  const float* const prow = t.P + (int64_t)min(row0 + i, t.rows - 1) * t.rank;
+  // thread: pieces of 4 ranks of rows threadIdx / 8 + 64 u of the run's Q
+  constexpr int QN = kRun * ADF_RANKS / 4 / (ADF_WAVES * 64);
+  const int qr = threadIdx.x >> 3, qc = threadIdx.x & 7;
+  f32x4_t qn[QN];
+  auto load_q = [&](int k) {
 #pragma unroll
-    for (int f = 0; f < 16; ++f) {
-      if (f >= nf) continue;
-      const f32x4_t qv = ld_quad<float>(qp + (int64_t)min(c0 + 16 * f + i, t.cols - 1) * t.rank + k, left);
+    for (int u = 0; u < QN; ++u)
+      qn[u] = ld_quad<float>(t.Q + (int64_t)min(c0 + qr + u * (ADF_WAVES * 8), t.cols - 1) * t.rank + k + 4 * qc,
+                             t.rank - k - 4 * qc);
+  };
+  load_q(0);
+  for (int k = 0; k < t.rank; k += ADF_RANKS) {
+    f32x4_t pv[2];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(qv[j], pv[j], acc[f], 0, 0, 0);
+    for (int s = 0; s < 2; ++s) pv[s] = ld_quad<float>(prow + k + 16 * s + 4 * q, t.rank - k - 16 * s - 4 * q);
+    if (k) __syncthreads();
+#pragma unroll
+    for (int u = 0; u < QN; ++u) {
+      const int r = qr + u * (ADF_WAVES * 8);
+      qs[r * 8 + (qc ^ (r & 7))] = qn[u];
+    }
+    __syncthreads();
+    if (k + ADF_RANKS < t.rank) load_q(k + ADF_RANKS);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      if (k + 16 * s >= t.rank) continue;
+#pragma unroll
+      for (int f = 0; f < 16; ++f) {
+        const f32x4_t qv = qs[(16 * f + i) * 8 + ((4 * s + q) ^ (i & 7))];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          acc[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(qv[j], pv[s][j], acc[f], 0, 0, 0);
+      }
     }
   }
-  const int64_t e0 = (int64_t)row * t.cols + c0 + 4 * q;
-  const int left0 = mine ? t.cols - c0 - 4 * q : 0;
-  if constexpr (BITS == 32) {
-    float* const M = (float*)t.m;
-    float* const V = (float*)t.v;
+
+  float tm[4] = {}, tv[4] = {};
+  f32x4_t ms[BITS == 8 ? 4 : 1][4], roots[BITS == 8 ? 4 : 1][4];
 #pragma unroll
-    for (int f = 0; f < 16; ++f) {
-      if (f >= nf) continue;
-      const int64_t e = e0 + 16 * f;
-      const int left = left0 - 16 * f;
-      f32x4_t w = ld_quad<float>(t.W + e, left), m = ld_quad<float>(M + e, left), v = ld_quad<float>(V + e, left);
-      f32x4_t root;
-      adam_quad(g, t.keep, scale, acc[f], w, m, v, root);
-      st_quad(t.W + e, w, left);
-      st_quad(M + e, m, left);
-      st_quad(V + e, v, left);
-      if (t.W16) st_quad(t.W16 + e, w, left);
+  for (int j = 0; j < 4; ++j) {
+    if (64 * j >= cols_left) continue;
+    if (j < 3 && 64 * (j + 1) < cols_left) load(next, j + 1);
+#pragma unroll
+    for (int f = 0; f < 4; ++f) turn[wave][i * 16 + ((4 * f + q) ^ i)] = acc[4 * j + f];
+    __builtin_amdgcn_wave_barrier();
+    f32x4_t gr[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) gr[k] = turn[wave][(4 * k + q) * 16 + (i ^ (4 * k + q))];
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int row = row0 + 4 * k + q;
+      const int64_t e = (int64_t)row * t.cols + c0 + 64 * j + 4 * i;
+      const int left = row < t.rows ? cols_left - 64 * j - 4 * i : 0;
+      f32x4_t m, v, root;
+      if constexpr (BITS == 32) {
+        m = now.m[k];
+        v = now.v[k];
+      } else {
+        m = e4m3_decode(now.cm[k]) * sm[k];
+        root = e4m3_decode(now.cv[k]) * sv[k];
+        v = root * root;
+      }
+      adam_quad(g, t.keep, scale, gr[k], now.w[k], m, v, root);
+      st_quad(t.W + e, now.w[k], left);
+      if (t.W16) st_quad(t.W16 + e, now.w[k], left);
+      if constexpr (BITS == 32) {
+        st_quad((float*)t.m + e, m, left);
+        st_quad((float*)t.v + e, v, left);
+      } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (c >= left) m[c] = root[c] = 0.0f;
+        tm[k] = fmaxf(tm[k], quad_top(m));
+        tv[k] = fmaxf(tv[k], quad_top(root));
+        ms[j][k] = m;
+        roots[j][k] = root;
+      }
     }
-  } else {
-    uint8_t* const M = (uint8_t*)t.m;
-    uint8_t* const V = (uint8_t*)t.v;
-    const int64_t sr = (int64_t)min(row, t.rows - 1) * per_row + run;
-    const float sm = t.m_scale[sr], sv = t.v_scale[sr];
-    float tm = 0.0f, tv = 0.0f;
-    f32x4_t roots[16];
+    now = next;
+  }
+  if constexpr (BITS == 8) {
 #pragma unroll
-    for (int f = 0; f < 16; ++f) {
-      if (f >= nf) continue;
-      const int64_t e = e0 + 16 * f;
-      const int left = left0 - 16 * f;
-      f32x4_t w = ld_quad<float>(t.W + e, left);
-      f32x4_t m = e4m3_decode(ld_codes(M + e, left)) * sm, root = e4m3_decode(ld_codes(V + e, left)) * sv;
-      f32x4_t v = root * root;
-      adam_quad(g, t.keep, scale, acc[f], w, m, v, root);
-      st_quad(t.W + e, w, left);
-      if (t.W16) st_quad(t.W16 + e, w, left);
+    for (int k = 0; k < 4; ++k) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (k >= left) m[k] = root[k] = 0.0f;
-      tm = fmaxf(tm, quad_top(m));
-      tv = fmaxf(tv, quad_top(root));
-      acc[f] = m;
-      roots[f] = root;
-    }
-    // a row's run lies in the lanes i, i + 16, i + 32 and i + 48
-    tm = fmaxf(tm, __shfl_xor(tm, 16));
-    tv = fmaxf(tv, __shfl_xor(tv, 16));
-    tm = run_top(fmaxf(tm, __shfl_xor(tm, 32)));
-    tv = run_top(fmaxf(tv, __shfl_xor(tv, 32)));
-    const float im = (1.0f / tm) * 448.0f, iv = (1.0f / tv) * 448.0f;
+      for (int s = 1; s < 16; s <<= 1) {   // a row's run lies in 16 lanes
+        tm[k] = fmaxf(tm[k], __shfl_xor(tm[k], s));
+        tv[k] = fmaxf(tv[k], __shfl_xor(tv[k], s));
+      }
+      tm[k] = run_top(tm[k]);
+      tv[k] = run_top(tv[k]);
+      const float im = (1.0f / tm[k]) * 448.0f, iv = (1.0f / tv[k]) * 448.0f;
+      const int row = row0 + 4 * k + q;
 #pragma unroll
-    for (int f = 0; f < 16; ++f) {
-      if (f >= nf) continue;
-      const int64_t e = e0 + 16 * f;
-      const int left = left0 - 16 * f;
-      uint32_t cm, cv;
-      encode_quad(acc[f], roots[f], im, iv, (uint64_t)e, t.key, cm, cv);
-      st_codes(M + e, cm, left);
-      st_codes(V + e, cv, left);
-    }
-    if (q == 0 && mine) {
-      t.m_scale[sr] = tm * (1.0f / 448.0f);
-      t.v_scale[sr] = tv * (1.0f / 448.0f);
+      for (int j = 0; j < 4; ++j) {
+        if (64 * j >= cols_left) continue;
+        const int64_t e = (int64_t)row * t.cols + c0 + 64 * j + 4 * i;
+        const int left = row < t.rows ? cols_left - 64 * j - 4 * i : 0;
+        uint32_t cm, cv;
+        encode_quad(ms[j][k], roots[j][k], im, iv, (uint64_t)e, t.key, cm, cv);
+        st_codes((uint8_t*)t.m + e, cm, left);
+        st_codes((uint8_t*)t.v + e, cv, left);
+      }
+      if (i == 0 && row < t.rows) {
+        const int64_t sr = (int64_t)row * per_row + run;
+        t.m_scale[sr] = tm[k] * (1.0f / 448.0f);
+        t.v_scale[sr] = tv[k] * (1.0f / 448.0f);
+      }
     }
   }
 }

@@ -525,15 +525,15 @@ occ_status_t check_param(const occ_param_t& p, std::vector<Span>& spans) {
 }
 
 occ_status_t launch_adam(AdamKind kind, const AdamArgs& a, int64_t blocks, hipStream_t s) {
-  const dim3 grid((unsigned)blocks), block(256);
+  const dim3 grid((unsigned)blocks), block(256), fblock(ADF_WAVES * 64);
   return launch("adamw", s, [&] {
     switch (kind) {
       case AK_F32_32: hipLaunchKernelGGL((k_adamw32<float>), grid, block, 0, s, a); break;
       case AK_BF16_32: hipLaunchKernelGGL((k_adamw32<uint16_t>), grid, block, 0, s, a); break;
       case AK_F32_8: hipLaunchKernelGGL((k_adamw8<float>), grid, block, 0, s, a); break;
       case AK_BF16_8: hipLaunchKernelGGL((k_adamw8<uint16_t>), grid, block, 0, s, a); break;
-      case AK_FACTORS_32: hipLaunchKernelGGL((k_adamw_factors<32>), grid, block, 0, s, a); break;
-      default: hipLaunchKernelGGL((k_adamw_factors<8>), grid, block, 0, s, a); break;
+      case AK_FACTORS_32: hipLaunchKernelGGL((k_adamw_factors<32>), grid, fblock, 0, s, a); break;
+      default: hipLaunchKernelGGL((k_adamw_factors<8>), grid, fblock, 0, s, a); break;
     }
   });
 }
