@@ -128,15 +128,24 @@ template <> __device__ __forceinline__ float ld_elem<uint16_t>(const uint16_t* p
 __device__ __forceinline__ void st_elem(float* p, float v) { *p = v; }
 __device__ __forceinline__ void st_elem(uint16_t* p, float v) { *p = bf16_rne(v); }
 
-// Four consecutive elements, the first `left` of them inside the row.
-template <class T>
+// Four consecutive elements, the first `left` of them inside the row.  NT:
+// nontemporal, for streams whose rows all start on 64 bytes.
+template <class T, bool NT = false>
 __device__ __forceinline__ f32x4_t ld_quad(const T* p, int left) {
   if (left >= 4) {
     if constexpr (sizeof(T) == 4) {
+      if constexpr (NT) return __builtin_nontemporal_load((const f32x4_t*)p);
       const f4u_t v = *(const f4u_t*)p;
       return f32x4_t{v[0], v[1], v[2], v[3]};
     } else {
-      const u2h_t v = *(const u2h_t*)p;
+      typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+      u32x2_t v;
+      if constexpr (NT) {
+        v = __builtin_nontemporal_load((const u32x2_t*)p);
+      } else {
+        const u2h_t u = *(const u2h_t*)p;
+        v = u32x2_t{u[0], u[1]};
+      }
       return f32x4_t{bf16_lo(v[0]), bf16_hi(v[0]), bf16_lo(v[1]), bf16_hi(v[1])};
     }
   }
@@ -147,11 +156,18 @@ __device__ __forceinline__ f32x4_t ld_quad(const T* p, int left) {
   return r;
 }
 
-template <class T>
+template <class T, bool NT = false>
 __device__ __forceinline__ void st_quad(T* p, f32x4_t v, int left) {
   if (left >= 4) {
-    if constexpr (sizeof(T) == 4) *(f4u_t*)p = f4u_t{v[0], v[1], v[2], v[3]};
-    else *(u2h_t*)p = u2h_t{bf16_pack2(v[0], v[1]), bf16_pack2(v[2], v[3])};
+    if constexpr (sizeof(T) == 4) {
+      if constexpr (NT) __builtin_nontemporal_store(v, (f32x4_t*)p);
+      else *(f4u_t*)p = f4u_t{v[0], v[1], v[2], v[3]};
+    } else {
+      typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+      const u32x2_t u = {bf16_pack2(v[0], v[1]), bf16_pack2(v[2], v[3])};
+      if constexpr (NT) __builtin_nontemporal_store(u, (u32x2_t*)p);
+      else *(u2h_t*)p = u2h_t{u[0], u[1]};
+    }
     return;
   }
 #pragma unroll

@@ -524,17 +524,31 @@ occ_status_t check_param(const occ_param_t& p, std::vector<Span>& spans) {
   return OCC_OK;
 }
 
-occ_status_t launch_adam(AdamKind kind, const AdamArgs& a, int64_t blocks, hipStream_t s) {
-  const dim3 grid((unsigned)blocks), block(256), fblock(ADF_WAVES * 64);
+// Whole rows on 64 bytes: the streams may bypass the caches.
+bool streams(const occ_param_t& p) {
+  const bool rows = p.state_bits == 8 || !p.G;   // else W and the moments are one run each
+  if (!aligned(p.W, 64) || !aligned(p.W16, 64) || (rows && p.cols % 32)) return false;
+  if (p.state_bits == 32 && (!aligned(p.m, 64) || !aligned(p.v, 64))) return false;
+  return !p.G || (aligned(p.G, 64) && (p.ldg == p.cols || (size_t)p.ldg * elem_size(p.g_dtype) % 64 == 0));
+}
+
+template <bool NT>
+void start_adam(AdamKind kind, const AdamArgs& a, unsigned blocks, hipStream_t s) {
+  const dim3 grid(blocks), block(256), fblock(ADF_WAVES * 64);
+  switch (kind) {
+    case AK_F32_32: hipLaunchKernelGGL((k_adamw32<float, NT>), grid, block, 0, s, a); break;
+    case AK_BF16_32: hipLaunchKernelGGL((k_adamw32<uint16_t, NT>), grid, block, 0, s, a); break;
+    case AK_F32_8: hipLaunchKernelGGL((k_adamw8<float, NT>), grid, block, 0, s, a); break;
+    case AK_BF16_8: hipLaunchKernelGGL((k_adamw8<uint16_t, NT>), grid, block, 0, s, a); break;
+    case AK_FACTORS_32: hipLaunchKernelGGL((k_adamw_factors<32, NT>), grid, fblock, 0, s, a); break;
+    default: hipLaunchKernelGGL((k_adamw_factors<8, NT>), grid, fblock, 0, s, a); break;
+  }
+}
+
+occ_status_t launch_adam(AdamKind kind, bool nt, const AdamArgs& a, int64_t blocks, hipStream_t s) {
   return launch("adamw", s, [&] {
-    switch (kind) {
-      case AK_F32_32: hipLaunchKernelGGL((k_adamw32<float>), grid, block, 0, s, a); break;
-      case AK_BF16_32: hipLaunchKernelGGL((k_adamw32<uint16_t>), grid, block, 0, s, a); break;
-      case AK_F32_8: hipLaunchKernelGGL((k_adamw8<float>), grid, block, 0, s, a); break;
-      case AK_BF16_8: hipLaunchKernelGGL((k_adamw8<uint16_t>), grid, block, 0, s, a); break;
-      case AK_FACTORS_32: hipLaunchKernelGGL((k_adamw_factors<32>), grid, fblock, 0, s, a); break;
-      default: hipLaunchKernelGGL((k_adamw_factors<8>), grid, fblock, 0, s, a); break;
-    }
+    if (nt) start_adam<true>(kind, a, (unsigned)blocks, s);
+    else start_adam<false>(kind, a, (unsigned)blocks, s);
   });
 }
 
@@ -561,15 +575,18 @@ occ_status_t adamw(const occ_param_t* params, int count, const occ_adamw_t* h, h
   a.eps = (float)h->eps;
   a.grad_scale = h->grad_scale;
   a.flags = h->flags;
-  for (int kind = 0; kind < AK_NUM; ++kind) {
+  // one launch for each form of gradient, moments and alignment among the tensors
+  for (int form = 0; form < 2 * AK_NUM; ++form) {
+    const AdamKind kind = (AdamKind)(form >> 1);
+    const bool nt = form & 1;
     int64_t blocks = 0;
     a.count = 0;
     for (int j = 0; j < count; ++j) {
       const occ_param_t& p = params[j];
-      if (kind_of(p) != kind) continue;
+      if (kind_of(p) != kind || streams(p) != nt) continue;
       const int64_t nb = adam_blocks(p);
       if (a.count == kAdamTensors || blocks + nb >= kMaxTokens) {
-        OCC_TRY(launch_adam((AdamKind)kind, a, blocks, s));
+        OCC_TRY(launch_adam(kind, nt, a, blocks, s));
         a.count = 0;
         blocks = 0;
       }
@@ -592,7 +609,7 @@ occ_status_t adamw(const occ_param_t* params, int count, const occ_adamw_t* h, h
       t.key = (h->seed + (uint32_t)j * 0x6A09E667u) * 0xBB67AE85u;
       blocks += nb;
     }
-    if (a.count) OCC_TRY(launch_adam((AdamKind)kind, a, blocks, s));
+    if (a.count) OCC_TRY(launch_adam(kind, nt, a, blocks, s));
   }
   return OCC_OK;
 }
