@@ -60,14 +60,6 @@ __global__ __launch_bounds__(SK_WAVES * 64) void k_skinny(SkinnyArgs g) {
 #pragma unroll
   for (int t = 0; t < NT; ++t) x[t] = (const T*)g.X + (int64_t)min(16 * t + i, g.tokens - 1) * g.ldx + q * CH;
   f32x4_t acc[NW][NT] = {};
-  const int full = g.in / BK;
-  constexpr int U = NT == 1 ? 4 : 2;
-  auto step = [&](const Frag<ES>* fw, const Frag<ES>* fx) {
-#pragma unroll
-    for (int a = 0; a < NW; ++a)
-#pragma unroll
-      for (int t = 0; t < NT; ++t) acc[a][t] = mfma_tile<ES>(fw[a], fx[t], acc[a][t]);
-  };
   // pieces q and q + 4 of each row's tile
   auto load = [&](const T* p, int64_t k, int left) {
     Frag<ES> f;
@@ -75,29 +67,51 @@ __global__ __launch_bounds__(SK_WAVES * 64) void k_skinny(SkinnyArgs g) {
     for (int s = 0; s < 2; ++s) f.v[s] = ld_piece<T>(p + k + s * 4 * CH, left - s * 4 * CH);
     return f;
   };
-  int kt = wave;
-  for (; kt + (U - 1) * SK_WAVES < full; kt += U * SK_WAVES) {
-    Frag<ES> fw[U][NW], fx[U][NT];
+  struct Step {
+    Frag<ES> w[NW], x[NT];
+  };
+  auto step = [&](const Step& f) {
+#pragma unroll
+    for (int a = 0; a < NW; ++a)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) acc[a][t] = mfma_tile<ES>(f.w[a], f.x[t], acc[a][t]);
+  };
+  // Two runs of U tiles are in flight: one is multiplied while the next loads.
+  constexpr int U = NT == 1 ? 4 : 2;
+  const int full = g.in / BK;
+  const int runs = full > wave ? ((full - wave - 1) / SK_WAVES + 1) / U : 0;   // whole runs of this wave
+  Step one[U], two[U];
+  auto fetch = [&](Step* f, int run) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t k = (int64_t)(kt + u * SK_WAVES) * BK;
+      const int64_t k = (int64_t)(wave + (run * U + u) * SK_WAVES) * BK;
 #pragma unroll
-      for (int a = 0; a < NW; ++a) fw[u][a] = load(w[a], k, BK);
+      for (int a = 0; a < NW; ++a) f[u].w[a] = load(w[a], k, BK);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) fx[u][t] = load(x[t], k, BK);
+      for (int t = 0; t < NT; ++t) f[u].x[t] = load(x[t], k, BK);
     }
+  };
+  auto multiply = [&](const Step* f) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) step(fw[u], fx[u]);
+    for (int u = 0; u < U; ++u) step(f[u]);
+  };
+  if (runs) fetch(one, 0);
+  for (int r = 0; r < runs; r += 2) {
+    if (r + 1 < runs) fetch(two, r + 1);
+    multiply(one);
+    if (r + 1 >= runs) break;
+    if (r + 2 < runs) fetch(one, r + 2);
+    multiply(two);
   }
-  for (; (int64_t)kt * BK < g.in; kt += SK_WAVES) {
+  for (int kt = wave + runs * U * SK_WAVES; (int64_t)kt * BK < g.in; kt += SK_WAVES) {
     const int64_t k = (int64_t)kt * BK;
     const int left = (int)min((int64_t)BK, g.in - k) - q * CH;
-    Frag<ES> fw[NW], fx[NT];
+    Step f;
 #pragma unroll
-    for (int a = 0; a < NW; ++a) fw[a] = load(w[a], k, left);
+    for (int a = 0; a < NW; ++a) f.w[a] = load(w[a], k, left);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) fx[t] = load(x[t], k, left);
-    step(fw, fx);
+    for (int t = 0; t < NT; ++t) f.x[t] = load(x[t], k, left);
+    step(f);
   }
 #pragma unroll
   for (int a = 0; a < NW; ++a)

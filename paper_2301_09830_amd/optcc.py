@@ -270,15 +270,23 @@ def occ_status_str(status: int) -> str:
 # ----------------------------------------------------------------------------
 # tensor marshalling
 # ----------------------------------------------------------------------------
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def _stream(stream=None) -> int:
+    if stream is not None:
+        return int(stream.cuda_stream)
     torch = _torch()
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return int(s.cuda_stream)
+    # torch.cuda.current_stream().cuda_stream without the Stream object (3 us a call)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _ptr(t) -> int | None:
@@ -569,17 +577,22 @@ def _mat(t, name: str, rows: int, cols: int, dtype):
     """(pointer, leading dimension) of an optional rows x cols matrix."""
     if t is None:
         return None, 0
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}")
-    if tuple(t.shape) != (rows, cols):
+    if t.shape != (rows, cols):
         raise ValueError(f"{name} must be {rows} x {cols}")
-    return t.data_ptr() if rows else None, _ld(t, name) if rows else cols
+    ld, unit = t.stride()
+    if unit != 1 and cols > 1:
+        raise ValueError(f"{name} must have unit column stride (row-major)")
+    if rows <= 1:
+        return (t.data_ptr() if rows else None), cols
+    return t.data_ptr(), ld
 
 
 def _vec(t, name: str, n: int):
     if t is None:
         return None
-    if t.dtype != _torch().float32:
+    if t.dtype is not _torch().float32:
         raise TypeError(f"{name} must be float32")
     if t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name} must hold {n} contiguous values")
@@ -598,28 +611,44 @@ def _workspace(nbytes: int, ws, device):
     return ws, ws.data_ptr(), ws.numel()
 
 
+def _rows_cols(t, name: str):
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be 2-D")
+    return t.shape
+
+
 def _layer_fwd(name: str, wide: int, X, W, bias, act, R, Y, Z, ws, stream):
-    torch = _torch()
-    tokens, n_in = X.shape
-    if W.shape[0] % wide:
+    tokens, n_in = _rows_cols(X, "X")
+    rows, _ = _rows_cols(W, "W")
+    out = rows // wide
+    if rows != wide * out:
         raise ValueError("W must hold the rows of both projections")
-    out = W.shape[0] // wide
+    dt = X.dtype
     if Y is None:
-        Y = torch.empty((tokens, out), dtype=X.dtype, device=X.device)
-    a = occ_linear_t()
-    a.dtype, a.act = _mdtype(X), int(act)
-    a.tokens, a.in_, a.out = tokens, n_in, out
-    a.X, a.ldx = _mat(X, "X", tokens, n_in, X.dtype)
-    a.W, a.ldw = _mat(W, "W", wide * out, n_in, X.dtype)
-    a.bias = _vec(bias, "bias", wide * out)
-    a.R, a.ldr = _mat(R, "R", tokens, out, X.dtype)
-    a.Z, a.ldz = _mat(Z, "Z", tokens, wide * out, X.dtype)
-    a.Y, a.ldy = _mat(Y, "Y", tokens, out, X.dtype)
-    L = lib()
-    p = ctypes.byref(a)
-    keep, wp, wn = _workspace(getattr(L, name + "_workspace_bytes")(p), ws, X.device)
-    _check(name, getattr(L, name)(p, wp, wn, _stream(stream)))
+        Y = _torch().empty((tokens, out), dtype=dt, device=X.device)
+    x, ldx = _mat(X, "X", tokens, n_in, dt)
+    w, ldw = _mat(W, "W", rows, n_in, dt)
+    r, ldr = _mat(R, "R", tokens, out, dt)
+    z, ldz = _mat(Z, "Z", tokens, rows, dt)
+    y, ldy = _mat(Y, "Y", tokens, out, dt)
+    a = occ_linear_t(_mdtype(X), act, tokens, n_in, out, x, ldx, w, ldw, _vec(bias, "bias", rows),
+                     r, ldr, z, ldz, y, ldy)
+    call, size = _layer_calls(name)
+    keep, wp, wn = _workspace(size(a), ws, X.device)
+    _check(name, call(a, wp, wn, _stream(stream)))
     return Y
+
+
+_layer_functions = {}
+
+
+def _layer_calls(name: str):
+    """(the call, its workspace size) of a layer's function."""
+    got = _layer_functions.get(name)
+    if got is None:
+        L = lib()
+        got = _layer_functions[name] = (getattr(L, name), getattr(L, name + "_workspace_bytes"))
+    return got
 
 
 def occ_linear_fwd(X, W, bias=None, act: int = OCC_ACT_NONE, R=None, Y=None, Z=None, ws=None,
@@ -643,29 +672,25 @@ def occ_gated_fwd(X, W, bias=None, act: int = OCC_ACT_SILU, R=None, Y=None, Z=No
 
 def _layer_bwd(name: str, wide: int, dY, X, W, Z, act, dX, dW, dbias, accumulate, ws, stream):
     torch = _torch()
-    tokens, out = dY.shape
+    tokens, out = _rows_cols(dY, "dY")
     some = X if X is not None else W if W is not None else dX if dX is not None else dW
-    n_in = 1 if some is None else some.shape[1]
-    a = occ_linear_grad_t()
-    a.dtype = _mdtype(dY)
-    a.dw_dtype = a.dtype if dW is None else _mdtype(dW)
-    a.act = int(act)
-    a.tokens, a.in_, a.out = tokens, n_in, out
-    a.dY, a.lddy = _mat(dY, "dY", tokens, out, dY.dtype)
-    a.X, a.ldx = _mat(X, "X", tokens, n_in, dY.dtype)
-    a.W, a.ldw = _mat(W, "W", wide * out, n_in, dY.dtype)
-    a.Z, a.ldz = _mat(Z, "Z", tokens, wide * out, dY.dtype)
-    a.dX, a.lddx = _mat(dX, "dX", tokens, n_in, dY.dtype)
-    a.dW, a.lddw = _mat(dW, "dW", wide * out, n_in, torch.float32 if a.dw_dtype == OCC_F32
-                        else torch.bfloat16)
-    a.dbias = _vec(dbias, "dbias", wide * out)
+    n_in = 1 if some is None else _rows_cols(some, "X and W")[1]
     if tokens == 0 and dX is not None and dW is None and dbias is None:
         return      # an empty dX
-    L = lib()
-    p = ctypes.byref(a)
-    keep, wp, wn = _workspace(getattr(L, name + "_workspace_bytes")(p), ws, dY.device)
-    _check(name, getattr(L, name)(p, OCC_GRAD_ACCUMULATE if accumulate else 0, wp, wn,
-                                  _stream(stream)))
+    dt, rows = dY.dtype, wide * out
+    dw_dt = dt if dW is None or dW.dtype is not torch.float32 else torch.float32
+    dy, lddy = _mat(dY, "dY", tokens, out, dt)
+    x, ldx = _mat(X, "X", tokens, n_in, dt)
+    w, ldw = _mat(W, "W", rows, n_in, dt)
+    z, ldz = _mat(Z, "Z", tokens, rows, dt)
+    dx, lddx = _mat(dX, "dX", tokens, n_in, dt)
+    dw, lddw = _mat(dW, "dW", rows, n_in, dw_dt)
+    a = occ_linear_grad_t(_mdtype(dY), OCC_F32 if dw_dt is torch.float32 else OCC_BF16, act, 0,
+                          tokens, n_in, out, dy, lddy, x, ldx, w, ldw, z, ldz, dx, lddx, dw, lddw,
+                          _vec(dbias, "dbias", rows))
+    call, size = _layer_calls(name)
+    keep, wp, wn = _workspace(size(a), ws, dY.device)
+    _check(name, call(a, OCC_GRAD_ACCUMULATE if accumulate else 0, wp, wn, _stream(stream)))
 
 
 def occ_linear_bwd(dY, X=None, W=None, Z=None, act: int = OCC_ACT_NONE, dX=None, dW=None,
