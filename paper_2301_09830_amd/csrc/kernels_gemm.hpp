@@ -86,34 +86,45 @@ __device__ __forceinline__ f32x4_t act_quad(int act, f32x4_t z) {
 }
 
 // act(z) and act'(z)
-__device__ __forceinline__ void act_grad_f(int act, float z, float& a, float& da) {
+__device__ __forceinline__ void act_grad_quad(int act, f32x4_t z, f32x4_t& a, f32x4_t& da) {
   float e;
   switch (act) {
     case ACT_RELU:
-      a = z > 0.0f || z != z ? z : 0.0f;
-      da = z > 0.0f ? 1.0f : 0.0f;
-      return;
-    case ACT_GELU: {
-      const float c = normal_cdf(z, e);
-      a = z * c;
-      da = __builtin_fmaf(z * 0.3989422804014327f, e, c);
-      return;
-    }
-    case ACT_GELU_TANH: {
-      const float zz = fminf(z * z, 1e30f);   // finite: it meets a factor that is 0 there
-      const float s = sigmoid_f(2.0f * kGeluC * z * __builtin_fmaf(kGeluA, zz, 1.0f));
-      a = z * s;
-      // z s (1 - s) 2 q'(z) + s
-      da = __builtin_fmaf(a * (1.0f - s), 2.0f * kGeluC * __builtin_fmaf(3.0f * kGeluA, zz, 1.0f), s);
-      return;
-    }
-    case ACT_SILU: {
-      const float s = sigmoid_f(z);
-      a = z * s;
-      da = __builtin_fmaf(a, 1.0f - s, s);
-      return;
-    }
-    default: a = z; da = 1.0f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        a[i] = z[i] > 0.0f || z[i] != z[i] ? z[i] : 0.0f;
+        da[i] = z[i] > 0.0f ? 1.0f : 0.0f;
+      }
+      break;
+    case ACT_GELU:
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float c = normal_cdf(z[i], e);
+        a[i] = z[i] * c;
+        da[i] = __builtin_fmaf(z[i] * 0.3989422804014327f, e, c);
+      }
+      break;
+    case ACT_GELU_TANH:
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float zz = fminf(z[i] * z[i], 1e30f);   // finite: it meets a factor that is 0 there
+        const float s = sigmoid_f(z[i] * __builtin_fmaf(2.0f * kGeluC * kGeluA, zz, 2.0f * kGeluC));
+        a[i] = z[i] * s;
+        // z s (1 - s) 2 q'(z) + s
+        da[i] = __builtin_fmaf(a[i] * (1.0f - s), __builtin_fmaf(6.0f * kGeluC * kGeluA, zz, 2.0f * kGeluC), s);
+      }
+      break;
+    case ACT_SILU:
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float s = sigmoid_f(z[i]);
+        a[i] = z[i] * s;
+        da[i] = __builtin_fmaf(a[i], 1.0f - s, s);
+      }
+      break;
+    default:
+      a = z;
+      da = f32x4_t{1.0f, 1.0f, 1.0f, 1.0f};
   }
 }
 
@@ -187,6 +198,7 @@ struct FwdEpi {
   int64_t ldr;
   const float* bias;   // may be null
   int32_t act;
+  int32_t stream;      // Y and Z bypass the caches (rows on 64 bytes)
   int32_t out;         // columns of Y; gated: W, bias and Z hold the gate's rows, then the others'
 };
 
@@ -195,20 +207,36 @@ __device__ __forceinline__ f32x4_t bias_quad(const FwdEpi& e, int n, int left) {
   return e.bias ? ld_quad<float>(e.bias + n, left) : f32x4_t{};
 }
 
+// R[m][n .. n + 3], zeros without one
+template <class T>
+__device__ __forceinline__ f32x4_t residual_quad(const FwdEpi& e, int64_t m, int n, int left) {
+  return e.R ? ld_quad<T>((const T*)e.R + m * e.ldr + n, left) : f32x4_t{};
+}
+
 // Columns n .. n + 3 of token m: z (and u, the other projection, when gated)
-// are sums of products in fp32, the bias added.
+// are sums of products in fp32, the bias added; r is the residual.
 template <class T, bool GATED>
-__device__ __forceinline__ void fwd_epilogue(const FwdEpi& e, int64_t m, int n, f32x4_t z, f32x4_t u) {
+__device__ __forceinline__ void fwd_epilogue(const FwdEpi& e, int64_t m, int n, f32x4_t z, f32x4_t u, f32x4_t r) {
   const int left = e.out - n;
   if (left <= 0) return;
-  if (e.Z) {
-    st_quad((T*)e.Z + m * e.ldz + n, z, left);
-    if constexpr (GATED) st_quad((T*)e.Z + m * e.ldz + e.out + n, u, left);
-  }
+  T* const zp = (T*)e.Z + m * e.ldz + n;
+  T* const yp = (T*)e.Y + m * e.ldy + n;
   f32x4_t y = act_quad(e.act, z);
   if constexpr (GATED) y *= u;
-  if (e.R) y += ld_quad<T>((const T*)e.R + m * e.ldr + n, left);
-  st_quad((T*)e.Y + m * e.ldy + n, y, left);
+  y += r;
+  if (e.stream) {
+    if (e.Z) {
+      st_quad<T, true>(zp, z, left);
+      if constexpr (GATED) st_quad<T, true>(zp + e.out, u, left);
+    }
+    st_quad<T, true>(yp, y, left);
+  } else {
+    if (e.Z) {
+      st_quad(zp, z, left);
+      if constexpr (GATED) st_quad(zp + e.out, u, left);
+    }
+    st_quad(yp, y, left);
+  }
 }
 
 // ----------------------------------------------------------------------------
@@ -225,7 +253,7 @@ struct GemmArgs {
   float* part;        // splits > 1: partial sums, splits x M x width
   void* C;            // EP_STORE: the result
   int64_t ldc;
-  int32_t c_f32, accumulate;
+  int32_t c_f32, accumulate, stream;
   FwdEpi fwd;
 };
 
@@ -268,7 +296,9 @@ struct Operand {
   // takes rows k + {0..3} (bf16: of two groups 8 rows apart; fp32: rows 4
   // apart) and a run of 32 (64) bytes of each.
   static __device__ __forceinline__ int turn(int k) {
-    return ES == 2 ? ((k & 3) | ((k >> 1) & 4)) << 1 : ((k >> 2) & 3) << 2;
+    if (ES == 4) return ((k >> 2) & 3) << 2;
+    // rows of 128 bytes: odd and even rows lie in different halves of the banks
+    return (KROW == 128 ? (k & 3) ^ ((k >> 3) & 1) : (k & 3) | ((k >> 1) & 4)) << 1;
   }
 
   // row_of(r): row of the operand held in row r of the tile, inside the array;
@@ -321,80 +351,82 @@ template <int R, bool KS, int ES>
 struct Reader {
   uint32_t at[KS ? R / 16 : 2];
 
-  // first: the wave's first row in the tile (K strided: a multiple of R rows)
+  // first: the wave's first row in the tile (K strided: a multiple of R rows);
+  // KROW: bytes of a row of the tile, K strided
+  template <int KROW>
   __device__ __forceinline__ void init(int first, int lane) {
     const int i = lane & 15, g = lane >> 4;
     if constexpr (!KS) {
 #pragma unroll
       for (int s = 0; s < 2; ++s) at[s] = (first + i) * kRowBytes + (((4 * s + g) ^ (i & 7)) << 4);
     } else if constexpr (ES == 2) {
-      const int r = i >> 2, f = r | ((g & 1) << 2);
+      const int k = 8 * g + (i >> 2), f = Operand<KROW / ES, true, ES, 1>::turn(k) >> 1;
 #pragma unroll
-      for (int a = 0; a < R / 16; ++a) at[a] = ((((first >> 4) + a) ^ f) << 5) + (i & 3) * 8;
+      for (int a = 0; a < R / 16; ++a) at[a] = k * KROW + ((((first >> 4) + a) ^ f) << 5) + (i & 3) * 8;
     } else {
 #pragma unroll
-      for (int a = 0; a < R / 16; ++a) at[a] = ((((first >> 4) + a) ^ g) << 6) + i * 4;
+      for (int a = 0; a < R / 16; ++a) at[a] = 4 * g * KROW + ((((first >> 4) + a) ^ g) << 6) + i * 4;
     }
   }
 
+  // half s of K, of rows 16 a .. 16 a + 15
   template <int KROW>
-  __device__ __forceinline__ void add_row(int lane) {
-    const int i = lane & 15, g = lane >> 4;
-    if constexpr (KS) {
-      const int k = ES == 2 ? 8 * g + (i >> 2) : 4 * g;
+  __device__ __forceinline__ f32x4_t read_half(const lds_char* tile, int a, int s) const {
+    if constexpr (!KS) {
+      return *(const __attribute__((address_space(3))) f32x4_t*)(tile + at[s] + a * 16 * kRowBytes);
+    } else if constexpr (ES == 2) {
+      typedef __attribute__((address_space(3))) s16x4_t lds_s4;
+      const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(tile + at[a] + 32 * s * KROW));
+      const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(tile + at[a] + (32 * s + 4) * KROW));
+      typedef short s16x8_t __attribute__((ext_vector_type(8)));
+      return __builtin_bit_cast(f32x4_t, (s16x8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+      f32x4_t v;
 #pragma unroll
-      for (int a = 0; a < R / 16; ++a) at[a] += k * KROW;
+      for (int j = 0; j < 4; ++j)
+        v[j] = *(const __attribute__((address_space(3))) float*)(tile + at[a] + (16 * s + j) * KROW);
+      return v;
     }
   }
 
   template <int KROW>
   __device__ __forceinline__ Frag<ES> read(const lds_char* tile, int a) const {
     Frag<ES> f;
-    if constexpr (!KS) {
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
-        f.v[s] = *(const __attribute__((address_space(3))) f32x4_t*)(tile + at[s] + a * 16 * kRowBytes);
-    } else if constexpr (ES == 2) {
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        typedef __attribute__((address_space(3))) s16x4_t lds_s4;
-        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(tile + at[a] + 32 * s * KROW));
-        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(tile + at[a] + (32 * s + 4) * KROW));
-        typedef short s16x8_t __attribute__((ext_vector_type(8)));
-        f.v[s] = __builtin_bit_cast(f32x4_t, (s16x8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-      }
-    } else {
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          f.v[s][j] = *(const __attribute__((address_space(3))) float*)(tile + at[a] + (16 * s + j) * KROW);
-    }
+    for (int s = 0; s < 2; ++s) f.v[s] = read_half<KROW>(tile, a, s);
     return f;
   }
 };
 
 template <int ES>
-__device__ __forceinline__ f32x4_t mfma_tile(const Frag<ES>& b, const Frag<ES>& a, f32x4_t c) {
+__device__ __forceinline__ f32x4_t mfma_half(f32x4_t b, f32x4_t a, f32x4_t c) {
   if constexpr (ES == 2) {
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, b.v[s]),
-                                                  __builtin_bit_cast(bf16x8_t, a.v[s]), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, b), __builtin_bit_cast(bf16x8_t, a), c,
+                                                   0, 0, 0);
   } else {
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(b.v[s][j], a.v[s][j], c, 0, 0, 0);
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(b[j], a[j], c, 0, 0, 0);
+    return c;
   }
+}
+
+template <int ES>
+__device__ __forceinline__ f32x4_t mfma_tile(const Frag<ES>& b, const Frag<ES>& a, f32x4_t c) {
+#pragma unroll
+  for (int s = 0; s < 2; ++s) c = mfma_half<ES>(b.v[s], a.v[s], c);
   return c;
 }
 
 // Tile (tm, tn) of a block.  Workgroups are dealt to the XCDs round-robin;
-// xcd_tile() gives each XCD a contiguous run of tiles, and the run walks
+// xcd_order gives each XCD a contiguous run of the n tiles, and the run walks
 // bands of kBand tile rows column by column, so that the tiles of one XCD at
 // one time form a near-square and share rows of A and B in its L2.
 constexpr int kBand = 8;
+
+__device__ __forceinline__ int xcd_order(int b, int n) {
+  const int n8 = n & ~7;
+  return b < n8 ? (b & 7) * (n8 >> 3) + (b >> 3) : b;
+}
 
 __device__ __forceinline__ void band_tile(int t, int tiles_m, int tiles_n, int& tm, int& tn) {
   const int per = kBand * tiles_n;
@@ -404,43 +436,58 @@ __device__ __forceinline__ void band_tile(int t, int tiles_m, int tiles_n, int& 
   tm = band * kBand + in - tn * h;
 }
 
-// Passes that the results of a tile take through the LDS of its two stages.
-template <int BM, int BN, int STAGE>
-constexpr int PR_PASSES = BM * BN * 4 / (2 * STAGE) > 0 ? BM * BN * 4 / (2 * STAGE) : 1;
+// Passes that the results of a tile take through the LDS of its stages.
+template <int BM, int BN, int BYTES>
+constexpr int PR_PASSES = (BM * BN * 4 + BYTES - 1) / BYTES;
 
 // Four results of a gradient: stored, or added to what is there.
-template <class T>
-__device__ __forceinline__ void store_result(const GemmArgs& g, int64_t m, int n, f32x4_t v, int left) {
-  if (sizeof(T) == 4 || g.c_f32) {
-    float* const p = (float*)g.C + m * g.ldc + n;
-    if (g.accumulate) v += ld_quad<float>(p, left);
-    st_quad(p, v, left);
-  } else {
-    uint16_t* const p = (uint16_t*)g.C + m * g.ldc + n;
-    if (g.accumulate) v += ld_quad<uint16_t>(p, left);
-    st_quad(p, v, left);
-  }
+template <class TC>
+__device__ __forceinline__ void store_as(const GemmArgs& g, int64_t m, int n, f32x4_t v, int left) {
+  TC* const p = (TC*)g.C + m * g.ldc + n;
+  if (g.accumulate) v += ld_quad<TC>(p, left);
+  if (g.stream) st_quad<TC, true>(p, v, left);
+  else st_quad(p, v, left);
 }
 
-// WM x WN waves, each 16 FA x 16 FB results.  PP: the waves form two groups
-// (one wave of each on every SIMD) that alternate between matrix
-// instructions and LDS reads; see the loop.
-template <class T, int WM, int WN, int FA, int FB, bool AKS, bool BKS, int EP, bool PP>
-__global__ __launch_bounds__(WM * WN * 64, PP ? 2 : 2) void k_gemm(GemmArgs g) {
-  constexpr int ES = sizeof(T), NW = WM * WN;
-  constexpr int BM = WM * FA * 16, BN = WN * FB * 16;
+template <class T>
+__device__ __forceinline__ void store_result(const GemmArgs& g, int64_t m, int n, f32x4_t v, int left) {
+  if (sizeof(T) == 4 || g.c_f32) store_as<float>(g, m, n, v, left);
+  else store_as<uint16_t>(g, m, n, v, left);
+}
+
+// A form of the product: WM x WN waves, each 16 FA x 16 FB results, S stages
+// of K tiles in LDS.
+// S == 2 (256 x 256): the waves form two groups, one wave of each on every
+// SIMD, that alternate between matrix instructions and LDS reads.
+// S == 4 (128 x 128 and 64 x 64): tiles are loaded three ahead, one barrier a
+// tile; two waves a SIMD, since one alone stands still while its loads are
+// issued (4096^3 bf16 at 128 x 128: 203 us on four waves, 151 on eight).
+template <int WM_, int WN_, int FA_, int FB_, int S_>
+struct Form {
+  static constexpr int WM = WM_, WN = WN_, FA = FA_, FB = FB_, S = S_;
+  static constexpr int NW = WM * WN, BM = WM * FA * 16, BN = WN * FB * 16;
+  static constexpr int LDS = S * (BM + BN) * kRowBytes;
+};
+using Form256 = Form<2, 4, 8, 4, 2>;
+using Form128 = Form<2, 4, 4, 2, 4>;
+using Form64 = Form<4, 2, 1, 2, 4>;
+
+// Block `block` of a product: all of its tile's K, or one part of it.
+template <class T, class F, bool AKS, bool BKS, int EP>
+__device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_char* lds) {
+  constexpr int ES = sizeof(T), S = F::S, NW = F::NW, WM = F::WM, WN = F::WN, FA = F::FA, FB = F::FB;
+  constexpr int BM = F::BM, BN = F::BN;
+  constexpr bool PP = S == 2;
   using OA = Operand<BM, AKS, ES, NW>;
   using OB = Operand<BN, BKS, ES, NW>;
   constexpr int STAGE = OA::BYTES + OB::BYTES;
   constexpr int BK = OA::BK;
-  __shared__ __attribute__((aligned(1024))) char sm[2 * STAGE];
-  lds_char* const lds = (lds_char*)sm;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
   const int wave = wave_id(), lane = threadIdx.x & 63;
   const int wm = wave / WN, wn = wave % WN;
   int tm, tn;
-  const int t = xcd_tile();
   const int per_split = g.tiles_m * g.tiles_n;
+  const int t = xcd_order(block, per_split * g.splits);
   const int split = t / per_split;
   band_tile(t - split * per_split, g.tiles_m, g.tiles_n, tm, tn);
   const int kt0 = split * g.k_per_split;
@@ -464,10 +511,8 @@ __global__ __launch_bounds__(WM * WN * 64, PP ? 2 : 2) void k_gemm(GemmArgs g) {
   });
   Reader<FA * 16, AKS, ES> ra;
   Reader<FB * 16, BKS, ES> rb;
-  ra.init(wm * FA * 16, lane);
-  rb.init(wn * FB * 16, lane);
-  ra.template add_row<OA::KROW>(lane);
-  rb.template add_row<OB::KROW>(lane);
+  ra.template init<OA::KROW>(wm * FA * 16, lane);
+  rb.template init<OB::KROW>(wn * FB * 16, lane);
 
   f32x4_t acc[FA][FB];
 #pragma unroll
@@ -479,89 +524,119 @@ __global__ __launch_bounds__(WM * WN * 64, PP ? 2 : 2) void k_gemm(GemmArgs g) {
   auto load_a = [&](int stage) { oa.load(lds0 + stage * STAGE, wave, left_a); left_a -= BK; };
   auto load_b = [&](int stage) { ob.load(lds0 + stage * STAGE + OA::BYTES, wave, left_b); left_b -= BK; };
 
-  constexpr int HA = FA / 2, HB = FB / 2;
-  Frag<ES> a0[HA], a1[HA], b0[HB], b1[HB];
-  // fragments i0 .. i1 - 1 of a half
-  auto read_a = [&](Frag<ES>* f, int stage, int half, int i0, int i1) {
-    const lds_char* p = lds + stage * STAGE;
+  if constexpr (PP) {
+    constexpr int HA = FA / 2, HB = FB / 2, Q1 = HA / 4, Q2 = HA / 2;
+    Frag<ES> a0[HA], a1[HA], b0[HB], b1[HB];
+    // fragments i0 .. i1 - 1 of a half
+    auto read_a = [&](Frag<ES>* f, int stage, int half, int i0, int i1) {
+      const lds_char* p = lds + stage * STAGE;
 #pragma unroll
-    for (int i = 0; i < HA; ++i)
-      if (i >= i0 && i < i1) f[i] = ra.template read<OA::KROW>(p, half * HA + i);
-  };
-  auto read_b = [&](Frag<ES>* f, int stage, int half) {
-    const lds_char* p = lds + stage * STAGE + OA::BYTES;
+      for (int i = 0; i < HA; ++i)
+        if (i >= i0 && i < i1) f[i] = ra.template read<OA::KROW>(p, half * HA + i);
+    };
+    auto read_b = [&](Frag<ES>* f, int stage, int half) {
+      const lds_char* p = lds + stage * STAGE + OA::BYTES;
 #pragma unroll
-    for (int i = 0; i < HB; ++i) f[i] = rb.template read<OB::KROW>(p, half * HB + i);
-  };
-  auto multiply = [&](const Frag<ES>* a, const Frag<ES>* b, int ha, int hb) {
-#pragma unroll
-    for (int i = 0; i < HA; ++i)
-#pragma unroll
-      for (int j = 0; j < HB; ++j)
-        acc[ha * HA + i][hb * HB + j] = mfma_tile<ES>(b[j], a[i], acc[ha * HA + i][hb * HB + j]);
-  };
-  auto before = [&]() {   // of a run of matrix instructions
-    if constexpr (PP) {
+      for (int i = 0; i < HB; ++i) f[i] = rb.template read<OB::KROW>(p, half * HB + i);
+    };
+    // a run of matrix instructions, while the other group reads
+    auto multiply = [&](const Frag<ES>* a, const Frag<ES>* b, int ha, int hb) {
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
       __builtin_amdgcn_sched_barrier(0);
       __builtin_amdgcn_s_setprio(1);
-    }
-  };
-  auto after = [&]() {
-    if constexpr (PP) {
+#pragma unroll
+      for (int i = 0; i < HA; ++i)
+#pragma unroll
+        for (int j = 0; j < HB; ++j)
+          acc[ha * HA + i][hb * HB + j] = mfma_tile<ES>(b[j], a[i], acc[ha * HA + i][hb * HB + j]);
       __builtin_amdgcn_s_setprio(0);
       __builtin_amdgcn_sched_barrier(0);
       asm volatile("s_barrier" ::: "memory");
+    };
+    load_a(0);
+    load_b(0);
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    if (nk > 1) {
+      load_b(1);
+      load_a(1);
     }
-  };
-
-  load_a(0);
-  load_b(0);
-  asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-  if (nk > 1) {
-    load_b(1);
-    load_a(1);
-  }
-  read_a(a0, 0, 0, 0, HA);
-  if constexpr (PP) {
+    read_a(a0, 0, 0, 0, HA);
     if (wave >= NW / 2) asm volatile("s_barrier" ::: "memory");
-  }
-  // The quarters of the wave's results, in an order that needs one new half
-  // operand each; the reads are spread so that each run of matrix
-  // instructions covers the same number of them.  Loads of tile t + 1 end
-  // before its first read (the wait before the second quarter, and a barrier
-  // after it); the stage of tile t is loaded again only after every wave's
-  // last read of it: B from the third quarter on, A from the fourth.
-  constexpr int Q1 = HA / 4, Q2 = HA / 2;
-  for (int kt = 0; kt < nk; ++kt) {
-    const int st = kt & 1;
-    read_b(b0, st, 0);
-    read_a(a1, st, 1, 0, Q1);
-    before();
-    multiply(a0, b0, 0, 0);
-    after();
-    read_b(b1, st, 1);
-    read_a(a1, st, 1, Q1, Q2);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    if constexpr (!PP) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    before();
-    multiply(a0, b1, 0, 1);
-    after();
-    read_a(a1, st, 1, Q2, HA);
-    if (kt + 1 < nk) read_a(a0, st ^ 1, 0, 0, Q1);
-    if (kt + 2 < nk) load_b(st);
-    if constexpr (!PP) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    before();
-    multiply(a1, b1, 1, 1);
-    after();
-    if (kt + 1 < nk) read_a(a0, st ^ 1, 0, Q1, HA);
-    if (kt + 2 < nk) load_a(st);
-    before();
-    multiply(a1, b0, 1, 0);
-    after();
-  }
-  if constexpr (PP) {
+    // The quarters of the wave's results, in an order that needs one new half
+    // operand each; the reads are spread so that each run of matrix
+    // instructions covers the same number of them.  Loads of tile t + 1 end
+    // before its first read (the wait before the second quarter, and a barrier
+    // after it); the stage of tile t is loaded again only after every wave's
+    // last read of it: B from the third quarter on, A from the fourth.
+    for (int kt = 0; kt < nk; ++kt) {
+      const int st = kt & 1;
+      read_b(b0, st, 0);
+      read_a(a1, st, 1, 0, Q1);
+      multiply(a0, b0, 0, 0);
+      read_b(b1, st, 1);
+      read_a(a1, st, 1, Q1, Q2);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      multiply(a0, b1, 0, 1);
+      read_a(a1, st, 1, Q2, HA);
+      if (kt + 1 < nk) read_a(a0, st ^ 1, 0, 0, Q1);
+      if (kt + 2 < nk) load_b(st);
+      multiply(a1, b1, 1, 1);
+      if (kt + 1 < nk) read_a(a0, st ^ 1, 0, Q1, HA);
+      if (kt + 2 < nk) load_a(st);
+      multiply(a1, b0, 1, 0);
+    }
     if (wave < NW / 2) asm volatile("s_barrier" ::: "memory");
+  } else {
+    constexpr int NI = OA::NI + OB::NI;   // loads of a tile, in flight together
+    struct Half {
+      f32x4_t a[FA], b[FB];
+    } h0, h1;
+    auto read = [&](Half& h, int stage, int s) {
+      const lds_char* p = lds + stage * STAGE;
+#pragma unroll
+      for (int i = 0; i < FA; ++i) h.a[i] = ra.template read_half<OA::KROW>(p, i, s);
+#pragma unroll
+      for (int i = 0; i < FB; ++i) h.b[i] = rb.template read_half<OB::KROW>(p + OA::BYTES, i, s);
+    };
+    auto multiply = [&](const Half& h) {
+#pragma unroll
+      for (int i = 0; i < FA; ++i)
+#pragma unroll
+        for (int j = 0; j < FB; ++j) acc[i][j] = mfma_half<ES>(h.b[j], h.a[i], acc[i][j]);
+    };
+#pragma unroll
+    for (int j = 0; j < S - 1; ++j)
+      if (j < nk) {
+        load_a(j);
+        load_b(j);
+      }
+    if (nk >= S - 1) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"((S - 2) * NI) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    read(h0, 0, 0);
+    // In the middle of tile t every wave waits for its loads of tile t + 1
+    // (those of the S - 3 tiles behind may be on their way) and for its own
+    // reads; after the barrier tile t + 1 is whole and the stage of tile t - 1
+    // is free.
+    int st = 0, fill = S - 1;
+    for (int kt = 0; kt < nk; ++kt) {
+      read(h1, st, 1);
+      multiply(h0);
+      if (kt + 1 < nk) {
+        if (kt + S - 2 < nk)
+          asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"((S - 3) * NI) : "memory");
+        else
+          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (kt + S - 1 < nk) {
+          load_a(fill);
+          load_b(fill);
+        }
+        fill = fill == S - 1 ? 0 : fill + 1;
+        st = st == S - 1 ? 0 : st + 1;
+        read(h0, st, 0);
+      }
+      multiply(h1);
+    }
+    asm volatile("s_barrier" ::: "memory");   // every wave's reads have ended
   }
 
   // The results go through LDS, so that the epilogue runs along whole rows of
@@ -570,22 +645,26 @@ __global__ __launch_bounds__(WM * WN * 64, PP ? 2 : 2) void k_gemm(GemmArgs g) {
   // length is a power of two (8192 x 16384 results: 229 us at K = 64 that way).
   // Pieces of 16 bytes are exchanged within a row by the row's number: a
   // lane holds 4 columns of row lane % 16 of each 16 x 16 block.
-  constexpr int NP = PR_PASSES<BM, BN, STAGE>;
+  constexpr int NP = PR_PASSES<BM, BN, S * STAGE>;
   constexpr int WR = FA / NP * 16, PR = WM * WR;   // rows of a wave and of a pass
   constexpr int QPR = BNC / 4, RPI = 64 / QPR;     // quads of a row; rows at a time
   const int li = lane & 15, lg = lane >> 4;
   const int q = lane % QPR, n = n0 + q * 4, left = g.N - n;
   const bool split_k = g.splits > 1;
+  const int64_t width = EP == EP_GATED ? 2 * (int64_t)g.N : g.N;
+  typedef __attribute__((address_space(3))) f32x4_t lds_f4;
+  // The loads of a run of rows (the residual's) end before its stores begin,
+  // and the bias is in before all of them: memory operations are counted in
+  // order, so a load that is waited for behind stores waits for them too.
   f32x4_t bz = {}, bu = {};
   if (EP != EP_STORE && !split_k && left > 0) {
     bz = bias_quad(g.fwd, n, left);
     if constexpr (EP == EP_GATED) bu = bias_quad(g.fwd, g.N + n, left);
   }
-  const int64_t width = EP == EP_GATED ? 2 * (int64_t)g.N : g.N;
-  typedef __attribute__((address_space(3))) f32x4_t lds_f4;
+  asm volatile("" : "+v"(bz), "+v"(bu));
+  constexpr int STEPS = PR / NW / RPI, RUN = STEPS < 4 ? STEPS : 4;
 #pragma unroll
   for (int p = 0; p < NP; ++p) {
-    // (the stores of the pass before need not have ended)
     if (p) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
     for (int a = 0; a < FA / NP; ++a)
@@ -596,33 +675,52 @@ __global__ __launch_bounds__(WM * WN * 64, PP ? 2 : 2) void k_gemm(GemmArgs g) {
         *(lds_f4*)(lds + (wm * WR + a * 16 + li) * BN * 4 + ((c ^ li) << 4)) = acc[p * (FA / NP) + a][b];
       }
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-#pragma unroll 4
-    for (int r = 0; r < PR / NW / RPI; ++r) {
-      const int row = wave * (PR / NW) + r * RPI + lane / QPR;
-      const int64_t m = m0 + row / WR * (FA * 16) + p * WR + row % WR;
-      if (m >= g.M || left <= 0) continue;
-      f32x4_t z = *(const lds_f4*)(lds + row * BN * 4 + ((q ^ (row & 15)) << 4)), u = {};
-      if constexpr (EP == EP_GATED) u = *(const lds_f4*)(lds + row * BN * 4 + (((QPR + q) ^ (row & 15)) << 4));
-      if (split_k) {
-        float* const dst = g.part + ((int64_t)split * g.M + m) * width + n;
-        st_quad(dst, z, left);
-        if constexpr (EP == EP_GATED) st_quad(dst + g.N, u, left);
-      } else if constexpr (EP == EP_STORE) {
-        store_result<T>(g, m, n, z, left);
-      } else {
-        fwd_epilogue<T, EP == EP_GATED>(g.fwd, m, n, z + bz, u + bu);
+    for (int r0 = 0; r0 < STEPS; r0 += RUN) {
+      f32x4_t res[RUN] = {};
+      if (EP != EP_STORE && !split_k && g.fwd.R && left > 0) {
+#pragma unroll
+        for (int r = 0; r < RUN; ++r) {
+          const int row = wave * (PR / NW) + (r0 + r) * RPI + lane / QPR;
+          const int64_t m = m0 + row / WR * (FA * 16) + p * WR + row % WR;
+          if (m < g.M) res[r] = residual_quad<T>(g.fwd, m, n, left);
+        }
+#pragma unroll
+        for (int r = 0; r < RUN; ++r) asm volatile("" : "+v"(res[r]));
+      }
+#pragma unroll
+      for (int r = 0; r < RUN; ++r) {
+        const int row = wave * (PR / NW) + (r0 + r) * RPI + lane / QPR;
+        const int64_t m = m0 + row / WR * (FA * 16) + p * WR + row % WR;
+        if (m >= g.M || left <= 0) continue;
+        f32x4_t z = *(const lds_f4*)(lds + row * BN * 4 + ((q ^ (row & 15)) << 4)), u = {};
+        if constexpr (EP == EP_GATED) u = *(const lds_f4*)(lds + row * BN * 4 + (((QPR + q) ^ (row & 15)) << 4));
+        if (split_k) {
+          float* const dst = g.part + ((int64_t)split * g.M + m) * width + n;
+          st_quad(dst, z, left);
+          if constexpr (EP == EP_GATED) st_quad(dst + g.N, u, left);
+        } else if constexpr (EP == EP_STORE) {
+          store_result<T>(g, m, n, z, left);
+        } else {
+          fwd_epilogue<T, EP == EP_GATED>(g.fwd, m, n, z + bz, u + bu, res[r]);
+        }
       }
     }
   }
 }
 
+template <class T, class F, int EP>
+__global__ __launch_bounds__(F::NW * 64, 2) void k_gemm(GemmArgs g) {
+  __shared__ __attribute__((aligned(1024))) char sm[F::LDS];
+  gemm_block<T, F, false, false, EP>(g, blockIdx.x, (lds_char*)sm);
+}
+
 // Sum of the partial products of a split K, in split order, and the epilogue.
 template <class T, int EP>
-__global__ __launch_bounds__(256) void k_gemm_join(GemmArgs g) {
+__device__ __forceinline__ void join_block(const GemmArgs& g, int block, int blocks) {
   const int quads = (g.N + 3) / 4;
   const int width = EP == EP_GATED ? 2 * g.N : g.N;
   const int64_t total = (int64_t)g.M * quads, stride = (int64_t)g.M * width;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+  for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < total; i += (int64_t)blocks * 256) {
     const int64_t m = i / quads;
     const int n = (int)(i - m * quads) * 4, left = g.N - n;
     const float* p = g.part + m * width + n;
@@ -636,9 +734,14 @@ __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs g) {
     } else {
       z += bias_quad(g.fwd, n, left);
       if constexpr (EP == EP_GATED) u += bias_quad(g.fwd, g.N + n, left);
-      fwd_epilogue<T, EP == EP_GATED>(g.fwd, m, n, z, u);
+      fwd_epilogue<T, EP == EP_GATED>(g.fwd, m, n, z, u, residual_quad<T>(g.fwd, m, n, left));
     }
   }
+}
+
+template <class T, int EP>
+__global__ __launch_bounds__(256) void k_gemm_join(GemmArgs g) {
+  join_block<T, EP>(g, blockIdx.x, gridDim.x);
 }
 
 }  // namespace occ

@@ -39,6 +39,110 @@ __device__ __forceinline__ f32x4_t ld_piece(const T* p, int left) {
   return r;
 }
 
+// One column of one token.
+template <class T, bool GATED>
+__device__ __forceinline__ void fwd_epilogue_one(const FwdEpi& e, int64_t m, int n, float z, float u) {
+  if (e.bias) {
+    z += e.bias[n];
+    if constexpr (GATED) u += e.bias[e.out + n];
+  }
+  if (e.Z) {
+    st_elem((T*)e.Z + m * e.ldz + n, z);
+    if constexpr (GATED) st_elem((T*)e.Z + m * e.ldz + e.out + n, u);
+  }
+  float y = act_quad(e.act, f32x4_t{z, z, z, z})[0];
+  if constexpr (GATED) y *= u;
+  if (e.R) y += ld_elem<T>((const T*)e.R + m * e.ldr + n);
+  st_elem((T*)e.Y + m * e.ldy + n, y);
+}
+
+// Sum over the wave, in every lane.
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+  for (int s = 32; s; s >>= 1) x += __shfl_xor(x, s);
+  return x;
+}
+
+// Up to NT tokens, NT <= 4: a wave takes two rows of W (gated: a gate's row
+// and the other projection's) along K, 1024 bytes of a row an instruction, so
+// that the stream runs through the memory channels in order; sums stay in the
+// lanes until the end.
+constexpr int DOT_WAVES = 4;
+
+template <class T, int NT, bool GATED>
+__global__ __launch_bounds__(DOT_WAVES * 64) void k_dot(SkinnyArgs g) {
+  constexpr int CH = 16 / sizeof(T), BK = 64 * CH;
+  const int lane = threadIdx.x & 63;
+  const int id = blockIdx.x * DOT_WAVES + wave_id();
+  const int n0 = GATED ? id : 2 * id;
+  if (n0 >= g.fwd.out) return;
+  const bool both = GATED || n0 + 1 < g.fwd.out;
+  const T* const w0 = (const T*)g.W + (int64_t)n0 * g.ldw;
+  const T* const w1 = GATED ? w0 + (int64_t)g.fwd.out * g.ldw : both ? w0 + g.ldw : w0;
+  float z[2][NT] = {};
+  auto load = [&](const T* p, int64_t k) { return ld_piece<T>(p + k, (int)min((int64_t)CH, g.in - k)); };
+  auto widen = [&](f32x4_t v, float* e) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) e[i] = v[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        e[2 * i] = bf16_lo(__float_as_uint(v[i]));
+        e[2 * i + 1] = bf16_hi(__float_as_uint(v[i]));
+      }
+    }
+  };
+  constexpr int U = NT <= 2 ? 4 : 2;
+  auto add = [&](f32x4_t a, f32x4_t b, const f32x4_t* x) {
+    float ea[CH], eb[CH], ex[CH];
+    widen(a, ea);
+    widen(b, eb);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      widen(x[t], ex);
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        z[0][t] = __builtin_fmaf(ea[i], ex[i], z[0][t]);
+        z[1][t] = __builtin_fmaf(eb[i], ex[i], z[1][t]);
+      }
+    }
+  };
+  const T* x[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) x[t] = (const T*)g.X + (int64_t)min(t, g.tokens - 1) * g.ldx;
+  int64_t k = lane * CH;
+  for (; k + (U - 1) * BK + CH <= g.in; k += U * BK) {
+    f32x4_t a[U], b[U], xv[U][NT];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      a[u] = ld_piece<T>(w0 + k + u * BK, CH);
+      b[u] = ld_piece<T>(w1 + k + u * BK, CH);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) xv[u][t] = ld_piece<T>(x[t] + k + u * BK, CH);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) add(a[u], b[u], xv[u]);
+  }
+  for (; k < g.in; k += BK) {
+    f32x4_t xv[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) xv[t] = load(x[t], k);
+    add(load(w0, k), load(w1, k), xv);
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const float s0 = wave_sum(z[0][t]), s1 = wave_sum(z[1][t]);
+    if (t >= g.tokens) continue;
+    if constexpr (GATED) {
+      if (lane == t) fwd_epilogue_one<T, true>(g.fwd, t, n0, s0, s1);
+    } else {
+      const int c = lane - 2 * t;
+      if (c == 0 || (c == 1 && both)) fwd_epilogue_one<T, false>(g.fwd, t, n0 + c, c ? s1 : s0, 0.0f);
+    }
+  }
+}
+
 // A block makes 16 columns of Y (gated: the 16 rows of both projections) for
 // up to 16 NT tokens: its SK_WAVES waves take K in turns of one tile of 128
 // bytes a row, with weights and tokens loaded straight into the registers of
@@ -131,18 +235,18 @@ __global__ __launch_bounds__(SK_WAVES * 64) void k_skinny(SkinnyArgs g) {
     if (m < g.tokens && left > 0) {
       z += bias_quad(g.fwd, n, left);
       if constexpr (GATED) u += bias_quad(g.fwd, g.fwd.out + n, left);
-      fwd_epilogue<T, GATED>(g.fwd, m, n, z, u);
+      fwd_epilogue<T, GATED>(g.fwd, m, n, z, u, residual_quad<T>(g.fwd, m, n, left));
     }
   }
 }
 
 // ----------------------------------------------------------------------------
-// gradient at the pre-activation, and the bias gradient
+// before the products: the gradient at the pre-activation, aligned operands
 // ----------------------------------------------------------------------------
 // dZ = dY act'(Z); gated, with Z = [G U]: dG = dY U act'(G), dU = dY act(G).
 // dZ is rounded to the layer's type, the type its products take.  Bias sums
 // are taken from the values before that rounding, in fp32 over a strip of
-// rows, and the strips are added by k_dz_bias in strip order.
+// rows; bias_block adds the strips.
 struct DzArgs {
   const void* dY;
   const void* Z;     // null: dZ = dY, and only the bias sums are made
@@ -150,16 +254,19 @@ struct DzArgs {
   float* bias_part;  // strips x width, or null
   int64_t ldy, ldz, ldd;
   int32_t tokens, out, act, strip;   // strip: rows of a block
+  int32_t across;                    // blocks along a row
 };
 
 constexpr int DZ_LANES = 32;   // threads along a row, 4 columns each
 constexpr int DZ_ROWS = 8;     // rows at a time
 
 template <class T, bool GATED>
-__global__ __launch_bounds__(256) void k_dz(DzArgs g) {
+__device__ __forceinline__ void dz_block(const DzArgs& g, int block) {
+  __shared__ f32x4_t part[GATED ? 2 : 1][DZ_ROWS][DZ_LANES];
   const int cx = threadIdx.x & (DZ_LANES - 1), ry = threadIdx.x / DZ_LANES;
-  const int n = (blockIdx.x * DZ_LANES + cx) * 4, left = g.out - n;
-  const int64_t r0 = (int64_t)blockIdx.y * g.strip;
+  const int by = block / g.across, bx = block - by * g.across;
+  const int n = (bx * DZ_LANES + cx) * 4, left = g.out - n;
+  const int64_t r0 = (int64_t)by * g.strip;
   const int64_t r1 = min(r0 + g.strip, (int64_t)g.tokens);
   f32x4_t s0 = {}, s1 = {};
   if (left > 0) {
@@ -169,18 +276,14 @@ __global__ __launch_bounds__(256) void k_dz(DzArgs g) {
       if (g.Z) {
         const T* const zr = (const T*)g.Z + m * g.ldz + n;
         const f32x4_t z = ld_quad<T>(zr, left);
-        f32x4_t u = {};
+        f32x4_t u = {}, a, da;
         if constexpr (GATED) u = ld_quad<T>(zr + g.out, left);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float a, da;
-          act_grad_f(g.act, z[i], a, da);
-          if constexpr (GATED) {
-            d0[i] = dy[i] * u[i] * da;
-            d1[i] = dy[i] * a;
-          } else {
-            d0[i] = dy[i] * da;
-          }
+        act_grad_quad(g.act, z, a, da);
+        if constexpr (GATED) {
+          d0 = dy * u * da;
+          d1 = dy * a;
+        } else {
+          d0 = dy * da;
         }
       }
       if (g.dZ) {
@@ -196,7 +299,6 @@ __global__ __launch_bounds__(256) void k_dz(DzArgs g) {
     }
   }
   if (!g.bias_part) return;
-  __shared__ f32x4_t part[GATED ? 2 : 1][DZ_ROWS][DZ_LANES];
   part[0][ry][cx] = s0;
   if constexpr (GATED) part[1][ry][cx] = s1;
   __syncthreads();
@@ -205,31 +307,118 @@ __global__ __launch_bounds__(256) void k_dz(DzArgs g) {
 #pragma unroll
     for (int r = 0; r < DZ_ROWS; ++r) s += part[ry][r][cx];
     const int64_t width = GATED ? 2 * (int64_t)g.out : g.out;
-    st_quad(g.bias_part + blockIdx.y * width + ry * (int64_t)g.out + n, s, left);
+    st_quad(g.bias_part + by * width + ry * (int64_t)g.out + n, s, left);
   }
-}
-
-__global__ __launch_bounds__(256) void k_dz_bias(const float* part, int strips, int64_t width, float* dbias,
-                                                 int accumulate) {
-  const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (n >= width) return;
-  float s = accumulate ? dbias[n] : 0.0f;
-  for (int i = 0; i < strips; ++i) s += part[i * width + n];
-  dbias[n] = s;
 }
 
 // Copy of an operand with rows on 16 bytes, whole pieces and zeros behind
 // their ends.
+struct CopyArgs {
+  const void* src;
+  void* dst;
+  int64_t ld, rows;
+  int32_t cols, pieces, blocks;
+};
+
 template <class T>
-__global__ __launch_bounds__(256) void k_align_rows(const T* src, int64_t lds, T* dst, int64_t rows, int cols,
-                                                    int pieces) {
+__device__ __forceinline__ void copy_block(const CopyArgs& g, int block) {
   constexpr int CH = 16 / sizeof(T);
-  const int64_t total = rows * pieces;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / pieces;
-    const int c = (int)(i - r * pieces) * CH;
-    *(f32x4_t*)(dst + i * CH) = ld_piece<T>(src + r * lds + c, cols - c);
+  const int64_t total = g.rows * g.pieces;
+  for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < total; i += (int64_t)g.blocks * 256) {
+    const int64_t r = i / g.pieces;
+    const int c = (int)(i - r * g.pieces) * CH;
+    *(f32x4_t*)((T*)g.dst + i * CH) = ld_piece<T>((const T*)g.src + r * g.ld + c, g.cols - c);
   }
+}
+
+// All of it in one launch: dz_blocks blocks make dZ, the rest copy.
+struct PrepArgs {
+  DzArgs dz;
+  CopyArgs copy[3];   // of dY, W and X
+  int32_t dz_blocks;
+};
+
+template <class T, bool GATED>
+__global__ __launch_bounds__(256) void k_prep(PrepArgs g) {
+  int b = blockIdx.x;
+  if (b < g.dz_blocks) return dz_block<T, GATED>(g.dz, b);
+  b -= g.dz_blocks;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    if (b < g.copy[i].blocks) return copy_block<T>(g.copy[i], b);
+    b -= g.copy[i].blocks;
+  }
+}
+
+// ----------------------------------------------------------------------------
+// the products of the backward pass
+// ----------------------------------------------------------------------------
+struct BiasArgs {
+  const float* part;   // strips x width
+  float* dbias;
+  int64_t width;
+  int32_t strips, accumulate;
+};
+
+// 64 columns a block of 512 threads: 8 threads a column add every 8th strip,
+// and their sums are added in order.
+__device__ __forceinline__ void bias_block(const BiasArgs& g, int block, float* lds) {
+  constexpr int G = 8;
+  const int c = threadIdx.x & 63, r = threadIdx.x >> 6;
+  const int64_t n = (int64_t)block * 64 + c;
+  float s = 0.0f;
+  if (n < g.width) {
+    const float* p = g.part + n;
+    int i = r;
+    for (; i + 3 * G < g.strips; i += 4 * G) {
+      float v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] = p[(i + u * G) * g.width];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) s += v[u];
+    }
+    for (; i < g.strips; i += G) s += p[i * g.width];
+  }
+  lds[threadIdx.x] = s;
+  __syncthreads();
+  if (r || n >= g.width) return;
+#pragma unroll
+  for (int u = 1; u < G; ++u) s += lds[u * 64 + c];
+  g.dbias[n] = g.accumulate ? g.dbias[n] + s : s;
+}
+
+// The bias gradient, dX = dZ W and dW = dZ^T X in one launch: where one of the
+// products alone leaves CUs idle, or ends in a part of a round, the other's
+// blocks fill them.
+struct BackwardArgs {
+  GemmArgs dx, dw;
+  BiasArgs bias;
+  int32_t dx_blocks, dw_blocks;
+};
+
+template <class T, class F>
+__global__ __launch_bounds__(F::NW * 64, 2) void k_backward(BackwardArgs g) {
+  __shared__ __attribute__((aligned(1024))) char sm[F::LDS];
+  int b = blockIdx.x;
+  if (b < g.dx_blocks) return gemm_block<T, F, false, true, EP_STORE>(g.dx, b, (lds_char*)sm);
+  b -= g.dx_blocks;
+  if (b < g.dw_blocks) return gemm_block<T, F, true, true, EP_STORE>(g.dw, b, (lds_char*)sm);
+  static_assert(F::NW == 8, "bias_block runs on eight waves");
+  bias_block(g.bias, b - g.dw_blocks, (float*)sm);
+}
+
+// Joins the parts of both products.
+template <class T>
+__global__ __launch_bounds__(256) void k_backward_join(GemmArgs dx, GemmArgs dw, int dx_blocks) {
+  const int b = blockIdx.x;
+  if (b < dx_blocks) return join_block<T, EP_STORE>(dx, b, dx_blocks);
+  join_block<T, EP_STORE>(dw, b - dx_blocks, gridDim.x - dx_blocks);
+}
+
+// dbias alone
+__global__ __launch_bounds__(512) void k_bias(BiasArgs g) {
+  __shared__ float sm[512];
+  bias_block(g, blockIdx.x, sm);
 }
 
 // Zeros where no token contributes to a gradient.

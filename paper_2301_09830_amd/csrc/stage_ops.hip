@@ -55,82 +55,141 @@ bool ld_ok(int64_t cols, int64_t ld) { return ld >= cols && ld < kMaxDim; }
 // ----------------------------------------------------------------------------
 // plan of one tiled product
 // ----------------------------------------------------------------------------
-// Two tiles.  256 x 256 on eight waves (one block a CU) moves the fewest
-// bytes through LDS per product; 128 x 128 on four waves (two blocks a CU)
-// leaves fewer CUs idle when the result is small.  K is split, and the parts
-// joined by a second kernel, where even the small tiles do not fill the chip.
-// The cost of a choice is the rounds of blocks it takes times their length in
-// clocks of one CU.
-struct ProductPlan {
-  bool big = false;
-  int bm = 0, bn = 0;
+// Three tiles: 256 x 256 moves the fewest bytes per product, 128 x 128 and
+// 64 x 64 leave fewer CUs idle when the result is small.  K is split, and the
+// parts joined by a second kernel, where even the small tiles do not fill the
+// chip.  The choice is the one of least estimated time: a block's length is
+// its K tiles times the measured time of one, plus a fixed part (launch, first
+// loads, results); blocks go to the CUs in rounds.
+enum Tile { TILE_256, TILE_128, TILE_64, TILE_NUM };
+
+struct TileTimes {
+  int side, resident;              // resident: blocks a CU
+  double k_bf16, k_f32, fixed;     // us; K tiles of all resident blocks
+};
+// bf16: 8192 x 8192 x K, slope and intercept; 128 and 64: one round at K = 4096.
+// fp32 is bound by the matrix unit (256 x 256 x 32 in 16384 clocks) in each.
+constexpr TileTimes kTiles[TILE_NUM] = {{256, 1, 1.38, 7.9, 11.0}, {128, 1, 0.57, 2.0, 4.0}, {64, 2, 0.42, 1.0, 3.0}};
+constexpr double kJoinUs = 4.0, kJoinBytesPerUs = 10e6;
+constexpr int kCUs = 256;
+constexpr int kSplits = 8;
+constexpr int kSplitCounts[kSplits] = {1, 2, 3, 4, 6, 8, 12, 16};
+constexpr double kMaxPartBytes = 512e6;
+
+// One product of m x width results over k: its blocks with a tile and a split.
+struct Product {
   int64_t tiles_m = 0, tiles_n = 0, tiles_k = 0;
   int splits = 1, k_per_split = 1;
+  double block_us = 0.0, join_us = 0.0;
   size_t part_bytes = 0;
+  int64_t blocks() const { return tiles_m * tiles_n * splits; }
 };
 
-constexpr int kCUs = 256;
+// pair: columns come in pairs of rows of W (gated), so a tile makes half as many
+Product make_product(int64_t m, int64_t width, int64_t k, size_t es, Tile tile, int splits, bool pair) {
+  Product p;
+  const TileTimes& t = kTiles[tile];
+  p.tiles_m = div_up(m, t.side);
+  p.tiles_n = pair ? div_up(width / 2, t.side / 2) : div_up(width, t.side);
+  p.tiles_k = div_up(k, kRowBytes / (int64_t)es);
+  p.k_per_split = (int)div_up(p.tiles_k, splits);
+  p.splits = (int)div_up(p.tiles_k, p.k_per_split);
+  p.block_us = (double)p.k_per_split * (es == 2 ? t.k_bf16 : t.k_f32) + t.fixed;
+  if (p.splits > 1) {
+    const double part = (double)p.splits * (double)m * (double)width * 4.0;
+    p.part_bytes = (size_t)part;
+    p.join_us = kJoinUs + part / kJoinBytesPerUs;
+  }
+  return p;
+}
 
-ProductPlan plan_product(int64_t m, int64_t width, int64_t k, size_t es) {
+bool product_fits(const Product& p) {
+  return p.tiles_m * p.tiles_n < ((int64_t)1 << 26) && p.tiles_k < ((int64_t)1 << 24) &&
+         (double)p.part_bytes <= kMaxPartBytes;
+}
+
+struct ProductPlan {
+  Tile tile = TILE_256;
+  Product x, w;   // of the backward pass; the forward pass has x alone
+  bool fits = false;
+};
+
+// Time of a launch on `slots` resident blocks: the blocks of x, then those of
+// w, each to the first free slot.
+double launch_us(const Product& x, const Product& w, int64_t slots) {
+  const int64_t nx = x.blocks(), nw = w.blocks();
+  const int64_t rest = nx % slots, free = slots - rest;
+  const double full = (double)(nx / slots) * x.block_us;   // whole rounds of x
+  if (!rest) return full + (double)div_up(nw, slots) * w.block_us;
+  if (!nw) return full + x.block_us;
+  const int64_t beside = (int64_t)(x.block_us / w.block_us);   // rounds of w beside the last blocks of x
+  const int64_t left = nw - beside * free;
+  if (left <= 0) return full + std::max(x.block_us, (double)div_up(nw, free) * w.block_us);
+  if (left <= free) return full + std::max(x.block_us, (double)(beside + 1) * w.block_us);
+  return full + x.block_us + (double)div_up(left - free, slots) * w.block_us;
+}
+
+// Up to two products of one launch, with the same tile.  m, width, k: of each
+// (m = 0: not there).
+ProductPlan plan_products(const int64_t (&m)[2], const int64_t (&width)[2], const int64_t (&k)[2], size_t es,
+                          bool pair) {
   ProductPlan best;
-  double best_cost = INFINITY;
-  const int64_t tk = div_up(k, kRowBytes / (int64_t)es);
-  for (int big = 0; big < 2; ++big) {
-    const int side = big ? 256 : 128;
-    const int64_t tm = div_up(m, side), tn = div_up(width, side);
-    const int64_t slots = big ? kCUs : 2 * kCUs;
-    const double per_k = (es == 2 ? (big ? 2600.0 : 1700.0) : (big ? 17000.0 : 8600.0));
-    for (int s = 1; s <= 16; s *= 2) {
-      if (s > 1 && tk < 4 * s) break;
-      const int64_t kps = div_up(tk, s), sp = div_up(tk, kps);
-      const double rounds = (double)div_up(tm * tn * sp, slots);
-      double cost = rounds * ((double)kps * per_k + 8000.0);
-      const double part = (double)sp * (double)m * (double)width * 4.0;
-      if (sp > 1) {
-        if (part > 512e6) break;
-        cost += 2.0 * part / 2000.0 + 8000.0;   // bytes a clock of the whole chip; a launch
+  double best_us = INFINITY;
+  for (int t = 0; t < TILE_NUM; ++t) {
+    const double slots = (double)kCUs * kTiles[t].resident;
+    Product of[2][kSplits];
+    int n[2] = {0, 0};
+    for (int i = 0; i < 2; ++i) {
+      if (!m[i]) {
+        of[i][n[i]++] = Product{};
+        continue;
       }
-      if (cost < best_cost) {
-        best_cost = cost;
-        best.big = big != 0;
-        best.bm = best.bn = side;
-        best.tiles_m = tm;
-        best.tiles_n = tn;
-        best.tiles_k = tk;
-        best.splits = (int)sp;
-        best.k_per_split = (int)kps;
-        best.part_bytes = sp > 1 ? (size_t)part : 0;
+      for (const int s : kSplitCounts) {
+        const Product p = make_product(m[i], width[i], k[i], es, (Tile)t, s, pair);
+        if (p.splits != s || (s > 1 && p.k_per_split < 4) || !product_fits(p)) break;
+        of[i][n[i]++] = p;
+        if ((double)p.blocks() > 2.0 * slots) break;   // parts of K would only add work
+      }
+    }
+    for (int x = 0; x < n[0]; ++x) {
+      for (int w = 0; w < n[1]; ++w) {
+        const Product &px = of[0][x], &pw = of[1][w];
+        const double us = std::max(px.join_us, pw.join_us) + launch_us(px, pw, kCUs * kTiles[t].resident);
+        if (us < best_us) {
+          best_us = us;
+          best.tile = (Tile)t;
+          best.x = px;
+          best.w = pw;
+          best.fits = true;
+        }
       }
     }
   }
   return best;
 }
 
-bool grid_fits(const ProductPlan& p) {
-  return p.tiles_m * p.tiles_n < ((int64_t)1 << 26) && p.tiles_k < ((int64_t)1 << 24);
-}
-
-template <class T, bool AKS, bool BKS, int EP>
-occ_status_t run_product(const char* name, const ProductPlan& p, GemmArgs g, char* ws, size_t part_off, hipStream_t s) {
+void set_tiles(GemmArgs& g, const Product& p, char* part) {
   g.tiles_m = (int32_t)p.tiles_m;
   g.tiles_n = (int32_t)p.tiles_n;
   g.tiles_k = (int32_t)p.tiles_k;
   g.splits = p.splits;
   g.k_per_split = p.k_per_split;
-  g.part = p.splits > 1 ? (float*)(ws + part_off) : nullptr;
-  const unsigned grid = (unsigned)(p.tiles_m * p.tiles_n * p.splits);
-  OCC_TRY(launch(name, s, [&] {
-    if (p.big)
-      hipLaunchKernelGGL((k_gemm<T, 2, 4, 8, 4, AKS, BKS, EP, true>), dim3(grid), dim3(512), 0, s, g);
-    else
-      hipLaunchKernelGGL((k_gemm<T, 2, 2, 4, 4, AKS, BKS, EP, false>), dim3(grid), dim3(256), 0, s, g);
-  }));
-  if (p.splits == 1) return OCC_OK;
-  const int64_t quads = (int64_t)g.M * div_up(g.N, 4);
-  return launch("gemm_join", s, [&] {
-    hipLaunchKernelGGL((k_gemm_join<T, EP>), dim3((unsigned)std::min<int64_t>(div_up(quads, 256), 4096)), dim3(256), 0,
-                       s, g);
-  });
+  g.part = p.splits > 1 ? (float*)part : nullptr;
+}
+
+// Results bypass the caches when the call's operands and results pass
+// kStreamBytes, most of what the memory-side cache holds: they would not
+// survive there until they are used, but push out operands that other tiles
+// still need (8192 x 4096 x 16384 bf16, 470 MB: 861 us with ordinary stores, 807
+// with these).  Rows have to start on 64 bytes.
+constexpr double kStreamBytes = 192e6;
+
+bool rows_on_lines(const void* p, int64_t ld, int64_t cols, size_t es) {
+  return !p || (aligned(p, 64) && (size_t)ld * es % 64 == 0 && (size_t)cols * es % 64 == 0);
+}
+
+unsigned join_blocks(const GemmArgs& g) {
+  return (unsigned)std::min<int64_t>(div_up((int64_t)g.M * div_up(g.N, 4), 256), 4096);
 }
 
 // An operand the tiled product cannot take in place: rows off 16 bytes, rows
@@ -142,19 +201,35 @@ bool needs_copy(const void* p, int64_t ld, int64_t cols, size_t es) {
 int64_t piece_ld(int64_t cols, size_t es) { return up(cols, 16 / (int64_t)es); }
 
 template <class T>
-occ_status_t copy_operand(const void* src, int64_t ld, int64_t rows, int64_t cols, char* dst, hipStream_t s) {
-  const int64_t pieces = piece_ld(cols, sizeof(T)) * (int64_t)sizeof(T) / 16;
-  const int64_t blocks = std::min<int64_t>(div_up(rows * pieces, 256), 8192);
-  return launch("align_rows", s, [&] {
-    hipLaunchKernelGGL((k_align_rows<T>), dim3((unsigned)blocks), dim3(256), 0, s, (const T*)src, ld, (T*)dst, rows,
-                       (int)cols, (int)pieces);
+CopyArgs copy_operand(const void* src, int64_t ld, int64_t rows, int64_t cols, char* dst) {
+  CopyArgs c{};
+  c.src = src;
+  c.dst = dst;
+  c.ld = ld;
+  c.rows = rows;
+  c.cols = (int32_t)cols;
+  c.pieces = (int32_t)(piece_ld(cols, sizeof(T)) * (int64_t)sizeof(T) / 16);
+  c.blocks = (int32_t)std::min<int64_t>(div_up(rows * c.pieces, 256), 8192);
+  return c;
+}
+
+template <class T, bool GATED>
+occ_status_t run_prep(const PrepArgs& p, hipStream_t s) {
+  const int blocks = p.dz_blocks + p.copy[0].blocks + p.copy[1].blocks + p.copy[2].blocks;
+  if (!blocks) return OCC_OK;
+  return launch("layer_prep", s, [&] {
+    hipLaunchKernelGGL((k_prep<T, GATED>), dim3((unsigned)blocks), dim3(256), 0, s, p);
   });
 }
 
 // ----------------------------------------------------------------------------
 // forward
 // ----------------------------------------------------------------------------
-// Up to this many tokens the weights are streamed through registers.
+// Up to kFewTokens the weights are streamed through registers: row by row
+// along K up to kDotTokens (one token, 8192 x 8192 bf16: 23.6 us; through the
+// matrix instructions 31.6), by matrix instructions above (8 tokens, 4096 x
+// 16384: 31.4 us; row by row 36.7).
+constexpr int64_t kDotTokens = 4;
 constexpr int64_t kFewTokens = 64;
 
 struct FwdPlan {
@@ -183,14 +258,13 @@ occ_status_t plan_fwd(const occ_linear_t& l, bool gated, FwdPlan& f) {
   const int64_t wide = gated ? 2 * l.out : l.out;
   f.copy_x = needs_copy(l.X, l.ldx, l.in, es);
   f.copy_w = needs_copy(l.W, l.ldw, l.in, es);
-  f.prod = plan_product(l.tokens, wide, l.in, es);
-  if (gated) f.prod.tiles_n = div_up(l.out, f.prod.bn / 2);
-  if (!grid_fits(f.prod)) return OCC_E_SHAPE;
+  f.prod = plan_products({l.tokens, 0}, {wide, 0}, {l.in, 0}, es, gated);
+  if (!f.prod.fits) return OCC_E_SHAPE;
   Carve c;
   const size_t row = (size_t)piece_ld(l.in, es) * es;
   if (f.copy_x) f.x_off = c.take((size_t)l.tokens * row);
   if (f.copy_w) f.w_off = c.take((size_t)wide * row);
-  if (f.prod.splits > 1) f.part_off = c.take(f.prod.part_bytes);
+  if (f.prod.x.splits > 1) f.part_off = c.take(f.prod.x.part_bytes);
   f.bytes = c.total();
   return OCC_OK;
 }
@@ -207,6 +281,11 @@ occ_status_t run_fwd(const occ_linear_t& l, const FwdPlan& f, char* ws, hipStrea
   e.bias = l.bias;
   e.act = l.act;
   e.out = (int32_t)l.out;
+  const int64_t wide = GATED ? 2 * l.out : l.out;
+  const double bytes = (double)sizeof(T) * ((double)l.tokens * (double)(l.in + l.out + (l.Z ? wide : 0)) +
+                                            (double)wide * (double)l.in);
+  e.stream = bytes > kStreamBytes && rows_on_lines(l.Y, l.ldy, l.out, sizeof(T)) &&
+             rows_on_lines(l.Z, l.ldz, l.out, sizeof(T));
   if (f.few) {
     SkinnyArgs g{};
     g.X = l.X;
@@ -217,6 +296,14 @@ occ_status_t run_fwd(const occ_linear_t& l, const FwdPlan& f, char* ws, hipStrea
     g.in = (int32_t)l.in;
     g.fwd = e;
     const dim3 grid((unsigned)div_up(l.out, 16)), block(SK_WAVES * 64);
+    if (l.tokens <= kDotTokens) {
+      const dim3 rows((unsigned)div_up(GATED ? l.out : div_up(l.out, 2), DOT_WAVES)), waves(DOT_WAVES * 64);
+      return launch(GATED ? "gated_few" : "linear_few", s, [&] {
+        if (l.tokens == 1) hipLaunchKernelGGL((k_dot<T, 1, GATED>), rows, waves, 0, s, g);
+        else if (l.tokens == 2) hipLaunchKernelGGL((k_dot<T, 2, GATED>), rows, waves, 0, s, g);
+        else hipLaunchKernelGGL((k_dot<T, 4, GATED>), rows, waves, 0, s, g);
+      });
+    }
     return launch(GATED ? "gated_few" : "linear_few", s, [&] {
       if (l.tokens <= 16) hipLaunchKernelGGL((k_skinny<T, 1, GATED>), grid, block, 0, s, g);
       else if (l.tokens <= 32) hipLaunchKernelGGL((k_skinny<T, 2, GATED>), grid, block, 0, s, g);
@@ -228,23 +315,36 @@ occ_status_t run_fwd(const occ_linear_t& l, const FwdPlan& f, char* ws, hipStrea
   g.lda = l.ldx;
   g.B = l.W;
   g.ldb = l.ldw;
-  const int64_t wide = GATED ? 2 * l.out : l.out;
+  PrepArgs prep{};
   if (f.copy_x) {
-    OCC_TRY(copy_operand<T>(l.X, l.ldx, l.tokens, l.in, ws + f.x_off, s));
+    prep.copy[0] = copy_operand<T>(l.X, l.ldx, l.tokens, l.in, ws + f.x_off);
     g.A = ws + f.x_off;
     g.lda = piece_ld(l.in, sizeof(T));
   }
   if (f.copy_w) {
-    OCC_TRY(copy_operand<T>(l.W, l.ldw, wide, l.in, ws + f.w_off, s));
+    prep.copy[1] = copy_operand<T>(l.W, l.ldw, wide, l.in, ws + f.w_off);
     g.B = ws + f.w_off;
     g.ldb = piece_ld(l.in, sizeof(T));
   }
+  OCC_TRY((run_prep<T, GATED>(prep, s)));
   g.M = (int32_t)l.tokens;
   g.N = (int32_t)l.out;
   g.ka = g.kb = (int32_t)piece_ld(l.in, sizeof(T));
   g.fwd = e;
-  return run_product<T, false, false, GATED ? EP_GATED : EP_FWD>(GATED ? "gated_fwd" : "linear_fwd", f.prod, g, ws,
-                                                                 f.part_off, s);
+  set_tiles(g, f.prod.x, ws + f.part_off);
+  constexpr int EP = GATED ? EP_GATED : EP_FWD;
+  const dim3 grid((unsigned)f.prod.x.blocks()), block(512);
+  OCC_TRY(launch(GATED ? "gated_fwd" : "linear_fwd", s, [&] {
+    switch (f.prod.tile) {
+      case TILE_256: hipLaunchKernelGGL((k_gemm<T, Form256, EP>), grid, block, 0, s, g); break;
+      case TILE_128: hipLaunchKernelGGL((k_gemm<T, Form128, EP>), grid, block, 0, s, g); break;
+      default: hipLaunchKernelGGL((k_gemm<T, Form64, EP>), grid, block, 0, s, g); break;
+    }
+  }));
+  if (g.splits == 1) return OCC_OK;
+  return launch("layer_join", s, [&] {
+    hipLaunchKernelGGL((k_gemm_join<T, EP>), dim3(join_blocks(g)), dim3(256), 0, s, g);
+  });
 }
 
 occ_status_t check_ws(const void* ws, size_t ws_bytes, size_t need) {
@@ -286,9 +386,9 @@ struct BwdPlan {
   bool has_dz = false;    // dZ is made (else it is dY)
   bool copy_dy = false, copy_x = false, copy_w = false;
   int64_t strip = 0, strips = 0;
-  size_t dz_off = 0, bias_off = 0, x_off = 0, w_off = 0, part_off = 0, bytes = 0;
+  size_t dz_off = 0, bias_off = 0, x_off = 0, w_off = 0, dx_part = 0, dw_part = 0, bytes = 0;
   int64_t ldd = 0;
-  ProductPlan dx, dw;
+  ProductPlan prod;
 };
 
 occ_status_t check_bwd(const occ_linear_grad_t* l, bool gated) {
@@ -323,29 +423,29 @@ occ_status_t plan_bwd(const occ_linear_grad_t& l, bool gated, BwdPlan& f) {
     f.dz_off = c.take((size_t)l.tokens * f.ldd * es);
   }
   if (f.has_dz || l.dbias) {
-    // enough blocks to fill the chip several times, whole groups of rows in each
-    const int64_t across = div_up(l.out, DZ_LANES * 4);
-    const int64_t down = std::max<int64_t>(1, std::min<int64_t>(div_up(4096, across), div_up(l.tokens, DZ_ROWS)));
+    // enough blocks to fill the chip several times, whole groups of rows in
+    // each; fewer, longer strips where their sums have to be added
+    const int64_t across = div_up(l.out, DZ_LANES * 4), most = l.dbias ? 2048 : 8192;
+    const int64_t down = std::max<int64_t>(1, std::min<int64_t>(div_up(most, across), div_up(l.tokens, DZ_ROWS)));
     f.strip = up(div_up(l.tokens, down), DZ_ROWS);
     f.strips = div_up(l.tokens, f.strip);
+    if (across * f.strips >= ((int64_t)1 << 30)) return OCC_E_SHAPE;
     if (l.dbias) f.bias_off = c.take((size_t)f.strips * wide * 4);
   }
-  size_t part = 0;
   if (l.dX) {
     f.copy_w = needs_copy(l.W, l.ldw, l.in, es);
     if (f.copy_w) f.w_off = c.take((size_t)wide * piece_ld(l.in, es) * es);
-    f.dx = plan_product(l.tokens, l.in, wide, es);
-    if (!grid_fits(f.dx)) return OCC_E_SHAPE;
-    part = f.dx.part_bytes;
   }
   if (l.dW) {
     f.copy_x = needs_copy(l.X, l.ldx, l.in, es);
     if (f.copy_x) f.x_off = c.take((size_t)l.tokens * piece_ld(l.in, es) * es);
-    f.dw = plan_product(wide, l.in, l.tokens, es);
-    if (!grid_fits(f.dw)) return OCC_E_SHAPE;
-    part = std::max(part, f.dw.part_bytes);
   }
-  if (part) f.part_off = c.take(part);   // one product after the other
+  if (prod) {
+    f.prod = plan_products({l.dX ? l.tokens : 0, l.dW ? wide : 0}, {l.in, l.in}, {wide, l.tokens}, es, false);
+    if (!f.prod.fits) return OCC_E_SHAPE;
+    if (f.prod.x.splits > 1) f.dx_part = c.take(f.prod.x.part_bytes);
+    if (f.prod.w.splits > 1) f.dw_part = c.take(f.prod.w.part_bytes);
+  }
   f.bytes = c.total();
   return OCC_OK;
 }
@@ -354,8 +454,9 @@ template <class T, bool GATED>
 occ_status_t run_bwd(const occ_linear_grad_t& l, const BwdPlan& f, bool accumulate, char* ws, hipStream_t s) {
   const int64_t wide = GATED ? 2 * l.out : l.out;
   const bool act = GATED || l.act != OCC_ACT_NONE;
+  PrepArgs prep{};
   if (f.strips) {
-    DzArgs d{};
+    DzArgs& d = prep.dz;
     d.dY = l.dY;
     d.ldy = l.lddy;
     d.Z = act ? l.Z : nullptr;
@@ -367,15 +468,8 @@ occ_status_t run_bwd(const occ_linear_grad_t& l, const BwdPlan& f, bool accumula
     d.out = (int32_t)l.out;
     d.act = l.act;
     d.strip = (int32_t)f.strip;
-    OCC_TRY(launch("dz", s, [&] {
-      hipLaunchKernelGGL((k_dz<T, GATED>), dim3((unsigned)div_up(l.out, DZ_LANES * 4), (unsigned)f.strips), dim3(256),
-                         0, s, d);
-    }));
-    if (l.dbias)
-      OCC_TRY(launch("dz_bias", s, [&] {
-        hipLaunchKernelGGL(k_dz_bias, dim3((unsigned)div_up(wide, 256)), dim3(256), 0, s, (const float*)d.bias_part,
-                           (int)f.strips, wide, l.dbias, accumulate ? 1 : 0);
-      }));
+    d.across = (int32_t)div_up(l.out, DZ_LANES * 4);
+    prep.dz_blocks = (int32_t)(d.across * f.strips);
   }
   const void* dz = l.dY;
   int64_t ldd = l.lddy;
@@ -383,37 +477,39 @@ occ_status_t run_bwd(const occ_linear_grad_t& l, const BwdPlan& f, bool accumula
     dz = ws + f.dz_off;
     ldd = f.ldd;
   }
-  if (f.copy_dy) OCC_TRY(copy_operand<T>(l.dY, l.lddy, l.tokens, l.out, ws + f.dz_off, s));
+  CopyArgs copies[3] = {};
+  int nc = 0;
+  if (f.copy_dy) copies[nc++] = copy_operand<T>(l.dY, l.lddy, l.tokens, l.out, ws + f.dz_off);
+  if (f.copy_w) copies[nc++] = copy_operand<T>(l.W, l.ldw, wide, l.in, ws + f.w_off);
+  if (f.copy_x) copies[nc++] = copy_operand<T>(l.X, l.ldx, l.tokens, l.in, ws + f.x_off);
+  for (int i = 0; i < 3; ++i) prep.copy[i] = copies[i];
+  OCC_TRY((run_prep<T, GATED>(prep, s)));
+
+  const double bytes = (double)sizeof(T) * ((double)l.tokens * (double)(2 * l.in + wide) + 2.0 * (double)wide * (double)l.in);
+  const bool stream = bytes > kStreamBytes;
+  BackwardArgs a{};
   if (l.dX) {
-    GemmArgs g{};
+    GemmArgs& g = a.dx;
     g.A = dz;
     g.lda = ldd;
-    g.B = l.W;
-    g.ldb = l.ldw;
-    if (f.copy_w) {
-      OCC_TRY(copy_operand<T>(l.W, l.ldw, wide, l.in, ws + f.w_off, s));
-      g.B = ws + f.w_off;
-      g.ldb = piece_ld(l.in, sizeof(T));
-    }
+    g.B = f.copy_w ? ws + f.w_off : l.W;
+    g.ldb = f.copy_w ? piece_ld(l.in, sizeof(T)) : l.ldw;
     g.M = (int32_t)l.tokens;
     g.N = (int32_t)l.in;
     g.ka = (int32_t)f.ldd;
     g.kb = (int32_t)wide;
     g.C = l.dX;
     g.ldc = l.lddx;
-    OCC_TRY((run_product<T, false, true, EP_STORE>("dgrad", f.dx, g, ws, f.part_off, s)));
+    g.stream = stream && rows_on_lines(l.dX, l.lddx, l.in, sizeof(T));
+    set_tiles(g, f.prod.x, ws + f.dx_part);
+    a.dx_blocks = (int32_t)f.prod.x.blocks();
   }
   if (l.dW) {
-    GemmArgs g{};
+    GemmArgs& g = a.dw;
     g.A = dz;
     g.lda = ldd;
-    g.B = l.X;
-    g.ldb = l.ldx;
-    if (f.copy_x) {
-      OCC_TRY(copy_operand<T>(l.X, l.ldx, l.tokens, l.in, ws + f.x_off, s));
-      g.B = ws + f.x_off;
-      g.ldb = piece_ld(l.in, sizeof(T));
-    }
+    g.B = f.copy_x ? ws + f.x_off : l.X;
+    g.ldb = f.copy_x ? piece_ld(l.in, sizeof(T)) : l.ldx;
     g.M = (int32_t)wide;
     g.N = (int32_t)l.in;
     g.ka = g.kb = (int32_t)l.tokens;
@@ -421,9 +517,38 @@ occ_status_t run_bwd(const occ_linear_grad_t& l, const BwdPlan& f, bool accumula
     g.ldc = l.lddw;
     g.c_f32 = l.dw_dtype == OCC_F32;
     g.accumulate = accumulate;
-    OCC_TRY((run_product<T, true, true, EP_STORE>("wgrad", f.dw, g, ws, f.part_off, s)));
+    g.stream = stream && rows_on_lines(l.dW, l.lddw, l.in, elem_size(l.dw_dtype));
+    set_tiles(g, f.prod.w, ws + f.dw_part);
+    a.dw_blocks = (int32_t)f.prod.w.blocks();
   }
-  return OCC_OK;
+  int64_t bias_blocks = 0;
+  if (l.dbias) {
+    a.bias.part = (const float*)(ws + f.bias_off);
+    a.bias.dbias = l.dbias;
+    a.bias.width = wide;
+    a.bias.strips = (int32_t)f.strips;
+    a.bias.accumulate = accumulate;
+    bias_blocks = div_up(wide, 64);
+  }
+  const int64_t blocks = (int64_t)a.dx_blocks + a.dw_blocks + bias_blocks;
+  if (!a.dx_blocks && !a.dw_blocks)
+    return launch("layer_bias", s, [&] {
+      hipLaunchKernelGGL(k_bias, dim3((unsigned)bias_blocks), dim3(512), 0, s, a.bias);
+    });
+  const dim3 grid((unsigned)blocks), block(512);
+  OCC_TRY(launch("layer_bwd", s, [&] {
+    switch (f.prod.tile) {
+      case TILE_256: hipLaunchKernelGGL((k_backward<T, Form256>), grid, block, 0, s, a); break;
+      case TILE_128: hipLaunchKernelGGL((k_backward<T, Form128>), grid, block, 0, s, a); break;
+      default: hipLaunchKernelGGL((k_backward<T, Form64>), grid, block, 0, s, a); break;
+    }
+  }));
+  const unsigned jx = l.dX && a.dx.splits > 1 ? join_blocks(a.dx) : 0;
+  const unsigned jw = l.dW && a.dw.splits > 1 ? join_blocks(a.dw) : 0;
+  if (!jx && !jw) return OCC_OK;
+  return launch("layer_join", s, [&] {
+    hipLaunchKernelGGL((k_backward_join<T>), dim3(jx + jw), dim3(256), 0, s, a.dx, a.dw, (int)jx);
+  });
 }
 
 template <class T>
