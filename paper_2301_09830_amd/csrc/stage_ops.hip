@@ -69,8 +69,8 @@ struct TileTimes {
 };
 // bf16: 8192 x 8192 x K, slope and intercept; 128 and 64: one round at K = 4096.
 // fp32 is bound by the matrix unit (256 x 256 x 32 in 16384 clocks) in each.
-constexpr TileTimes kTiles[TILE_NUM] = {{256, 1, 1.38, 7.9, 11.0}, {128, 1, 0.57, 2.0, 4.0}, {64, 2, 0.42, 1.0, 3.0}};
-constexpr double kJoinUs = 4.0, kJoinBytesPerUs = 10e6;
+constexpr TileTimes kTiles[TILE_NUM] = {{256, 1, 1.38, 7.9, 11.0}, {128, 1, 0.57, 2.0, 4.0}, {64, 2, 0.42, 1.15, 3.0}};
+constexpr double kJoinUs = 6.0, kJoinBytesPerUs = 10e6;
 constexpr int kCUs = 256;
 constexpr int kSplits = 8;
 constexpr int kSplitCounts[kSplits] = {1, 2, 3, 4, 6, 8, 12, 16};
@@ -111,6 +111,7 @@ bool product_fits(const Product& p) {
 struct ProductPlan {
   Tile tile = TILE_256;
   Product x, w;   // of the backward pass; the forward pass has x alone
+  double us = 0.0;
   bool fits = false;
 };
 
@@ -160,6 +161,7 @@ ProductPlan plan_products(const int64_t (&m)[2], const int64_t (&width)[2], cons
           best.tile = (Tile)t;
           best.x = px;
           best.w = pw;
+          best.us = us;
           best.fits = true;
         }
       }
@@ -225,12 +227,26 @@ occ_status_t run_prep(const PrepArgs& p, hipStream_t s) {
 // ----------------------------------------------------------------------------
 // forward
 // ----------------------------------------------------------------------------
-// Up to kFewTokens the weights are streamed through registers: row by row
+// Up to kFewTokens the weights can be streamed through registers: row by row
 // along K up to kDotTokens (one token, 8192 x 8192 bf16: 23.6 us; through the
 // matrix instructions 31.6), by matrix instructions above (8 tokens, 4096 x
-// 16384: 31.4 us; row by row 36.7).
+// 16384: 31.4 us; row by row 36.7).  Above kDotTokens the tiled product takes
+// over where it is estimated to be faster: 8192 x 8192 bf16 with 8 tokens 24.6
+// against 32.0 us and with 64 tokens 26.1 against 74.8, but 4096 x 4096 with 8
+// tokens 13.5 (two launches) against 8.6.
 constexpr int64_t kDotTokens = 4;
 constexpr int64_t kFewTokens = 64;
+
+// us of the streaming form: a block reads 16 rows of W (of each projection),
+// and the more tokens it holds the slower; bf16 rows off 16 bytes take twice as long.
+double few_us(int64_t tokens, int64_t n_in, int64_t out, size_t es, bool gated, bool on_pieces) {
+  const double bytes = (double)div_up(div_up(out, 16), kCUs) * 16.0 * (gated ? 2 : 1) * (double)n_in * (double)es;
+  const double rate = 20e3 / (1.0 + (double)tokens / 40.0);   // bytes a us of one CU
+  return 2.0 + bytes / rate * (on_pieces || es == 4 ? 1.0 : 2.0);
+}
+
+// us of the copy of an operand that the tiled product cannot take in place
+double copy_us(int64_t rows, int64_t cols, size_t es) { return 3.0 + 2.0 * (double)rows * (double)cols * (double)es / 6e6; }
 
 struct FwdPlan {
   bool few = false, copy_x = false, copy_w = false;
@@ -252,7 +268,7 @@ occ_status_t check_fwd(const occ_linear_t* l, bool gated) {
 
 occ_status_t plan_fwd(const occ_linear_t& l, bool gated, FwdPlan& f) {
   if (l.tokens == 0) return OCC_OK;
-  f.few = l.tokens <= kFewTokens;
+  f.few = l.tokens <= kDotTokens;
   if (f.few) return OCC_OK;
   const size_t es = elem_size(l.dtype);
   const int64_t wide = gated ? 2 * l.out : l.out;
@@ -260,6 +276,11 @@ occ_status_t plan_fwd(const occ_linear_t& l, bool gated, FwdPlan& f) {
   f.copy_w = needs_copy(l.W, l.ldw, l.in, es);
   f.prod = plan_products({l.tokens, 0}, {wide, 0}, {l.in, 0}, es, gated);
   if (!f.prod.fits) return OCC_E_SHAPE;
+  if (l.tokens <= kFewTokens) {
+    const double tiled = f.prod.us + (f.copy_w ? copy_us(wide, l.in, es) : 0.0);
+    f.few = few_us(l.tokens, l.in, l.out, es, gated, !f.copy_w) <= tiled;
+    if (f.few) return OCC_OK;
+  }
   Carve c;
   const size_t row = (size_t)piece_ld(l.in, es) * es;
   if (f.copy_x) f.x_off = c.take((size_t)l.tokens * row);
