@@ -250,7 +250,7 @@ struct GemmArgs {
   int32_t ka, kb;     // K of each operand; K contiguous: whole 16-byte pieces, zeros behind K's end
   int32_t tiles_m, tiles_n;
   int32_t splits, tiles_k, k_per_split;   // K in tiles of 128 bytes of elements
-  float* part;        // splits > 1: partial sums, splits x M x width
+  float* part;        // splits > 1: partial sums, splits x M x part_width(N)
   void* C;            // EP_STORE: the result
   int64_t ldc;
   int32_t c_f32, accumulate, stream;
@@ -258,6 +258,12 @@ struct GemmArgs {
 };
 
 enum { EP_STORE = 0, EP_FWD = 1, EP_GATED = 2 };
+
+// Columns of a partial sum's row: whole quads, the gate's and then the others'.
+template <int EP>
+__device__ __forceinline__ int64_t part_width(const GemmArgs& g) {
+  return (int64_t)((g.N + 3) & ~3) * (EP == EP_GATED ? 2 : 1);
+}
 
 constexpr int kRowBytes = 128;   // of a row of K in a tile: 64 bf16 or 32 fp32
 
@@ -651,7 +657,6 @@ __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_cha
   const int li = lane & 15, lg = lane >> 4;
   const int q = lane % QPR, n = n0 + q * 4, left = g.N - n;
   const bool split_k = g.splits > 1;
-  const int64_t width = EP == EP_GATED ? 2 * (int64_t)g.N : g.N;
   typedef __attribute__((address_space(3))) f32x4_t lds_f4;
   // The loads of a run of rows (the residual's) end before its stores begin,
   // and the bias is in before all of them: memory operations are counted in
@@ -695,9 +700,9 @@ __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_cha
         f32x4_t z = *(const lds_f4*)(lds + row * BN * 4 + ((q ^ (row & 15)) << 4)), u = {};
         if constexpr (EP == EP_GATED) u = *(const lds_f4*)(lds + row * BN * 4 + (((QPR + q) ^ (row & 15)) << 4));
         if (split_k) {
-          float* const dst = g.part + ((int64_t)split * g.M + m) * width + n;
-          st_quad(dst, z, left);
-          if constexpr (EP == EP_GATED) st_quad(dst + g.N, u, left);
+          float* const dst = g.part + ((int64_t)split * g.M + m) * part_width<EP>(g) + n;
+          *(f32x4_t*)dst = z;
+          if constexpr (EP == EP_GATED) *(f32x4_t*)(dst + part_width<EP>(g) / 2) = u;
         } else if constexpr (EP == EP_STORE) {
           store_result<T>(g, m, n, z, left);
         } else {
@@ -718,16 +723,27 @@ __global__ __launch_bounds__(F::NW * 64, 2) void k_gemm(GemmArgs g) {
 template <class T, int EP>
 __device__ __forceinline__ void join_block(const GemmArgs& g, int block, int blocks) {
   const int quads = (g.N + 3) / 4;
-  const int width = EP == EP_GATED ? 2 * g.N : g.N;
-  const int64_t total = (int64_t)g.M * quads, stride = (int64_t)g.M * width;
+  const int64_t width = part_width<EP>(g), total = (int64_t)g.M * quads, stride = g.M * width;
   for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < total; i += (int64_t)blocks * 256) {
-    const int64_t m = i / quads;
+    const int64_t m = total >> 32 ? i / quads : (int64_t)((uint32_t)i / (uint32_t)quads);
     const int n = (int)(i - m * quads) * 4, left = g.N - n;
     const float* p = g.part + m * width + n;
     f32x4_t z = {}, u = {};
-    for (int s = 0; s < g.splits; ++s, p += stride) {
-      z += ld_quad<float>(p, left);
-      if constexpr (EP == EP_GATED) u += ld_quad<float>(p + g.N, left);
+    // four parts at a time, so that their loads are in flight together
+    for (int s = 0; s < g.splits; s += 4, p += 4 * stride) {
+      f32x4_t a[4], b[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float* const q = p + min(j, g.splits - 1 - s) * stride;
+        a[j] = *(const f32x4_t*)q;
+        if constexpr (EP == EP_GATED) b[j] = *(const f32x4_t*)(q + width / 2);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (s + j < g.splits) {
+          z += a[j];
+          if constexpr (EP == EP_GATED) u += b[j];
+        }
     }
     if constexpr (EP == EP_STORE) {
       store_result<T>(g, m, n, z, left);

@@ -64,13 +64,15 @@ bool ld_ok(int64_t cols, int64_t ld) { return ld >= cols && ld < kMaxDim; }
 enum Tile { TILE_256, TILE_128, TILE_64, TILE_NUM };
 
 struct TileTimes {
-  int side, resident;              // resident: blocks a CU
+  int side;
+  int resident;                    // blocks a CU that do not slow each other down (bf16)
   double k_bf16, k_f32, fixed;     // us; K tiles of all resident blocks
 };
 // bf16: 8192 x 8192 x K, slope and intercept; 128 and 64: one round at K = 4096.
-// fp32 is bound by the matrix unit (256 x 256 x 32 in 16384 clocks) in each.
-constexpr TileTimes kTiles[TILE_NUM] = {{256, 1, 1.38, 7.9, 11.0}, {128, 1, 0.57, 2.0, 4.0}, {64, 2, 0.42, 1.15, 3.0}};
-constexpr double kJoinUs = 6.0, kJoinBytesPerUs = 10e6;
+// fp32 is bound by the matrix unit in each (256 x 256 x 32 in 16384 clocks), so
+// two resident blocks share its time.
+constexpr TileTimes kTiles[TILE_NUM] = {{256, 1, 1.38, 7.9, 13.0}, {128, 1, 0.57, 2.0, 4.0}, {64, 2, 0.42, 0.58, 3.0}};
+constexpr double kJoinUs = 6.0, kJoinBytesPerUs = 5e6;
 constexpr int kCUs = 256;
 constexpr int kSplits = 8;
 constexpr int kSplitCounts[kSplits] = {1, 2, 3, 4, 6, 8, 12, 16};
@@ -96,7 +98,7 @@ Product make_product(int64_t m, int64_t width, int64_t k, size_t es, Tile tile, 
   p.splits = (int)div_up(p.tiles_k, p.k_per_split);
   p.block_us = (double)p.k_per_split * (es == 2 ? t.k_bf16 : t.k_f32) + t.fixed;
   if (p.splits > 1) {
-    const double part = (double)p.splits * (double)m * (double)width * 4.0;
+    const double part = (double)p.splits * (double)m * (double)(pair ? 2 * up(width / 2, 4) : up(width, 4)) * 4.0;
     p.part_bytes = (size_t)part;
     p.join_us = kJoinUs + part / kJoinBytesPerUs;
   }
@@ -116,13 +118,16 @@ struct ProductPlan {
 };
 
 // Time of a launch on `slots` resident blocks: the blocks of x, then those of
-// w, each to the first free slot.
-double launch_us(const Product& x, const Product& w, int64_t slots) {
+// w, each to the first free slot.  halves: a block of w lands beside one of x
+// on the same CU and each runs at half speed.
+double launch_us(const Product& x, const Product& w, int64_t slots, bool halves) {
   const int64_t nx = x.blocks(), nw = w.blocks();
   const int64_t rest = nx % slots, free = slots - rest;
   const double full = (double)(nx / slots) * x.block_us;   // whole rounds of x
   if (!rest) return full + (double)div_up(nw, slots) * w.block_us;
   if (!nw) return full + x.block_us;
+  if (halves && rest + nw > slots)
+    return full + x.block_us + 0.5 * (double)nw * w.block_us / ((double)slots - 0.5 * (double)rest);
   const int64_t beside = (int64_t)(x.block_us / w.block_us);   // rounds of w beside the last blocks of x
   const int64_t left = nw - beside * free;
   if (left <= 0) return full + std::max(x.block_us, (double)div_up(nw, free) * w.block_us);
@@ -137,7 +142,8 @@ ProductPlan plan_products(const int64_t (&m)[2], const int64_t (&width)[2], cons
   ProductPlan best;
   double best_us = INFINITY;
   for (int t = 0; t < TILE_NUM; ++t) {
-    const double slots = (double)kCUs * kTiles[t].resident;
+    const bool halves = es == 4 && kTiles[t].resident > 1;
+    const int64_t slots = (int64_t)kCUs * (es == 4 ? 1 : kTiles[t].resident);
     Product of[2][kSplits];
     int n[2] = {0, 0};
     for (int i = 0; i < 2; ++i) {
@@ -149,13 +155,13 @@ ProductPlan plan_products(const int64_t (&m)[2], const int64_t (&width)[2], cons
         const Product p = make_product(m[i], width[i], k[i], es, (Tile)t, s, pair);
         if (p.splits != s || (s > 1 && p.k_per_split < 4) || !product_fits(p)) break;
         of[i][n[i]++] = p;
-        if ((double)p.blocks() > 2.0 * slots) break;   // parts of K would only add work
+        if (p.blocks() > 2 * slots) break;   // parts of K would only add work
       }
     }
     for (int x = 0; x < n[0]; ++x) {
       for (int w = 0; w < n[1]; ++w) {
         const Product &px = of[0][x], &pw = of[1][w];
-        const double us = std::max(px.join_us, pw.join_us) + launch_us(px, pw, kCUs * kTiles[t].resident);
+        const double us = std::max(px.join_us, pw.join_us) + launch_us(px, pw, slots, halves);
         if (us < best_us) {
           best_us = us;
           best.tile = (Tile)t;
