@@ -82,7 +82,7 @@ constexpr double kMaxPartBytes = 512e6;
 struct Product {
   int64_t tiles_m = 0, tiles_n = 0, tiles_k = 0;
   int splits = 1, k_per_split = 1;
-  double block_us = 0.0, join_us = 0.0;
+  double block_us = 0.0;
   size_t part_bytes = 0;
   int64_t blocks() const { return tiles_m * tiles_n * splits; }
 };
@@ -100,7 +100,6 @@ Product make_product(int64_t m, int64_t width, int64_t k, size_t es, Tile tile, 
   if (p.splits > 1) {
     const double part = (double)p.splits * (double)m * (double)(pair ? 2 * up(width / 2, 4) : up(width, 4)) * 4.0;
     p.part_bytes = (size_t)part;
-    p.join_us = kJoinUs + part / kJoinBytesPerUs;
   }
   return p;
 }
@@ -161,7 +160,8 @@ ProductPlan plan_products(const int64_t (&m)[2], const int64_t (&width)[2], cons
     for (int x = 0; x < n[0]; ++x) {
       for (int w = 0; w < n[1]; ++w) {
         const Product &px = of[0][x], &pw = of[1][w];
-        const double us = std::max(px.join_us, pw.join_us) + launch_us(px, pw, slots, halves);
+        const double parts = (double)(px.part_bytes + pw.part_bytes);
+        const double us = launch_us(px, pw, slots, halves) + (parts > 0.0 ? kJoinUs + parts / kJoinBytesPerUs : 0.0);
         if (us < best_us) {
           best_us = us;
           best.tile = (Tile)t;
