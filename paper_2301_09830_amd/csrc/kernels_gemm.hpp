@@ -59,29 +59,36 @@ __device__ __forceinline__ float normal_cdf(float z, float& e) {
 constexpr float kGeluC = 0.79788456080286536f;   // sqrt(2 / pi)
 constexpr float kGeluA = 0.044715f;
 
-__device__ __forceinline__ f32x4_t act_quad(int act, f32x4_t z) {
-  f32x4_t y = z;
-  float e;
+// y = act(z) of N quads: one branch for all of them
+template <int N>
+__device__ __forceinline__ void act_quads(int act, const f32x4_t* z, f32x4_t* y) {
+  auto each = [&](auto&& f) {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[k][i] = f(z[k][i]);
+  };
   switch (act) {   // the same for all lanes
-    case ACT_RELU:
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = z[i] > 0.0f || z[i] != z[i] ? z[i] : 0.0f;
-      break;
+    case ACT_RELU: each([](float v) { return v > 0.0f || v != v ? v : 0.0f; }); break;
     case ACT_GELU:
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = z[i] * normal_cdf(z[i], e);
+      each([](float v) {
+        float e;
+        return v * normal_cdf(v, e);
+      });
       break;
     case ACT_GELU_TANH:   // (1 + tanh q) / 2 = sigmoid(2 q)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        y[i] = z[i] * sigmoid_f(z[i] * __builtin_fmaf(2.0f * kGeluC * kGeluA, z[i] * z[i], 2.0f * kGeluC));
+      each([](float v) {
+        return v * sigmoid_f(v * __builtin_fmaf(2.0f * kGeluC * kGeluA, v * v, 2.0f * kGeluC));
+      });
       break;
-    case ACT_SILU:
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = z[i] * sigmoid_f(z[i]);
-      break;
-    default: break;
+    case ACT_SILU: each([](float v) { return v * sigmoid_f(v); }); break;
+    default: each([](float v) { return v; });
   }
+}
+
+__device__ __forceinline__ f32x4_t act_quad(int act, f32x4_t z) {
+  f32x4_t y;
+  act_quads<1>(act, &z, &y);
   return y;
 }
 
@@ -461,6 +468,68 @@ __device__ __forceinline__ void store_result(const GemmArgs& g, int64_t m, int n
   else store_as<uint16_t>(g, m, n, v, left);
 }
 
+// Rows m, m + RPI, .. of a tile that lies inside the result.
+template <class TC, int RUN, int RPI>
+__device__ __forceinline__ void store_rows(const GemmArgs& g, int64_t m, int n, f32x4_t* v) {
+  TC* const p = (TC*)g.C + m * g.ldc + n;
+  const int64_t step = RPI * g.ldc;
+  if (g.accumulate) {
+#pragma unroll
+    for (int r = 0; r < RUN; ++r) v[r] += ld_quad<TC>(p + r * step, 4);
+  }
+  if (g.stream) {
+#pragma unroll
+    for (int r = 0; r < RUN; ++r) st_quad<TC, true>(p + r * step, v[r], 4);
+  } else {
+#pragma unroll
+    for (int r = 0; r < RUN; ++r) st_quad(p + r * step, v[r], 4);
+  }
+}
+
+template <class T, bool GATED, int RUN, int RPI>
+__device__ __forceinline__ void fwd_rows(const FwdEpi& e, int64_t m, int n, const f32x4_t* z, const f32x4_t* u) {
+  f32x4_t res[RUN] = {}, y[RUN];
+  if (e.R) {
+    const T* const p = (const T*)e.R + m * e.ldr + n;
+#pragma unroll
+    for (int r = 0; r < RUN; ++r) res[r] = ld_quad<T>(p + r * RPI * e.ldr, 4);
+#pragma unroll
+    for (int r = 0; r < RUN; ++r) asm volatile("" : "+v"(res[r]));
+  }
+  if (e.Z) {
+    T* const p = (T*)e.Z + m * e.ldz + n;
+    const int64_t step = RPI * e.ldz;
+    if (e.stream) {
+#pragma unroll
+      for (int r = 0; r < RUN; ++r) {
+        st_quad<T, true>(p + r * step, z[r], 4);
+        if constexpr (GATED) st_quad<T, true>(p + r * step + e.out, u[r], 4);
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < RUN; ++r) {
+        st_quad(p + r * step, z[r], 4);
+        if constexpr (GATED) st_quad(p + r * step + e.out, u[r], 4);
+      }
+    }
+  }
+  act_quads<RUN>(e.act, z, y);
+#pragma unroll
+  for (int r = 0; r < RUN; ++r) {
+    if constexpr (GATED) y[r] *= u[r];
+    y[r] += res[r];
+  }
+  T* const p = (T*)e.Y + m * e.ldy + n;
+  const int64_t step = RPI * e.ldy;
+  if (e.stream) {
+#pragma unroll
+    for (int r = 0; r < RUN; ++r) st_quad<T, true>(p + r * step, y[r], 4);
+  } else {
+#pragma unroll
+    for (int r = 0; r < RUN; ++r) st_quad(p + r * step, y[r], 4);
+  }
+}
+
 // A form of the product: WM x WN waves, each 16 FA x 16 FB results, S stages
 // of K tiles in LDS.
 // S == 2 (256 x 256): the waves form two groups, one wave of each on every
@@ -658,9 +727,11 @@ __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_cha
   const int q = lane % QPR, n = n0 + q * 4, left = g.N - n;
   const bool split_k = g.splits > 1;
   typedef __attribute__((address_space(3))) f32x4_t lds_f4;
-  // The loads of a run of rows (the residual's) end before its stores begin,
-  // and the bias is in before all of them: memory operations are counted in
-  // order, so a load that is waited for behind stores waits for them too.
+  // Runs of rows without a test per row or column where the whole tile lies
+  // inside the result: a wave has 32 rows to go, and its MFMAs wait.  The loads
+  // of a run (the residual's) end before its stores begin, and the bias is in
+  // before all of them: memory operations are counted in order, so a load that
+  // is waited for behind stores waits for them too.
   f32x4_t bz = {}, bu = {};
   if (EP != EP_STORE && !split_k && left > 0) {
     bz = bias_quad(g.fwd, n, left);
@@ -668,6 +739,9 @@ __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_cha
   }
   asm volatile("" : "+v"(bz), "+v"(bu));
   constexpr int STEPS = PR / NW / RPI, RUN = STEPS < 4 ? STEPS : 4;
+  static_assert(PR / NW <= WR && WR % (PR / NW) == 0, "a wave's rows follow each other in the result");
+  const int row0 = wave * (PR / NW) + lane / QPR;
+  const bool whole = m0 + BM <= g.M && n0 + BNC <= g.N;
 #pragma unroll
   for (int p = 0; p < NP; ++p) {
     if (p) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -680,33 +754,43 @@ __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_cha
         *(lds_f4*)(lds + (wm * WR + a * 16 + li) * BN * 4 + ((c ^ li) << 4)) = acc[p * (FA / NP) + a][b];
       }
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    const int64_t mrow = m0 + row0 / WR * (FA * 16) + p * WR + row0 % WR;
+#pragma unroll 1
     for (int r0 = 0; r0 < STEPS; r0 += RUN) {
-      f32x4_t res[RUN] = {};
-      if (EP != EP_STORE && !split_k && g.fwd.R && left > 0) {
-#pragma unroll
-        for (int r = 0; r < RUN; ++r) {
-          const int row = wave * (PR / NW) + (r0 + r) * RPI + lane / QPR;
-          const int64_t m = m0 + row / WR * (FA * 16) + p * WR + row % WR;
-          if (m < g.M) res[r] = residual_quad<T>(g.fwd, m, n, left);
-        }
-#pragma unroll
-        for (int r = 0; r < RUN; ++r) asm volatile("" : "+v"(res[r]));
-      }
+      f32x4_t z[RUN], u[RUN] = {};
 #pragma unroll
       for (int r = 0; r < RUN; ++r) {
-        const int row = wave * (PR / NW) + (r0 + r) * RPI + lane / QPR;
-        const int64_t m = m0 + row / WR * (FA * 16) + p * WR + row % WR;
-        if (m >= g.M || left <= 0) continue;
-        f32x4_t z = *(const lds_f4*)(lds + row * BN * 4 + ((q ^ (row & 15)) << 4)), u = {};
-        if constexpr (EP == EP_GATED) u = *(const lds_f4*)(lds + row * BN * 4 + (((QPR + q) ^ (row & 15)) << 4));
-        if (split_k) {
-          float* const dst = g.part + ((int64_t)split * g.M + m) * part_width<EP>(g) + n;
-          *(f32x4_t*)dst = z;
-          if constexpr (EP == EP_GATED) *(f32x4_t*)(dst + part_width<EP>(g) / 2) = u;
-        } else if constexpr (EP == EP_STORE) {
-          store_result<T>(g, m, n, z, left);
-        } else {
-          fwd_epilogue<T, EP == EP_GATED>(g.fwd, m, n, z + bz, u + bu, res[r]);
+        const int row = row0 + (r0 + r) * RPI;
+        z[r] = *(const lds_f4*)(lds + row * BN * 4 + ((q ^ (row & 15)) << 4)) + bz;
+        if constexpr (EP == EP_GATED) u[r] = *(const lds_f4*)(lds + row * BN * 4 + (((QPR + q) ^ (row & 15)) << 4)) + bu;
+      }
+      const int64_t m = mrow + r0 * RPI;
+      if (split_k) {
+        const int64_t w = part_width<EP>(g);
+        float* const dst = g.part + ((int64_t)split * g.M + m) * w + n;
+#pragma unroll
+        for (int r = 0; r < RUN; ++r) {
+          if (!whole && (m + r * RPI >= g.M || left <= 0)) continue;
+          *(f32x4_t*)(dst + r * RPI * w) = z[r];
+          if constexpr (EP == EP_GATED) *(f32x4_t*)(dst + r * RPI * w + w / 2) = u[r];
+        }
+      } else if constexpr (EP == EP_STORE) {
+        if (whole) {
+          if (sizeof(T) == 4 || g.c_f32) store_rows<float, RUN, RPI>(g, m, n, z);
+          else store_rows<uint16_t, RUN, RPI>(g, m, n, z);
+        } else if (left > 0) {
+#pragma unroll
+          for (int r = 0; r < RUN; ++r)
+            if (m + r * RPI < g.M) store_result<T>(g, m + r * RPI, n, z[r], left);
+        }
+      } else if (whole) {
+        fwd_rows<T, EP == EP_GATED, RUN, RPI>(g.fwd, m, n, z, u);
+      } else if (left > 0) {
+#pragma unroll
+        for (int r = 0; r < RUN; ++r) {
+          const int64_t mr = m + r * RPI;
+          if (mr < g.M)
+            fwd_epilogue<T, EP == EP_GATED>(g.fwd, mr, n, z[r], u[r], residual_quad<T>(g.fwd, mr, n, left));
         }
       }
     }
