@@ -468,31 +468,39 @@ __device__ __forceinline__ void store_result(const GemmArgs& g, int64_t m, int n
   else store_as<uint16_t>(g, m, n, v, left);
 }
 
-// Rows m, m + RPI, .. of a tile that lies inside the result.
-template <class TC, int RUN, int RPI>
+// Rows m, m + RPI, .. (EDGE: those below M) of a lane whose four columns lie
+// inside the result.
+template <class TC, int RUN, int RPI, bool EDGE>
 __device__ __forceinline__ void store_rows(const GemmArgs& g, int64_t m, int n, f32x4_t* v) {
   TC* const p = (TC*)g.C + m * g.ldc + n;
   const int64_t step = RPI * g.ldc;
+  auto in = [&](int r) { return !EDGE || m + r * RPI < g.M; };
   if (g.accumulate) {
 #pragma unroll
-    for (int r = 0; r < RUN; ++r) v[r] += ld_quad<TC>(p + r * step, 4);
+    for (int r = 0; r < RUN; ++r)
+      if (in(r)) v[r] += ld_quad<TC>(p + r * step, 4);
   }
   if (g.stream) {
 #pragma unroll
-    for (int r = 0; r < RUN; ++r) st_quad<TC, true>(p + r * step, v[r], 4);
+    for (int r = 0; r < RUN; ++r)
+      if (in(r)) st_quad<TC, true>(p + r * step, v[r], 4);
   } else {
 #pragma unroll
-    for (int r = 0; r < RUN; ++r) st_quad(p + r * step, v[r], 4);
+    for (int r = 0; r < RUN; ++r)
+      if (in(r)) st_quad(p + r * step, v[r], 4);
   }
 }
 
-template <class T, bool GATED, int RUN, int RPI>
-__device__ __forceinline__ void fwd_rows(const FwdEpi& e, int64_t m, int n, const f32x4_t* z, const f32x4_t* u) {
+template <class T, bool GATED, int RUN, int RPI, bool EDGE>
+__device__ __forceinline__ void fwd_rows(const FwdEpi& e, int64_t M, int64_t m, int n, const f32x4_t* z,
+                                         const f32x4_t* u) {
   f32x4_t res[RUN] = {}, y[RUN];
+  auto in = [&](int r) { return !EDGE || m + r * RPI < M; };
   if (e.R) {
     const T* const p = (const T*)e.R + m * e.ldr + n;
 #pragma unroll
-    for (int r = 0; r < RUN; ++r) res[r] = ld_quad<T>(p + r * RPI * e.ldr, 4);
+    for (int r = 0; r < RUN; ++r)
+      if (in(r)) res[r] = ld_quad<T>(p + r * RPI * e.ldr, 4);
 #pragma unroll
     for (int r = 0; r < RUN; ++r) asm volatile("" : "+v"(res[r]));
   }
@@ -501,16 +509,18 @@ __device__ __forceinline__ void fwd_rows(const FwdEpi& e, int64_t m, int n, cons
     const int64_t step = RPI * e.ldz;
     if (e.stream) {
 #pragma unroll
-      for (int r = 0; r < RUN; ++r) {
-        st_quad<T, true>(p + r * step, z[r], 4);
-        if constexpr (GATED) st_quad<T, true>(p + r * step + e.out, u[r], 4);
-      }
+      for (int r = 0; r < RUN; ++r)
+        if (in(r)) {
+          st_quad<T, true>(p + r * step, z[r], 4);
+          if constexpr (GATED) st_quad<T, true>(p + r * step + e.out, u[r], 4);
+        }
     } else {
 #pragma unroll
-      for (int r = 0; r < RUN; ++r) {
-        st_quad(p + r * step, z[r], 4);
-        if constexpr (GATED) st_quad(p + r * step + e.out, u[r], 4);
-      }
+      for (int r = 0; r < RUN; ++r)
+        if (in(r)) {
+          st_quad(p + r * step, z[r], 4);
+          if constexpr (GATED) st_quad(p + r * step + e.out, u[r], 4);
+        }
     }
   }
   act_quads<RUN>(e.act, z, y);
@@ -523,10 +533,12 @@ __device__ __forceinline__ void fwd_rows(const FwdEpi& e, int64_t m, int n, cons
   const int64_t step = RPI * e.ldy;
   if (e.stream) {
 #pragma unroll
-    for (int r = 0; r < RUN; ++r) st_quad<T, true>(p + r * step, y[r], 4);
+    for (int r = 0; r < RUN; ++r)
+      if (in(r)) st_quad<T, true>(p + r * step, y[r], 4);
   } else {
 #pragma unroll
-    for (int r = 0; r < RUN; ++r) st_quad(p + r * step, y[r], 4);
+    for (int r = 0; r < RUN; ++r)
+      if (in(r)) st_quad(p + r * step, y[r], 4);
   }
 }
 
@@ -727,8 +739,8 @@ __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_cha
   const int q = lane % QPR, n = n0 + q * 4, left = g.N - n;
   const bool split_k = g.splits > 1;
   typedef __attribute__((address_space(3))) f32x4_t lds_f4;
-  // Runs of rows without a test per row or column where the whole tile lies
-  // inside the result: a wave has 32 rows to go, and its MFMAs wait.  The loads
+  // Runs of rows without a test per element (tested per element, this part was
+  // bound by its instructions: 8192 x 4096 x 16384 bf16 865 us, 814 this way).  The loads
   // of a run (the residual's) end before its stores begin, and the bias is in
   // before all of them: memory operations are counted in order, so a load that
   // is waited for behind stores waits for them too.
@@ -774,23 +786,27 @@ __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_cha
           *(f32x4_t*)(dst + r * RPI * w) = z[r];
           if constexpr (EP == EP_GATED) *(f32x4_t*)(dst + r * RPI * w + w / 2) = u[r];
         }
-      } else if constexpr (EP == EP_STORE) {
-        if (whole) {
-          if (sizeof(T) == 4 || g.c_f32) store_rows<float, RUN, RPI>(g, m, n, z);
-          else store_rows<uint16_t, RUN, RPI>(g, m, n, z);
-        } else if (left > 0) {
-#pragma unroll
-          for (int r = 0; r < RUN; ++r)
-            if (m + r * RPI < g.M) store_result<T>(g, m + r * RPI, n, z[r], left);
-        }
       } else if (whole) {
-        fwd_rows<T, EP == EP_GATED, RUN, RPI>(g.fwd, m, n, z, u);
-      } else if (left > 0) {
-#pragma unroll
+        if constexpr (EP == EP_STORE) {
+          if (sizeof(T) == 4 || g.c_f32) store_rows<float, RUN, RPI, false>(g, m, n, z);
+          else store_rows<uint16_t, RUN, RPI, false>(g, m, n, z);
+        } else {
+          fwd_rows<T, EP == EP_GATED, RUN, RPI, false>(g.fwd, g.M, m, n, z, u);
+        }
+      } else if (left >= 4) {
+        if constexpr (EP == EP_STORE) {
+          if (sizeof(T) == 4 || g.c_f32) store_rows<float, RUN, RPI, true>(g, m, n, z);
+          else store_rows<uint16_t, RUN, RPI, true>(g, m, n, z);
+        } else {
+          fwd_rows<T, EP == EP_GATED, RUN, RPI, true>(g.fwd, g.M, m, n, z, u);
+        }
+      } else if (left > 0) {   // the lanes of the last one to three columns
+#pragma unroll 1
         for (int r = 0; r < RUN; ++r) {
           const int64_t mr = m + r * RPI;
-          if (mr < g.M)
-            fwd_epilogue<T, EP == EP_GATED>(g.fwd, mr, n, z[r], u[r], residual_quad<T>(g.fwd, mr, n, left));
+          if (mr >= g.M) continue;
+          if constexpr (EP == EP_STORE) store_result<T>(g, mr, n, z[r], left);
+          else fwd_epilogue<T, EP == EP_GATED>(g.fwd, mr, n, z[r], u[r], residual_quad<T>(g.fwd, mr, n, left));
         }
       }
     }
