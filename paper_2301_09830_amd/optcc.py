@@ -574,9 +574,7 @@ def occ_get_flags(ws, clear: bool = False, stream=None) -> int:
 # stage operators
 # ----------------------------------------------------------------------------
 def _mat(t, name: str, rows: int, cols: int, dtype):
-    """(pointer, leading dimension) of an optional rows x cols matrix."""
-    if t is None:
-        return None, 0
+    """(pointer, leading dimension) of a rows x cols matrix."""
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}")
     if t.shape != (rows, cols):
@@ -584,19 +582,27 @@ def _mat(t, name: str, rows: int, cols: int, dtype):
     ld, unit = t.stride()
     if unit != 1 and cols > 1:
         raise ValueError(f"{name} must have unit column stride (row-major)")
-    if rows <= 1:
-        return (t.data_ptr() if rows else None), cols
-    return t.data_ptr(), ld
+    if rows > 1:
+        return t.data_ptr(), ld
+    return (t.data_ptr() if rows else None), cols
+
+
+_NO_MATRIX = (None, 0)
 
 
 def _vec(t, name: str, n: int):
-    if t is None:
-        return None
     if t.dtype is not _torch().float32:
         raise TypeError(f"{name} must be float32")
     if t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name} must hold {n} contiguous values")
     return t.data_ptr()
+
+
+def _stream_of(t, stream) -> int:
+    """The given stream, or the current one of a tensor's device."""
+    if stream is not None:
+        return int(stream.cuda_stream)
+    return _torch()._C._cuda_getCurrentRawStream(t.get_device())
 
 
 def _workspace(nbytes: int, ws, device):
@@ -619,7 +625,7 @@ def _rows_cols(t, name: str):
 
 def _layer_fwd(name: str, wide: int, X, W, bias, act, R, Y, Z, ws, stream):
     tokens, n_in = _rows_cols(X, "X")
-    rows, _ = _rows_cols(W, "W")
+    rows = _rows_cols(W, "W")[0]
     out = rows // wide
     if rows != wide * out:
         raise ValueError("W must hold the rows of both projections")
@@ -628,14 +634,18 @@ def _layer_fwd(name: str, wide: int, X, W, bias, act, R, Y, Z, ws, stream):
         Y = _torch().empty((tokens, out), dtype=dt, device=X.device)
     x, ldx = _mat(X, "X", tokens, n_in, dt)
     w, ldw = _mat(W, "W", rows, n_in, dt)
-    r, ldr = _mat(R, "R", tokens, out, dt)
-    z, ldz = _mat(Z, "Z", tokens, rows, dt)
     y, ldy = _mat(Y, "Y", tokens, out, dt)
-    a = occ_linear_t(_mdtype(X), act, tokens, n_in, out, x, ldx, w, ldw, _vec(bias, "bias", rows),
-                     r, ldr, z, ldz, y, ldy)
+    r, ldr = _NO_MATRIX if R is None else _mat(R, "R", tokens, out, dt)
+    z, ldz = _NO_MATRIX if Z is None else _mat(Z, "Z", tokens, rows, dt)
+    a = occ_linear_t(_mdtype(X), act, tokens, n_in, out, x, ldx, w, ldw,
+                     None if bias is None else _vec(bias, "bias", rows), r, ldr, z, ldz, y, ldy)
     call, size = _layer_calls(name)
-    keep, wp, wn = _workspace(size(a), ws, X.device)
-    _check(name, call(a, wp, wn, _stream(stream)))
+    need = size(a)
+    if need:
+        keep, wp, wn = _workspace(need, ws, X.device)
+    else:
+        wp = wn = None
+    _check(name, call(a, wp, wn or 0, _stream_of(X, stream)))
     return Y
 
 
@@ -680,17 +690,17 @@ def _layer_bwd(name: str, wide: int, dY, X, W, Z, act, dX, dW, dbias, accumulate
     dt, rows = dY.dtype, wide * out
     dw_dt = dt if dW is None or dW.dtype is not torch.float32 else torch.float32
     dy, lddy = _mat(dY, "dY", tokens, out, dt)
-    x, ldx = _mat(X, "X", tokens, n_in, dt)
-    w, ldw = _mat(W, "W", rows, n_in, dt)
-    z, ldz = _mat(Z, "Z", tokens, rows, dt)
-    dx, lddx = _mat(dX, "dX", tokens, n_in, dt)
-    dw, lddw = _mat(dW, "dW", rows, n_in, dw_dt)
+    x, ldx = _NO_MATRIX if X is None else _mat(X, "X", tokens, n_in, dt)
+    w, ldw = _NO_MATRIX if W is None else _mat(W, "W", rows, n_in, dt)
+    z, ldz = _NO_MATRIX if Z is None else _mat(Z, "Z", tokens, rows, dt)
+    dx, lddx = _NO_MATRIX if dX is None else _mat(dX, "dX", tokens, n_in, dt)
+    dw, lddw = _NO_MATRIX if dW is None else _mat(dW, "dW", rows, n_in, dw_dt)
     a = occ_linear_grad_t(_mdtype(dY), OCC_F32 if dw_dt is torch.float32 else OCC_BF16, act, 0,
                           tokens, n_in, out, dy, lddy, x, ldx, w, ldw, z, ldz, dx, lddx, dw, lddw,
-                          _vec(dbias, "dbias", rows))
+                          None if dbias is None else _vec(dbias, "dbias", rows))
     call, size = _layer_calls(name)
     keep, wp, wn = _workspace(size(a), ws, dY.device)
-    _check(name, call(a, OCC_GRAD_ACCUMULATE if accumulate else 0, wp, wn, _stream(stream)))
+    _check(name, call(a, OCC_GRAD_ACCUMULATE if accumulate else 0, wp, wn, _stream_of(dY, stream)))
 
 
 def occ_linear_bwd(dY, X=None, W=None, Z=None, act: int = OCC_ACT_NONE, dX=None, dW=None,
@@ -776,7 +786,7 @@ def occ_adamw_step(params, lr: float, step: int, beta1: float = 0.9, beta2: floa
     if not isinstance(params, ctypes.Array):
         params = make_params(params)
     h = occ_adamw_t(lr, beta1, beta2, eps, step, seed & 0xFFFFFFFF, 0,
-                    _vec(grad_scale, "grad_scale", 1), None)
+                    None if grad_scale is None else _vec(grad_scale, "grad_scale", 1), None)
     if flags is not None:
         if flags.numel() != 1 or flags.element_size() != 4:
             raise ValueError("flags must be one 32-bit word")
