@@ -63,6 +63,17 @@ __device__ __forceinline__ int adam_tensor(const AdamArgs& g, int b) {
   return lo;
 }
 
+// sqrt(x) to nearest: the hardware's result (1 ulp) against its neighbours, by
+// the sign of x minus the product of the two values a midpoint lies between.
+// 0, infinity and NaN pass the comparisons unchanged.  Below 2^-100, where the
+// residual loses bits, the result may be 1 ulp off.
+__device__ __forceinline__ float sqrt_rn(float x) {
+  const float s = __builtin_amdgcn_sqrtf(x);
+  const float lo = __uint_as_float(__float_as_uint(s) - 1u), hi = __uint_as_float(__float_as_uint(s) + 1u);
+  float r = __builtin_fmaf(-lo, s, x) <= 0.0f ? lo : s;
+  return __builtin_fmaf(-hi, s, x) > 0.0f ? hi : r;
+}
+
 // One step of four elements: w, m and v are updated, root = sqrt(v).
 __device__ __forceinline__ void adam_quad(const AdamArgs& g, float keep, float scale, f32x4_t grad, f32x4_t& w,
                                           f32x4_t& m, f32x4_t& v, f32x4_t& root) {
@@ -71,7 +82,7 @@ __device__ __forceinline__ void adam_quad(const AdamArgs& g, float keep, float s
     const float gr = grad[i] * scale;
     m[i] = m[i] * g.b1 + gr * g.c1;
     v[i] = v[i] * g.b2 + (gr * gr) * g.c2;
-    root[i] = __builtin_sqrtf(v[i]);
+    root[i] = sqrt_rn(v[i]);
     // the reciprocal's last bit is 2^-23 of the step, not of W
     w[i] = w[i] * keep - (m[i] * __builtin_amdgcn_rcpf(root[i] * g.c + g.eps)) * g.a;
   }
@@ -201,11 +212,71 @@ __global__ __launch_bounds__(256) void k_adamw32(AdamArgs g) {
 constexpr int AD8_RUNS = 2;                    // runs of a wave
 constexpr int AD8_BLOCK = 4 * AD8_RUNS;        // runs of a block
 
-__device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int s = 32; s; s >>= 1) x = fmaxf(x, __shfl_xor(x, s));
-  return x;
+// Largest value of the wave, in every lane.  Within 16 lanes by DPP: the
+// neighbour, the other pair, the mirrored 8, the mirrored 16.
+template <int CTRL>
+__device__ __forceinline__ float dpp_max(float x) {
+  return fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, false)));
 }
+
+__device__ __forceinline__ float row_max(float x) {   // of 16 lanes
+  x = dpp_max<0xB1>(x);    // quad_perm 1 0 3 2
+  x = dpp_max<0x4E>(x);    // quad_perm 2 3 0 1
+  x = dpp_max<0x141>(x);   // row_half_mirror
+  return dpp_max<0x140>(x);   // row_mirror
+}
+
+__device__ __forceinline__ float wave_max(float x) {
+  x = row_max(x);
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+
+// One run of a row; FULL: all its 256 columns are there.
+template <class TG, bool NT, bool FULL>
+struct Adam8Run {
+  f32x4_t grad, w;
+  uint32_t cm, cv;
+  float sm, sv;
+  int64_t at, run;
+  int left;
+
+  __device__ __forceinline__ void load(const AdamTensor& t, int64_t row, int c0, int64_t r, int lane) {
+    const int c = c0 + lane * 4;
+    run = r;
+    left = FULL ? 4 : t.cols - c;
+    at = row * t.cols + c;
+    grad = ld_quad<TG, NT>((const TG*)t.G + row * t.ldg + c, left);
+    w = ld_quad<float, NT>(t.W + at, left);
+    cm = ld_codes((const uint8_t*)t.m + at, left);
+    cv = ld_codes((const uint8_t*)t.v + at, left);
+    sm = t.m_scale[r];
+    sv = t.v_scale[r];
+  }
+
+  __device__ __forceinline__ void step(const AdamArgs& g, const AdamTensor& t, float scale, int lane) {
+    f32x4_t m = e4m3_decode(cm) * sm, root = e4m3_decode(cv) * sv;
+    f32x4_t v = root * root;
+    adam_quad(g, t.keep, scale, grad, w, m, v, root);
+    // lanes behind the row's end hold zeros and do not count
+    if constexpr (!FULL) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i >= left) m[i] = root[i] = 0.0f;
+    }
+    st_quad<float, NT>(t.W + at, w, left);
+    if (t.W16) st_quad<uint16_t, NT>(t.W16 + at, w, left);
+    const float tm = run_top(wave_max(quad_top(m))), tv = run_top(wave_max(quad_top(root)));
+    const float im = (1.0f / tm) * 448.0f, iv = (1.0f / tv) * 448.0f;
+    encode_quad(m, root, im, iv, (uint64_t)at, t.key, cm, cv);
+    st_codes((uint8_t*)t.m + at, cm, left);
+    st_codes((uint8_t*)t.v + at, cv, left);
+    if (lane == 0) {
+      t.m_scale[run] = tm * (1.0f / 448.0f);
+      t.v_scale[run] = tv * (1.0f / 448.0f);
+    }
+  }
+};
 
 template <class TG, bool NT>
 __global__ __launch_bounds__(256) void k_adamw8(AdamArgs g) {
@@ -216,51 +287,26 @@ __global__ __launch_bounds__(256) void k_adamw8(AdamArgs g) {
   const int per_row = (t.cols + kRun - 1) / kRun;
   const int64_t runs = (int64_t)t.rows * per_row;
   const int64_t r0 = (int64_t)((int)blockIdx.x - t.block0) * AD8_BLOCK + wave_id() * AD8_RUNS;
-  uint8_t* const M = (uint8_t*)t.m;
-  uint8_t* const V = (uint8_t*)t.v;
-  f32x4_t gr[AD8_RUNS], w[AD8_RUNS];
-  uint32_t cm[AD8_RUNS], cv[AD8_RUNS];
-  float sm[AD8_RUNS], sv[AD8_RUNS];
-  int64_t at[AD8_RUNS];
-  int lf[AD8_RUNS];
+  if (r0 >= runs) return;
+  int64_t row = runs >> 31 ? r0 / per_row : (int64_t)((uint32_t)r0 / (uint32_t)per_row);
+  int b = (int)(r0 - row * per_row);
+  if (t.cols % kRun == 0 && r0 + AD8_RUNS <= runs) {
+    Adam8Run<TG, NT, true> f[AD8_RUNS];
 #pragma unroll
-  for (int q = 0; q < AD8_RUNS; ++q) {
-    const int64_t run = r0 + q;
-    if (run < runs) {
-      const int64_t row = run / per_row;
-      const int c = (int)(run - row * per_row) * kRun + lane * 4;
-      lf[q] = t.cols - c;
-      at[q] = row * t.cols + c;
-      gr[q] = ld_quad<TG, NT>((const TG*)t.G + row * t.ldg + c, lf[q]);
-      w[q] = ld_quad<float, NT>(t.W + at[q], lf[q]);
-      cm[q] = ld_codes(M + at[q], lf[q]);
-      cv[q] = ld_codes(V + at[q], lf[q]);
-      sm[q] = t.m_scale[run];
-      sv[q] = t.v_scale[run];
+    for (int q = 0; q < AD8_RUNS; ++q) {
+      f[q].load(t, row, b * kRun, r0 + q, lane);
+      if (++b == per_row) b = 0, ++row;
     }
+#pragma unroll
+    for (int q = 0; q < AD8_RUNS; ++q) f[q].step(g, t, scale, lane);
+    return;
   }
-#pragma unroll
-  for (int q = 0; q < AD8_RUNS; ++q) {
-    const int64_t run = r0 + q;
-    if (run >= runs) break;
-    f32x4_t m = e4m3_decode(cm[q]) * sm[q], root = e4m3_decode(cv[q]) * sv[q];
-    f32x4_t v = root * root;
-    adam_quad(g, t.keep, scale, gr[q], w[q], m, v, root);
-    // lanes behind the row's end hold zeros and do not count
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i >= lf[q]) m[i] = root[i] = 0.0f;
-    const float tm = run_top(wave_max(quad_top(m))), tv = run_top(wave_max(quad_top(root)));
-    const float im = (1.0f / tm) * 448.0f, iv = (1.0f / tv) * 448.0f;
-    encode_quad(m, root, im, iv, (uint64_t)at[q], t.key, cm[q], cv[q]);
-    st_quad<float, NT>(t.W + at[q], w[q], lf[q]);
-    if (t.W16) st_quad<uint16_t, NT>(t.W16 + at[q], w[q], lf[q]);
-    st_codes(M + at[q], cm[q], lf[q]);
-    st_codes(V + at[q], cv[q], lf[q]);
-    if (lane == 0) {
-      t.m_scale[run] = tm * (1.0f / 448.0f);
-      t.v_scale[run] = tv * (1.0f / 448.0f);
-    }
+#pragma unroll 1
+  for (int q = 0; q < AD8_RUNS && r0 + q < runs; ++q) {
+    Adam8Run<TG, NT, false> f;
+    f.load(t, row, b * kRun, r0 + q, lane);
+    f.step(g, t, scale, lane);
+    if (++b == per_row) b = 0, ++row;
   }
 }
 
@@ -419,13 +465,8 @@ __global__ __launch_bounds__(ADF_WAVES * 64) void k_adamw_factors(AdamArgs g) {
   if constexpr (BITS == 8) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-#pragma unroll
-      for (int s = 1; s < 16; s <<= 1) {   // a row's run lies in 16 lanes
-        tm[k] = fmaxf(tm[k], __shfl_xor(tm[k], s));
-        tv[k] = fmaxf(tv[k], __shfl_xor(tv[k], s));
-      }
-      tm[k] = run_top(tm[k]);
-      tv[k] = run_top(tv[k]);
+      tm[k] = run_top(row_max(tm[k]));   // a row's run lies in 16 lanes
+      tv[k] = run_top(row_max(tv[k]));
       const float im = (1.0f / tm[k]) * 448.0f, iv = (1.0f / tv[k]) * 448.0f;
       const int row = row0 + 4 * k + q;
 #pragma unroll
