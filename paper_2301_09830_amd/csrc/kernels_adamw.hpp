@@ -333,20 +333,16 @@ struct AdamPiece {   // 4 rows x 4 columns of a lane, 4 rows apart
   uint32_t cm[4], cv[4];
 };
 
-template <int BITS, bool NT>
-__global__ __launch_bounds__(ADF_WAVES * 64) void k_adamw_factors(AdamArgs g) {
-  if (g.flags && (*g.flags & 1u)) return;
-  __shared__ f32x4_t qs[kRun * ADF_RANKS / 4];
-  __shared__ f32x4_t turn[ADF_WAVES][16 * 16];
-  const AdamTensor& t = g.t[adam_tensor(g, blockIdx.x)];
+// Rows 128 rb .. and run `run` of a tensor.  FULL: all of them are there.
+template <int BITS, bool NT, bool FULL>
+__device__ __forceinline__ void adamw_factors(const AdamArgs& g, const AdamTensor& t, int rb, int run, int per_row,
+                                              f32x4_t* qs, f32x4_t (*turn)[16 * 16]) {
   const float scale = g.grad_scale ? *g.grad_scale : 1.0f;
   const int wave = wave_id(), lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
-  const int per_row = (t.cols + kRun - 1) / kRun;
-  const int b = (int)blockIdx.x - t.block0;
-  const int rb = b / per_row, run = b - rb * per_row;
   const int row0 = rb * ADF_ROWS + wave * 16;
   const int c0 = run * kRun;
-  const int cols_left = t.cols - c0;
+  const int cols_left = FULL ? kRun : t.cols - c0;
+  auto left_of = [&](int row, int j) { return FULL ? 4 : row < t.rows ? cols_left - 64 * j - 4 * i : 0; };
 
   // rows row0 + 4 k + q, columns c0 + 64 j + 4 i of piece j
   AdamPiece<BITS> now, next;
@@ -355,7 +351,7 @@ __global__ __launch_bounds__(ADF_WAVES * 64) void k_adamw_factors(AdamArgs g) {
     for (int k = 0; k < 4; ++k) {
       const int row = row0 + 4 * k + q;
       const int64_t e = (int64_t)row * t.cols + c0 + 64 * j + 4 * i;
-      const int left = row < t.rows ? cols_left - 64 * j - 4 * i : 0;
+      const int left = left_of(row, j);
       p.w[k] = ld_quad<float, NT>(t.W + e, left);
       if constexpr (BITS == 32) {
         p.m[k] = ld_quad<float, NT>((const float*)t.m + e, left);
@@ -434,7 +430,7 @@ __global__ __launch_bounds__(ADF_WAVES * 64) void k_adamw_factors(AdamArgs g) {
     for (int k = 0; k < 4; ++k) {
       const int row = row0 + 4 * k + q;
       const int64_t e = (int64_t)row * t.cols + c0 + 64 * j + 4 * i;
-      const int left = row < t.rows ? cols_left - 64 * j - 4 * i : 0;
+      const int left = left_of(row, j);
       f32x4_t m, v, root;
       if constexpr (BITS == 32) {
         m = now.m[k];
@@ -451,9 +447,11 @@ __global__ __launch_bounds__(ADF_WAVES * 64) void k_adamw_factors(AdamArgs g) {
         st_quad<float, NT>((float*)t.m + e, m, left);
         st_quad<float, NT>((float*)t.v + e, v, left);
       } else {
+        if constexpr (!FULL) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-          if (c >= left) m[c] = root[c] = 0.0f;
+          for (int c = 0; c < 4; ++c)
+            if (c >= left) m[c] = root[c] = 0.0f;
+        }
         tm[k] = fmaxf(tm[k], quad_top(m));
         tv[k] = fmaxf(tv[k], quad_top(root));
         ms[j][k] = m;
@@ -473,19 +471,34 @@ __global__ __launch_bounds__(ADF_WAVES * 64) void k_adamw_factors(AdamArgs g) {
       for (int j = 0; j < 4; ++j) {
         if (64 * j >= cols_left) continue;
         const int64_t e = (int64_t)row * t.cols + c0 + 64 * j + 4 * i;
-        const int left = row < t.rows ? cols_left - 64 * j - 4 * i : 0;
+        const int left = left_of(row, j);
         uint32_t cm, cv;
         encode_quad(ms[j][k], roots[j][k], im, iv, (uint64_t)e, t.key, cm, cv);
         st_codes((uint8_t*)t.m + e, cm, left);
         st_codes((uint8_t*)t.v + e, cv, left);
       }
-      if (i == 0 && row < t.rows) {
+      if (i == 0 && (FULL || row < t.rows)) {
         const int64_t sr = (int64_t)row * per_row + run;
         t.m_scale[sr] = tm[k] * (1.0f / 448.0f);
         t.v_scale[sr] = tv[k] * (1.0f / 448.0f);
       }
     }
   }
+}
+
+template <int BITS, bool NT>
+__global__ __launch_bounds__(ADF_WAVES * 64) void k_adamw_factors(AdamArgs g) {
+  if (g.flags && (*g.flags & 1u)) return;
+  __shared__ f32x4_t qs[kRun * ADF_RANKS / 4];
+  __shared__ f32x4_t turn[ADF_WAVES][16 * 16];
+  const AdamTensor& t = g.t[adam_tensor(g, blockIdx.x)];
+  const int per_row = (t.cols + kRun - 1) / kRun;
+  const int b = (int)blockIdx.x - t.block0;
+  const int rb = b / per_row, run = b - rb * per_row;
+  if ((rb + 1) * ADF_ROWS <= t.rows && (run + 1) * kRun <= t.cols)
+    adamw_factors<BITS, NT, true>(g, t, rb, run, per_row, qs, turn);
+  else
+    adamw_factors<BITS, NT, false>(g, t, rb, run, per_row, qs, turn);
 }
 
 }  // namespace occ
