@@ -309,7 +309,10 @@ typedef enum {
  * X is tokens x in, Y and R tokens x out.  bias (fp32), R and Z may be NULL;
  * R may be Y (the residual is replaced in place).  Z is what the backward pass
  * needs: leave it out when serving.  tokens may be 0 (nothing is done).
- * in and out at most 2^24. */
+ * in and out at most 2^24.
+ * fp32 products of some size run on the bf16 matrix units, each operand as the
+ * sum of three bf16 values: a product is then off by at most 2^-25 of itself
+ * before it is added in fp32.  A non-finite input makes its row NaN there. */
 typedef struct {
   int32_t dtype; /* occ_dtype_t */
   int32_t act;   /* occ_act_t */

@@ -261,8 +261,31 @@ struct GemmArgs {
   void* C;            // EP_STORE: the result
   int64_t ldc;
   int32_t c_f32, accumulate, stream;
+  int64_t plane_a, plane_b;   // fp32 as three bf16 planes: bytes from one to the next
+  int32_t seg_tiles;          // K tiles of one pair of planes
   FwdEpi fwd;
 };
+
+// fp32 operands on the bf16 matrix units: x = h + m + l, each the bf16 nearest
+// to what the ones before leave, holds x to 2^-27 of itself, and six of the
+// nine products of two such sums hold the product to 2^-25 (those left out are
+// m l, l m and l l), less than its rounding to fp32.  The product runs over K
+// once for each pair, the small ones first.
+constexpr int kPlanes = 3, kPairs = 6;
+
+// plane of pair p: A takes l h m m h h, B takes h l m h m h
+__device__ __forceinline__ int plane_of_a(int p) { return (0x052 >> (2 * p)) & 3; }
+__device__ __forceinline__ int plane_of_b(int p) { return (0x118 >> (2 * p)) & 3; }
+
+// An infinity ends as NaN; a finite value that bf16 would round to infinity
+// keeps the largest bf16 as its first part.
+__device__ __forceinline__ void split3(float x, uint16_t* p) {
+  p[0] = bf16_rne(x);
+  if ((p[0] & 0x7fff) == 0x7f80) p[0] -= 1;
+  const float r = x - __uint_as_float((uint32_t)p[0] << 16);
+  p[1] = bf16_rne(r);
+  p[2] = bf16_rne(r - __uint_as_float((uint32_t)p[1] << 16));
+}
 
 enum { EP_STORE = 0, EP_FWD = 1, EP_GATED = 2 };
 
@@ -302,7 +325,7 @@ struct Operand {
   static constexpr int KROW = R * ES;                // bytes of a row, K strided
   uint32_t voff[NI];
   int kk[KS ? NI : 1];   // first K of the lane's piece
-  uintptr_t base;
+  uintptr_t base, start;   // of the present tile, and of K = 0
   int64_t step;
 
   // Exchange of 16-byte pieces within row k of a K-strided tile.  A read
@@ -328,7 +351,8 @@ struct Operand {
         const int r = (wave * NI + j) * 8 + (lane >> 3);
         voff[j] = (uint32_t)(row_of(r) - row_of(wave * NI * 8)) * (uint32_t)(ld * ES) + ch * 16;
       }
-      base = (uintptr_t)p + ((uintptr_t)row_of(wave * NI * 8) * ld + k0) * ES;
+      start = (uintptr_t)p + (uintptr_t)row_of(wave * NI * 8) * ld * ES;
+      base = start + k0 * ES;
       step = kRowBytes;
     } else {
       constexpr int PER = 1024 / KROW;       // rows of K an instruction covers
@@ -340,7 +364,8 @@ struct Operand {
         kk[j] = k;
         voff[j] = row0 + c < rows ? (uint32_t)(k - wave * NI * PER) * (uint32_t)(ld * ES) + c * ES : kOut;
       }
-      base = (uintptr_t)p + ((uintptr_t)(k0 + wave * NI * PER) * ld + row0) * ES;
+      start = (uintptr_t)p + ((uintptr_t)(wave * NI * PER) * ld + row0) * ES;
+      base = start + (uintptr_t)k0 * ld * ES;
       step = (int64_t)BK * ld * ES;
     }
   }
@@ -559,12 +584,13 @@ using Form256 = Form<2, 4, 8, 4, 2>;
 using Form128 = Form<2, 4, 4, 2, 4>;
 using Form64 = Form<4, 2, 1, 2, 4>;
 
-// Block `block` of a product: all of its tile's K, or one part of it.
-template <class T, class F, bool AKS, bool BKS, int EP>
+// Block `block` of a product: all of its tile's K, or one part of it.  T: type
+// of the operands, TE: of the layer (fp32 on bf16 planes: T bf16, TE fp32).
+template <class T, class TE, class F, bool AKS, bool BKS, int EP>
 __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_char* lds) {
   constexpr int ES = sizeof(T), S = F::S, NW = F::NW, WM = F::WM, WN = F::WN, FA = F::FA, FB = F::FB;
   constexpr int BM = F::BM, BN = F::BN;
-  constexpr bool PP = S == 2;
+  constexpr bool PP = S == 2, SEG = sizeof(T) != sizeof(TE);
   using OA = Operand<BM, AKS, ES, NW>;
   using OB = Operand<BN, BKS, ES, NW>;
   constexpr int STAGE = OA::BYTES + OB::BYTES;
@@ -583,10 +609,16 @@ __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_cha
   constexpr int BNC = EP == EP_GATED ? BN / 2 : BN;   // columns of the result
   const int n0 = tn * BNC;
 
+  // planes: the pair that the first tile belongs to, and the tile in it
+  int pair_a = SEG ? kt0 / g.seg_tiles : 0, pair_b = pair_a;
+  int in_a = SEG ? kt0 - pair_a * g.seg_tiles : kt0, in_b = in_a;
+  const char* const A = (const char*)g.A;
+  const char* const B = (const char*)g.B;
   OA oa;
   OB ob;
-  oa.init(g.A, g.lda, g.M, m0, wave, lane, (int64_t)kt0 * BK, [&](int r) { return min(m0 + r, g.M - 1); });
-  ob.init(g.B, g.ldb, g.N, n0, wave, lane, (int64_t)kt0 * BK, [&](int r) {
+  oa.init(SEG ? A + plane_of_a(pair_a) * g.plane_a : A, g.lda, g.M, m0, wave, lane, (int64_t)in_a * BK,
+          [&](int r) { return min(m0 + r, g.M - 1); });
+  ob.init(SEG ? B + plane_of_b(pair_b) * g.plane_b : B, g.ldb, g.N, n0, wave, lane, (int64_t)in_b * BK, [&](int r) {
     if constexpr (EP == EP_GATED) {
       // each wave's columns: half of them the gate's, then the same of the other projection
       constexpr int TN = FB * 16;
@@ -596,6 +628,10 @@ __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_cha
       return min(n0 + r, g.N - 1);
     }
   });
+  if constexpr (SEG) {   // plane 0
+    oa.start -= plane_of_a(pair_a) * g.plane_a;
+    ob.start -= plane_of_b(pair_b) * g.plane_b;
+  }
   Reader<FA * 16, AKS, ES> ra;
   Reader<FB * 16, BKS, ES> rb;
   ra.template init<OA::KROW>(wm * FA * 16, lane);
@@ -607,9 +643,25 @@ __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_cha
 #pragma unroll
     for (int b = 0; b < FB; ++b) acc[a][b] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 
-  int left_a = g.ka - kt0 * BK, left_b = g.kb - kt0 * BK;   // of K, at the next tile to load
-  auto load_a = [&](int stage) { oa.load(lds0 + stage * STAGE, wave, left_a); left_a -= BK; };
-  auto load_b = [&](int stage) { ob.load(lds0 + stage * STAGE + OA::BYTES, wave, left_b); left_b -= BK; };
+  int left_a = g.ka - in_a * BK, left_b = g.kb - in_b * BK;   // of K, at the next tile to load
+  auto load_a = [&](int stage) {
+    oa.load(lds0 + stage * STAGE, wave, left_a);
+    left_a -= BK;
+    if (SEG && ++in_a == g.seg_tiles) {
+      in_a = 0;
+      oa.base = oa.start + plane_of_a(++pair_a) * g.plane_a;
+      left_a = g.ka;
+    }
+  };
+  auto load_b = [&](int stage) {
+    ob.load(lds0 + stage * STAGE + OA::BYTES, wave, left_b);
+    left_b -= BK;
+    if (SEG && ++in_b == g.seg_tiles) {
+      in_b = 0;
+      ob.base = ob.start + plane_of_b(++pair_b) * g.plane_b;
+      left_b = g.kb;
+    }
+  };
 
   if constexpr (PP) {
     constexpr int HA = FA / 2, HB = FB / 2, Q1 = HA / 4, Q2 = HA / 2;
@@ -788,35 +840,35 @@ __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_cha
         }
       } else if (whole) {
         if constexpr (EP == EP_STORE) {
-          if (sizeof(T) == 4 || g.c_f32) store_rows<float, RUN, RPI, false>(g, m, n, z);
+          if (sizeof(TE) == 4 || g.c_f32) store_rows<float, RUN, RPI, false>(g, m, n, z);
           else store_rows<uint16_t, RUN, RPI, false>(g, m, n, z);
         } else {
-          fwd_rows<T, EP == EP_GATED, RUN, RPI, false>(g.fwd, g.M, m, n, z, u);
+          fwd_rows<TE, EP == EP_GATED, RUN, RPI, false>(g.fwd, g.M, m, n, z, u);
         }
       } else if (left >= 4) {
         if constexpr (EP == EP_STORE) {
-          if (sizeof(T) == 4 || g.c_f32) store_rows<float, RUN, RPI, true>(g, m, n, z);
+          if (sizeof(TE) == 4 || g.c_f32) store_rows<float, RUN, RPI, true>(g, m, n, z);
           else store_rows<uint16_t, RUN, RPI, true>(g, m, n, z);
         } else {
-          fwd_rows<T, EP == EP_GATED, RUN, RPI, true>(g.fwd, g.M, m, n, z, u);
+          fwd_rows<TE, EP == EP_GATED, RUN, RPI, true>(g.fwd, g.M, m, n, z, u);
         }
       } else if (left > 0) {   // the lanes of the last one to three columns
 #pragma unroll 1
         for (int r = 0; r < RUN; ++r) {
           const int64_t mr = m + r * RPI;
           if (mr >= g.M) continue;
-          if constexpr (EP == EP_STORE) store_result<T>(g, mr, n, z[r], left);
-          else fwd_epilogue<T, EP == EP_GATED>(g.fwd, mr, n, z[r], u[r], residual_quad<T>(g.fwd, mr, n, left));
+          if constexpr (EP == EP_STORE) store_result<TE>(g, mr, n, z[r], left);
+          else fwd_epilogue<TE, EP == EP_GATED>(g.fwd, mr, n, z[r], u[r], residual_quad<TE>(g.fwd, mr, n, left));
         }
       }
     }
   }
 }
 
-template <class T, class F, int EP>
+template <class T, class TE, class F, int EP>
 __global__ __launch_bounds__(F::NW * 64, 2) void k_gemm(GemmArgs g) {
   __shared__ __attribute__((aligned(1024))) char sm[F::LDS];
-  gemm_block<T, F, false, false, EP>(g, blockIdx.x, (lds_char*)sm);
+  gemm_block<T, TE, F, false, false, EP>(g, blockIdx.x, (lds_char*)sm);
 }
 
 // Sum of the partial products of a split K, in split order, and the epilogue.

@@ -255,7 +255,26 @@ struct DzArgs {
   int64_t ldy, ldz, ldd;
   int32_t tokens, out, act, strip;   // strip: rows of a block
   int32_t across;                    // blocks along a row
+  int64_t plane;                     // fp32: dZ as three bf16 planes this far apart (elements); else 0
 };
+
+// Four elements as three bf16 planes, the first `left` of them inside the row.
+__device__ __forceinline__ void st_planes(uint16_t* p, int64_t plane, f32x4_t v, int left) {
+  uint16_t e[4][kPlanes];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) split3(v[i], e[i]);
+#pragma unroll
+  for (int k = 0; k < kPlanes; ++k) {
+    uint16_t* const q = p + k * plane;
+    if (left >= 4) {
+      *(u2h_t*)q = u2h_t{e[0][k] | (uint32_t)e[1][k] << 16, e[2][k] | (uint32_t)e[3][k] << 16};
+    } else {
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+        if (i < left) q[i] = e[i][k];
+    }
+  }
+}
 
 constexpr int DZ_LANES = 32;   // threads along a row, 4 columns each
 constexpr int DZ_ROWS = 8;     // rows at a time
@@ -286,7 +305,15 @@ __device__ __forceinline__ void dz_block(const DzArgs& g, int block) {
           d0 = dy * da;
         }
       }
-      if (g.dZ) {
+      if (sizeof(T) == 4 && g.plane) {
+        uint16_t* const o = (uint16_t*)g.dZ + m * g.ldd + n;
+        st_planes(o, g.plane, d0, left);
+        if constexpr (GATED) st_planes(o + g.out, g.plane, d1, left);
+        if (left <= 4)
+          for (int k = 0; k < kPlanes; ++k)
+            for (int64_t c = GATED ? 2 * (int64_t)g.out : g.out; c < g.ldd; ++c)
+              ((uint16_t*)g.dZ)[k * g.plane + m * g.ldd + c] = 0;
+      } else if (g.dZ) {
         T* const o = (T*)g.dZ + m * g.ldd + n;
         st_quad(o, d0, left);
         if constexpr (GATED) st_quad(o + g.out, d1, left);
@@ -318,6 +345,7 @@ struct CopyArgs {
   void* dst;
   int64_t ld, rows;
   int32_t cols, pieces, blocks;
+  int64_t plane;   // fp32: as three bf16 planes this far apart (elements); else 0
 };
 
 template <class T>
@@ -326,6 +354,14 @@ __device__ __forceinline__ void copy_block(const CopyArgs& g, int block) {
   const int64_t total = g.rows * g.pieces;
   for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < total; i += (int64_t)g.blocks * 256) {
     const int64_t r = i / g.pieces;
+    if (sizeof(T) == 4 && g.plane) {
+      const int c = (int)(i - r * g.pieces) * 8;
+      const float* const p = (const float*)g.src + r * g.ld + c;
+      uint16_t* const q = (uint16_t*)g.dst + i * 8;
+      st_planes(q, g.plane, ld_quad<float>(p, g.cols - c), 4);
+      st_planes(q + 4, g.plane, ld_quad<float>(p + 4, g.cols - c - 4), 4);
+      continue;
+    }
     const int c = (int)(i - r * g.pieces) * CH;
     *(f32x4_t*)((T*)g.dst + i * CH) = ld_piece<T>((const T*)g.src + r * g.ld + c, g.cols - c);
   }
@@ -396,13 +432,13 @@ struct BackwardArgs {
   int32_t dx_blocks, dw_blocks;
 };
 
-template <class T, class F>
+template <class T, class TE, class F>
 __global__ __launch_bounds__(F::NW * 64, 2) void k_backward(BackwardArgs g) {
   __shared__ __attribute__((aligned(1024))) char sm[F::LDS];
   int b = blockIdx.x;
-  if (b < g.dx_blocks) return gemm_block<T, F, false, true, EP_STORE>(g.dx, b, (lds_char*)sm);
+  if (b < g.dx_blocks) return gemm_block<T, TE, F, false, true, EP_STORE>(g.dx, b, (lds_char*)sm);
   b -= g.dx_blocks;
-  if (b < g.dw_blocks) return gemm_block<T, F, true, true, EP_STORE>(g.dw, b, (lds_char*)sm);
+  if (b < g.dw_blocks) return gemm_block<T, TE, F, true, true, EP_STORE>(g.dw, b, (lds_char*)sm);
   static_assert(F::NW == 8, "bias_block runs on eight waves");
   bias_block(g.bias, b - g.dw_blocks, (float*)sm);
 }

@@ -88,12 +88,13 @@ struct Product {
 };
 
 // pair: columns come in pairs of rows of W (gated), so a tile makes half as many
-Product make_product(int64_t m, int64_t width, int64_t k, size_t es, Tile tile, int splits, bool pair) {
+// planes: fp32 operands as bf16 planes, K once for each pair of them
+Product make_product(int64_t m, int64_t width, int64_t k, size_t es, Tile tile, int splits, bool pair, bool planes) {
   Product p;
   const TileTimes& t = kTiles[tile];
   p.tiles_m = div_up(m, t.side);
   p.tiles_n = pair ? div_up(width / 2, t.side / 2) : div_up(width, t.side);
-  p.tiles_k = div_up(k, kRowBytes / (int64_t)es);
+  p.tiles_k = div_up(k, kRowBytes / (int64_t)es) * (planes ? kPairs : 1);
   p.k_per_split = (int)div_up(p.tiles_k, splits);
   p.splits = (int)div_up(p.tiles_k, p.k_per_split);
   p.block_us = (double)p.k_per_split * (es == 2 ? t.k_bf16 : t.k_f32) + t.fixed;
@@ -137,7 +138,7 @@ double launch_us(const Product& x, const Product& w, int64_t slots, bool halves)
 // Up to two products of one launch, with the same tile.  m, width, k: of each
 // (m = 0: not there).
 ProductPlan plan_products(const int64_t (&m)[2], const int64_t (&width)[2], const int64_t (&k)[2], size_t es,
-                          bool pair) {
+                          bool pair, bool planes = false) {
   ProductPlan best;
   double best_us = INFINITY;
   for (int t = 0; t < TILE_NUM; ++t) {
@@ -151,7 +152,7 @@ ProductPlan plan_products(const int64_t (&m)[2], const int64_t (&width)[2], cons
         continue;
       }
       for (const int s : kSplitCounts) {
-        const Product p = make_product(m[i], width[i], k[i], es, (Tile)t, s, pair);
+        const Product p = make_product(m[i], width[i], k[i], es, (Tile)t, s, pair, planes);
         if (p.splits != s || (s > 1 && p.k_per_split < 4) || !product_fits(p)) break;
         of[i][n[i]++] = p;
         if (p.blocks() > 2 * slots) break;   // parts of K would only add work
@@ -196,6 +197,9 @@ bool rows_on_lines(const void* p, int64_t ld, int64_t cols, size_t es) {
   return !p || (aligned(p, 64) && (size_t)ld * es % 64 == 0 && (size_t)cols * es % 64 == 0);
 }
 
+// us to write an operand as planes: 4 bytes of each element are read, 6 written
+double planes_us(double elements) { return elements * 10.0 / 4e6; }
+
 unsigned join_blocks(const GemmArgs& g) {
   return (unsigned)std::min<int64_t>(div_up((int64_t)g.M * div_up(g.N, 4), 256), 4096);
 }
@@ -209,14 +213,16 @@ bool needs_copy(const void* p, int64_t ld, int64_t cols, size_t es) {
 int64_t piece_ld(int64_t cols, size_t es) { return up(cols, 16 / (int64_t)es); }
 
 template <class T>
-CopyArgs copy_operand(const void* src, int64_t ld, int64_t rows, int64_t cols, char* dst) {
+CopyArgs copy_operand(const void* src, int64_t ld, int64_t rows, int64_t cols, char* dst, bool planes) {
   CopyArgs c{};
   c.src = src;
   c.dst = dst;
   c.ld = ld;
   c.rows = rows;
   c.cols = (int32_t)cols;
-  c.pieces = (int32_t)(piece_ld(cols, sizeof(T)) * (int64_t)sizeof(T) / 16);
+  const size_t es = planes ? 2 : sizeof(T);
+  c.pieces = (int32_t)(piece_ld(cols, es) * (int64_t)es / 16);
+  c.plane = planes ? rows * piece_ld(cols, es) : 0;
   c.blocks = (int32_t)std::min<int64_t>(div_up(rows * c.pieces, 256), 8192);
   return c;
 }
@@ -256,6 +262,7 @@ double copy_us(int64_t rows, int64_t cols, size_t es) { return 3.0 + 2.0 * (doub
 
 struct FwdPlan {
   bool few = false, copy_x = false, copy_w = false;
+  bool planes = false;   // fp32 on the bf16 matrix units
   size_t x_off = 0, w_off = 0, part_off = 0, bytes = 0;
   ProductPlan prod;
 };
@@ -287,8 +294,16 @@ occ_status_t plan_fwd(const occ_linear_t& l, bool gated, FwdPlan& f) {
     f.few = few_us(l.tokens, l.in, l.out, es, gated, !f.copy_w) <= tiled;
     if (f.few) return OCC_OK;
   }
+  if (l.dtype == OCC_F32) {
+    const ProductPlan p = plan_products({l.tokens, 0}, {wide, 0}, {l.in, 0}, 2, gated, true);
+    const double copies = f.copy_x || f.copy_w ? copy_us(l.tokens * f.copy_x + wide * f.copy_w, l.in, es) : 0.0;
+    if (p.fits && p.us + 3.0 + planes_us((double)(l.tokens + wide) * (double)l.in) < f.prod.us + copies) {
+      f.prod = p;
+      f.planes = f.copy_x = f.copy_w = true;
+    }
+  }
   Carve c;
-  const size_t row = (size_t)piece_ld(l.in, es) * es;
+  const size_t row = f.planes ? (size_t)piece_ld(l.in, 2) * 2 * kPlanes : (size_t)piece_ld(l.in, es) * es;
   if (f.copy_x) f.x_off = c.take((size_t)l.tokens * row);
   if (f.copy_w) f.w_off = c.take((size_t)wide * row);
   if (f.prod.x.splits > 1) f.part_off = c.take(f.prod.x.part_bytes);
@@ -343,31 +358,43 @@ occ_status_t run_fwd(const occ_linear_t& l, const FwdPlan& f, char* ws, hipStrea
   g.B = l.W;
   g.ldb = l.ldw;
   PrepArgs prep{};
+  const int64_t ldp = piece_ld(l.in, f.planes ? 2 : sizeof(T));
   if (f.copy_x) {
-    prep.copy[0] = copy_operand<T>(l.X, l.ldx, l.tokens, l.in, ws + f.x_off);
+    prep.copy[0] = copy_operand<T>(l.X, l.ldx, l.tokens, l.in, ws + f.x_off, f.planes);
     g.A = ws + f.x_off;
-    g.lda = piece_ld(l.in, sizeof(T));
+    g.lda = ldp;
+    g.plane_a = prep.copy[0].plane * 2;
   }
   if (f.copy_w) {
-    prep.copy[1] = copy_operand<T>(l.W, l.ldw, wide, l.in, ws + f.w_off);
+    prep.copy[1] = copy_operand<T>(l.W, l.ldw, wide, l.in, ws + f.w_off, f.planes);
     g.B = ws + f.w_off;
-    g.ldb = piece_ld(l.in, sizeof(T));
+    g.ldb = ldp;
+    g.plane_b = prep.copy[1].plane * 2;
   }
   OCC_TRY((run_prep<T, GATED>(prep, s)));
   g.M = (int32_t)l.tokens;
   g.N = (int32_t)l.out;
-  g.ka = g.kb = (int32_t)piece_ld(l.in, sizeof(T));
+  g.ka = g.kb = (int32_t)ldp;
   g.fwd = e;
   set_tiles(g, f.prod.x, ws + f.part_off);
   constexpr int EP = GATED ? EP_GATED : EP_FWD;
   const dim3 grid((unsigned)f.prod.x.blocks()), block(512);
-  OCC_TRY(launch(GATED ? "gated_fwd" : "linear_fwd", s, [&] {
-    switch (f.prod.tile) {
-      case TILE_256: hipLaunchKernelGGL((k_gemm<T, Form256, EP>), grid, block, 0, s, g); break;
-      case TILE_128: hipLaunchKernelGGL((k_gemm<T, Form128, EP>), grid, block, 0, s, g); break;
-      default: hipLaunchKernelGGL((k_gemm<T, Form64, EP>), grid, block, 0, s, g); break;
-    }
-  }));
+  auto product = [&](auto operand) {
+    using TI = decltype(operand);
+    return launch(GATED ? "gated_fwd" : "linear_fwd", s, [&] {
+      switch (f.prod.tile) {
+        case TILE_256: hipLaunchKernelGGL((k_gemm<TI, T, Form256, EP>), grid, block, 0, s, g); break;
+        case TILE_128: hipLaunchKernelGGL((k_gemm<TI, T, Form128, EP>), grid, block, 0, s, g); break;
+        default: hipLaunchKernelGGL((k_gemm<TI, T, Form64, EP>), grid, block, 0, s, g); break;
+      }
+    });
+  };
+  if (f.planes) {
+    g.seg_tiles = (int32_t)(f.prod.x.tiles_k / kPairs);
+    OCC_TRY(product(uint16_t{}));
+  } else {
+    OCC_TRY(product(T{}));
+  }
   if (g.splits == 1) return OCC_OK;
   return launch("layer_join", s, [&] {
     hipLaunchKernelGGL((k_gemm_join<T, EP>), dim3(join_blocks(g)), dim3(256), 0, s, g);
@@ -411,6 +438,7 @@ occ_status_t forward(const occ_linear_t* lp, void* ws, size_t ws_bytes, occ_stre
 // ----------------------------------------------------------------------------
 struct BwdPlan {
   bool has_dz = false;    // dZ is made (else it is dY)
+  bool planes = false;    // fp32 on the bf16 matrix units
   bool copy_dy = false, copy_x = false, copy_w = false;
   int64_t strip = 0, strips = 0;
   size_t dz_off = 0, bias_off = 0, x_off = 0, w_off = 0, dx_part = 0, dw_part = 0, bytes = 0;
@@ -441,14 +469,33 @@ occ_status_t plan_bwd(const occ_linear_grad_t& l, bool gated, BwdPlan& f) {
   const bool prod = l.dX || l.dW;
   const bool act = gated || l.act != OCC_ACT_NONE;
   f.has_dz = act && prod;
-  f.ldd = piece_ld(wide, es);
-  Carve c;
-  if (f.has_dz) {
-    f.dz_off = c.take((size_t)l.tokens * f.ldd * es);
-  } else if (prod && needs_copy(l.dY, l.lddy, l.out, es)) {
-    f.copy_dy = true;
-    f.dz_off = c.take((size_t)l.tokens * f.ldd * es);
+  if (prod) {
+    f.copy_dy = !act && needs_copy(l.dY, l.lddy, l.out, es);
+    f.copy_w = l.dX && needs_copy(l.W, l.ldw, l.in, es);
+    f.copy_x = l.dW && needs_copy(l.X, l.ldx, l.in, es);
+    const int64_t m[2] = {l.dX ? l.tokens : 0, l.dW ? wide : 0}, width[2] = {l.in, l.in}, k[2] = {wide, l.tokens};
+    f.prod = plan_products(m, width, k, es, false);
+    if (l.dtype == OCC_F32) {
+      const ProductPlan p = plan_products(m, width, k, 2, false, true);
+      const double x = l.dW ? (double)l.tokens * (double)l.in : 0.0, w = l.dX ? (double)wide * (double)l.in : 0.0;
+      const double dz = (double)l.tokens * (double)wide;
+      const double copied = (f.copy_x ? x : 0.0) + (f.copy_w ? w : 0.0) + (f.copy_dy ? dz : 0.0);
+      const double copies = copied > 0.0 && !act ? copy_us(1, (int64_t)copied, es) : copied * 8.0 / 6e6;
+      // dZ itself is written in either form
+      if (p.fits && p.us + 3.0 + planes_us(x + w + (act ? 0.2 : 1.0) * dz) < f.prod.us + copies) {
+        f.prod = p;
+        f.planes = true;
+        f.copy_x = l.dW;
+        f.copy_w = l.dX;
+        f.copy_dy = !act;
+      }
+    }
+    if (!f.prod.fits) return OCC_E_SHAPE;
   }
+  const size_t os = f.planes ? 2 : es, np = f.planes ? kPlanes : 1;   // of operands in the workspace
+  f.ldd = piece_ld(wide, os);
+  Carve c;
+  if (f.has_dz || f.copy_dy) f.dz_off = c.take((size_t)l.tokens * f.ldd * os * np);
   if (f.has_dz || l.dbias) {
     // enough blocks to fill the chip several times, whole groups of rows in
     // each; fewer, longer strips where their sums have to be added
@@ -459,20 +506,10 @@ occ_status_t plan_bwd(const occ_linear_grad_t& l, bool gated, BwdPlan& f) {
     if (across * f.strips >= ((int64_t)1 << 30)) return OCC_E_SHAPE;
     if (l.dbias) f.bias_off = c.take((size_t)f.strips * wide * 4);
   }
-  if (l.dX) {
-    f.copy_w = needs_copy(l.W, l.ldw, l.in, es);
-    if (f.copy_w) f.w_off = c.take((size_t)wide * piece_ld(l.in, es) * es);
-  }
-  if (l.dW) {
-    f.copy_x = needs_copy(l.X, l.ldx, l.in, es);
-    if (f.copy_x) f.x_off = c.take((size_t)l.tokens * piece_ld(l.in, es) * es);
-  }
-  if (prod) {
-    f.prod = plan_products({l.dX ? l.tokens : 0, l.dW ? wide : 0}, {l.in, l.in}, {wide, l.tokens}, es, false);
-    if (!f.prod.fits) return OCC_E_SHAPE;
-    if (f.prod.x.splits > 1) f.dx_part = c.take(f.prod.x.part_bytes);
-    if (f.prod.w.splits > 1) f.dw_part = c.take(f.prod.w.part_bytes);
-  }
+  if (f.copy_w) f.w_off = c.take((size_t)wide * piece_ld(l.in, os) * os * np);
+  if (f.copy_x) f.x_off = c.take((size_t)l.tokens * piece_ld(l.in, os) * os * np);
+  if (f.prod.x.splits > 1) f.dx_part = c.take(f.prod.x.part_bytes);
+  if (f.prod.w.splits > 1) f.dw_part = c.take(f.prod.w.part_bytes);
   f.bytes = c.total();
   return OCC_OK;
 }
@@ -496,6 +533,7 @@ occ_status_t run_bwd(const occ_linear_grad_t& l, const BwdPlan& f, bool accumula
     d.act = l.act;
     d.strip = (int32_t)f.strip;
     d.across = (int32_t)div_up(l.out, DZ_LANES * 4);
+    d.plane = f.planes && f.has_dz ? l.tokens * f.ldd : 0;
     prep.dz_blocks = (int32_t)(d.across * f.strips);
   }
   const void* dz = l.dY;
@@ -506,24 +544,29 @@ occ_status_t run_bwd(const occ_linear_grad_t& l, const BwdPlan& f, bool accumula
   }
   CopyArgs copies[3] = {};
   int nc = 0;
-  if (f.copy_dy) copies[nc++] = copy_operand<T>(l.dY, l.lddy, l.tokens, l.out, ws + f.dz_off);
-  if (f.copy_w) copies[nc++] = copy_operand<T>(l.W, l.ldw, wide, l.in, ws + f.w_off);
-  if (f.copy_x) copies[nc++] = copy_operand<T>(l.X, l.ldx, l.tokens, l.in, ws + f.x_off);
+  if (f.copy_dy) copies[nc++] = copy_operand<T>(l.dY, l.lddy, l.tokens, l.out, ws + f.dz_off, f.planes);
+  if (f.copy_w) copies[nc++] = copy_operand<T>(l.W, l.ldw, wide, l.in, ws + f.w_off, f.planes);
+  if (f.copy_x) copies[nc++] = copy_operand<T>(l.X, l.ldx, l.tokens, l.in, ws + f.x_off, f.planes);
   for (int i = 0; i < 3; ++i) prep.copy[i] = copies[i];
   OCC_TRY((run_prep<T, GATED>(prep, s)));
 
   const double bytes = (double)sizeof(T) * ((double)l.tokens * (double)(2 * l.in + wide) + 2.0 * (double)wide * (double)l.in);
   const bool stream = bytes > kStreamBytes;
   BackwardArgs a{};
+  const int64_t ldp = piece_ld(l.in, f.planes ? 2 : sizeof(T));
+  const int64_t dz_plane = f.planes ? l.tokens * f.ldd * 2 : 0;
   if (l.dX) {
     GemmArgs& g = a.dx;
     g.A = dz;
     g.lda = ldd;
     g.B = f.copy_w ? ws + f.w_off : l.W;
-    g.ldb = f.copy_w ? piece_ld(l.in, sizeof(T)) : l.ldw;
+    g.ldb = f.copy_w ? ldp : l.ldw;
+    g.plane_a = dz_plane;
+    g.plane_b = wide * ldp * 2;
+    g.seg_tiles = (int32_t)(f.prod.x.tiles_k / kPairs);
     g.M = (int32_t)l.tokens;
     g.N = (int32_t)l.in;
-    g.ka = (int32_t)f.ldd;
+    g.ka = (int32_t)(f.has_dz || f.copy_dy ? f.ldd : wide);
     g.kb = (int32_t)wide;
     g.C = l.dX;
     g.ldc = l.lddx;
@@ -536,7 +579,10 @@ occ_status_t run_bwd(const occ_linear_grad_t& l, const BwdPlan& f, bool accumula
     g.A = dz;
     g.lda = ldd;
     g.B = f.copy_x ? ws + f.x_off : l.X;
-    g.ldb = f.copy_x ? piece_ld(l.in, sizeof(T)) : l.ldx;
+    g.ldb = f.copy_x ? ldp : l.ldx;
+    g.plane_a = dz_plane;
+    g.plane_b = l.tokens * ldp * 2;
+    g.seg_tiles = (int32_t)(f.prod.w.tiles_k / kPairs);
     g.M = (int32_t)wide;
     g.N = (int32_t)l.in;
     g.ka = g.kb = (int32_t)l.tokens;
@@ -563,13 +609,18 @@ occ_status_t run_bwd(const occ_linear_grad_t& l, const BwdPlan& f, bool accumula
       hipLaunchKernelGGL(k_bias, dim3((unsigned)bias_blocks), dim3(512), 0, s, a.bias);
     });
   const dim3 grid((unsigned)blocks), block(512);
-  OCC_TRY(launch("layer_bwd", s, [&] {
-    switch (f.prod.tile) {
-      case TILE_256: hipLaunchKernelGGL((k_backward<T, Form256>), grid, block, 0, s, a); break;
-      case TILE_128: hipLaunchKernelGGL((k_backward<T, Form128>), grid, block, 0, s, a); break;
-      default: hipLaunchKernelGGL((k_backward<T, Form64>), grid, block, 0, s, a); break;
-    }
-  }));
+  auto products = [&](auto operand) {
+    using TI = decltype(operand);
+    return launch("layer_bwd", s, [&] {
+      switch (f.prod.tile) {
+        case TILE_256: hipLaunchKernelGGL((k_backward<TI, T, Form256>), grid, block, 0, s, a); break;
+        case TILE_128: hipLaunchKernelGGL((k_backward<TI, T, Form128>), grid, block, 0, s, a); break;
+        default: hipLaunchKernelGGL((k_backward<TI, T, Form64>), grid, block, 0, s, a); break;
+      }
+    });
+  };
+  if (f.planes) OCC_TRY(products(uint16_t{}));
+  else OCC_TRY(products(T{}));
   const unsigned jx = l.dX && a.dx.splits > 1 ? join_blocks(a.dx) : 0;
   const unsigned jw = l.dW && a.dw.splits > 1 ? join_blocks(a.dw) : 0;
   if (!jx && !jw) return OCC_OK;

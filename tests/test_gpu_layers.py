@@ -369,3 +369,36 @@ def test_on_another_stream_and_in_a_graph():
         work()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, (Y, dX, dW, db)))
+
+
+# fp32 products of some size run on the bf16 matrix units, each operand as
+# three bf16 planes; the bounds stay those of fp32
+PLANES = [(2048, 1030, 3000), (1500, 2304, 2200), (3001, 2047, 1533)]
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("size", PLANES, ids=lambda s: "x".join(map(str, s)))
+def test_fp32_planes(size, gated):
+    t, k, n = size
+    a = optcc.occ_linear_t(optcc.OCC_F32, 0, t, 2304, 2200, 4096, 2304, 4096, 2304, None, None, 0,
+                           None, 0, 4096, 2200)
+    assert optcc.lib().occ_linear_fwd_workspace_bytes(a) > 6 * t * 2304     # planes are made
+    run_forward(t, k, n, "f32", 4 if gated else 2, gated)
+    run_forward(t, k, n, "f32", 0, gated, bias=False, residual=False, pad=3, shift=1)
+    run_backward(t, k, n, "f32", 4 if gated else 2, gated, accumulate=True)
+    if not gated:
+        run_backward(t, k, n, "f32", 0, gated, pad=5, shift=2)
+
+
+def test_fp32_planes_of_the_largest_values():
+    """Values that bf16 would round to infinity, beside ordinary ones; a NaN
+    stays in its row."""
+    g = gen(21)
+    X, W = rand(g, 1500, 2304, torch.float32), rand(g, 2200, 2304, torch.float32, 1e-3)
+    X[7, :40] = 3.4028e38
+    X[9, 100] = float("nan")
+    Y = optcc.occ_linear_fwd(X, W)
+    keep = [i for i in range(1500) if i != 9]
+    y, _, by, _ = forward64(X[keep], W, None, 0, None, False)
+    within(Y[keep], y, by, "Y")
+    assert torch.isnan(Y[9]).all()
