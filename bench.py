@@ -31,6 +31,7 @@ import glob
 import hashlib
 import json
 import os
+import re
 import sys
 import time
 
@@ -57,13 +58,21 @@ def code_lines(text: str) -> str:
 
 
 def kernel_source_digest() -> str:
-    """Digest of the library's code (comments excluded); counter summaries
-    apply only to it."""
-    h = hashlib.sha256()
-    for path in sorted(glob.glob(os.path.join(CSRC, "*.hpp")) + glob.glob(os.path.join(CSRC, "*.hip"))):
+    """Digest of the compressor's code (comments excluded), api.hip and the
+    headers of csrc it takes in; counter summaries apply only to it."""
+    texts, todo = {}, ["api.hip"]
+    while todo:
+        name = todo.pop()
+        path = os.path.join(CSRC, name)
+        if name in texts or not os.path.exists(path):
+            continue
         with open(path, encoding="utf-8") as f:
-            h.update(os.path.basename(path).encode())
-            h.update(code_lines(f.read()).encode())
+            texts[name] = code_lines(f.read())
+        todo += re.findall(r'^#include "([^"]+)"', texts[name], re.M)
+    h = hashlib.sha256()
+    for name in sorted(texts):
+        h.update(name.encode())
+        h.update(texts[name].encode())
     return h.hexdigest()[:16]
 
 
