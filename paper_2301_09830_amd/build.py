@@ -5,7 +5,8 @@
 The library has two translation units: csrc/api.hip (the compressor) and
 csrc/stage_ops.hip (the operators a pipeline stage runs beside it), compiled
 side by side and linked.  Packed-fp32 VALU instructions are disabled for the
-device code.
+device code.  The binding of the layers, csrc/bind_layers.cpp, is host code
+against torch's headers: a Python module beside the library.
 """
 
 from __future__ import annotations
@@ -14,12 +15,14 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "liboptcc.so")
+LAYERS = os.path.join(PKG, "_layers.so")
 ARCH = "gfx950"
 
 
@@ -46,12 +49,31 @@ def compile_command(out: str = LIB, source: str = SOURCES[0]) -> list:
     ]
 
 
+def layers_command(out: str = LAYERS) -> list:
+    """g++'s command for the binding of the layers."""
+    import torch
+    home = os.path.dirname(torch.__file__)
+    include = os.path.join(home, "include")
+    return [
+        "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+        f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+        "-I", INCLUDE, "-isystem", include,
+        "-isystem", os.path.join(include, "torch", "csrc", "api", "include"),
+        "-isystem", sysconfig.get_paths()["include"],
+        os.path.join(CSRC, "bind_layers.cpp"),
+        "-L", os.path.join(home, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10",
+        "-o", out,
+    ]
+
+
 def build(verbose: bool = False) -> str:
-    """Compile liboptcc.so for gfx950 next to this file; returns its path."""
+    """Compile liboptcc.so for gfx950 and the binding of the layers next to
+    this file; returns the library's path."""
     tmp = LIB + ".tmp"
     objects = [LIB + f".{i}.o" for i in range(len(SOURCES))]
     steps = [[c for c in compile_command(o, src) if c != "-shared"] + ["-c"]
              for o, src in zip(objects, SOURCES)]
+    steps.append(layers_command(LAYERS + ".tmp"))
     try:
         procs = [subprocess.Popen(cmd, stdout=subprocess.DEVNULL, stderr=subprocess.PIPE, text=True)
                  for cmd in steps]
@@ -64,6 +86,7 @@ def build(verbose: bool = False) -> str:
         for o in objects:
             if os.path.exists(o):
                 os.remove(o)
+    os.replace(LAYERS + ".tmp", LAYERS)
     os.replace(tmp, LIB)
     return LIB
 
@@ -72,7 +95,7 @@ def _report(code: int, cmd: list, err: str, verbose: bool) -> None:
     noise = "is not a recognized feature for this target"
     lines = [ln for ln in err.splitlines() if noise not in ln]
     if code != 0:
-        raise RuntimeError("hipcc failed:\n" + " ".join(cmd) + "\n" + "\n".join(lines))
+        raise RuntimeError("compiler failed:\n" + " ".join(cmd) + "\n" + "\n".join(lines))
     if verbose and lines:
         print("\n".join(lines), file=sys.stderr)
 

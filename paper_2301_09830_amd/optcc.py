@@ -2,7 +2,7 @@
 
 Every function here converts torch tensors to the pointers, sizes and the
 stream the C ABI expects and calls the function of the same name in
-liboptcc.so; all computation happens in the library's HIP kernels.  There is
+liboptcc.so (the layers through csrc/bind_layers.cpp, native for its host time); all computation happens in the library's HIP kernels.  There is
 no fallback: if the library is missing or fails to load, every call raises.
 
 Tensors are row-major 2-D CUDA (HIP) tensors with unit column stride; the
@@ -573,23 +573,6 @@ def occ_get_flags(ws, clear: bool = False, stream=None) -> int:
 # ----------------------------------------------------------------------------
 # stage operators
 # ----------------------------------------------------------------------------
-def _mat(t, name: str, rows: int, cols: int, dtype):
-    """(pointer, leading dimension) of a rows x cols matrix."""
-    if t.dtype is not dtype:
-        raise TypeError(f"{name} must be {dtype}")
-    if t.shape != (rows, cols):
-        raise ValueError(f"{name} must be {rows} x {cols}")
-    ld, unit = t.stride()
-    if unit != 1 and cols > 1:
-        raise ValueError(f"{name} must have unit column stride (row-major)")
-    if rows > 1:
-        return t.data_ptr(), ld
-    return (t.data_ptr() if rows else None), cols
-
-
-_NO_MATRIX = (None, 0)
-
-
 def _vec(t, name: str, n: int):
     if t.dtype is not _torch().float32:
         raise TypeError(f"{name} must be float32")
@@ -598,67 +581,42 @@ def _vec(t, name: str, n: int):
     return t.data_ptr()
 
 
-def _stream_of(t, stream) -> int:
-    """The given stream, or the current one of a tensor's device."""
-    if stream is not None:
-        return int(stream.cuda_stream)
-    return _torch()._C._cuda_getCurrentRawStream(t.get_device())
+_layers_module = None
 
 
-def _workspace(nbytes: int, ws, device):
-    """(tensor, pointer, bytes) of the caller's workspace or of a new one; the
-    stage operators need no initialised header."""
-    if not nbytes:
-        return None, None, 0
-    if ws is None:
-        ws = _torch().empty(nbytes + 256, dtype=_torch().uint8, device=device)
-        at = (ws.data_ptr() + 255) // 256 * 256
-        return ws, at, nbytes
-    return ws, ws.data_ptr(), ws.numel()
+def _layers():
+    """The native binding of the layers, on the loaded library's functions."""
+    global _layers_module
+    if _layers_module is None:
+        torch, L = _torch(), lib()
+        path = os.path.join(PKG, "_layers.so")
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is missing: build it with "
+                               "`python -m paper_2301_09830_amd.build`")
+        from . import _layers as module
+        names = [n + e for e in ("", "_workspace_bytes")
+                 for n in ("occ_linear_fwd", "occ_gated_fwd", "occ_linear_bwd", "occ_gated_bwd")]
+        module.setup(*(ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in names),
+                     torch._C._cuda_getCurrentRawStream)
+        _layers_module = module
+    return _layers_module
 
 
-def _rows_cols(t, name: str):
-    if t.dim() != 2:
-        raise ValueError(f"{name} must be 2-D")
-    return t.shape
+def _on(stream, call, *args):
+    """A layer's call on a given stream: what it allocates belongs to it too."""
+    with _torch().cuda.stream(stream):
+        return call(*args)
 
 
-def _layer_fwd(name: str, wide: int, X, W, bias, act, R, Y, Z, ws, stream):
-    tokens, n_in = _rows_cols(X, "X")
-    rows = _rows_cols(W, "W")[0]
-    out = rows // wide
-    if rows != wide * out:
-        raise ValueError("W must hold the rows of both projections")
-    dt = X.dtype
+def _layer_fwd(name: str, gated: bool, X, W, bias, act, R, Y, Z, ws):
     if Y is None:
-        Y = _torch().empty((tokens, out), dtype=dt, device=X.device)
-    x, ldx = _mat(X, "X", tokens, n_in, dt)
-    w, ldw = _mat(W, "W", rows, n_in, dt)
-    y, ldy = _mat(Y, "Y", tokens, out, dt)
-    r, ldr = _NO_MATRIX if R is None else _mat(R, "R", tokens, out, dt)
-    z, ldz = _NO_MATRIX if Z is None else _mat(Z, "Z", tokens, rows, dt)
-    a = occ_linear_t(_mdtype(X), act, tokens, n_in, out, x, ldx, w, ldw,
-                     None if bias is None else _vec(bias, "bias", rows), r, ldr, z, ldz, y, ldy)
-    call, size = _layer_calls(name)
-    need = size(a)
-    if need:
-        keep, wp, wn = _workspace(need, ws, X.device)
-    else:
-        wp = wn = None
-    _check(name, call(a, wp, wn or 0, _stream_of(X, stream)))
+        if X.dim() != 2 or W.dim() != 2:
+            raise ValueError("X and W must be 2-D")
+        Y = X.new_empty((X.shape[0], W.shape[0] // 2 if gated else W.shape[0]))
+    status = (_layers_module or _layers()).forward(gated, X, W, bias, act, R, Y, Z, ws)
+    if status:
+        raise OccError(name, status)
     return Y
-
-
-_layer_functions = {}
-
-
-def _layer_calls(name: str):
-    """(the call, its workspace size) of a layer's function."""
-    got = _layer_functions.get(name)
-    if got is None:
-        L = lib()
-        got = _layer_functions[name] = (getattr(L, name), getattr(L, name + "_workspace_bytes"))
-    return got
 
 
 def occ_linear_fwd(X, W, bias=None, act: int = OCC_ACT_NONE, R=None, Y=None, Z=None, ws=None,
@@ -668,7 +626,9 @@ def occ_linear_fwd(X, W, bias=None, act: int = OCC_ACT_NONE, R=None, Y=None, Z=N
     X tokens x in, W out x in, R, Y and Z tokens x out, all float32 or all
     bfloat16; bias float32.  R may be Y.  Returns Y.
     """
-    return _layer_fwd("occ_linear_fwd", 1, X, W, bias, act, R, Y, Z, ws, stream)
+    if stream is not None:
+        return _on(stream, occ_linear_fwd, X, W, bias, act, R, Y, Z, ws)
+    return _layer_fwd("occ_linear_fwd", False, X, W, bias, act, R, Y, Z, ws)
 
 
 def occ_gated_fwd(X, W, bias=None, act: int = OCC_ACT_SILU, R=None, Y=None, Z=None, ws=None,
@@ -677,30 +637,16 @@ def occ_gated_fwd(X, W, bias=None, act: int = OCC_ACT_SILU, R=None, Y=None, Z=No
 
     W is 2 out x in: the gate's rows, then the other projection's.
     """
-    return _layer_fwd("occ_gated_fwd", 2, X, W, bias, act, R, Y, Z, ws, stream)
+    if stream is not None:
+        return _on(stream, occ_gated_fwd, X, W, bias, act, R, Y, Z, ws)
+    return _layer_fwd("occ_gated_fwd", True, X, W, bias, act, R, Y, Z, ws)
 
 
-def _layer_bwd(name: str, wide: int, dY, X, W, Z, act, dX, dW, dbias, accumulate, ws, stream):
-    torch = _torch()
-    tokens, out = _rows_cols(dY, "dY")
-    some = X if X is not None else W if W is not None else dX if dX is not None else dW
-    n_in = 1 if some is None else _rows_cols(some, "X and W")[1]
-    if tokens == 0 and dX is not None and dW is None and dbias is None:
-        return      # an empty dX
-    dt, rows = dY.dtype, wide * out
-    dw_dt = dt if dW is None or dW.dtype is not torch.float32 else torch.float32
-    dy, lddy = _mat(dY, "dY", tokens, out, dt)
-    x, ldx = _NO_MATRIX if X is None else _mat(X, "X", tokens, n_in, dt)
-    w, ldw = _NO_MATRIX if W is None else _mat(W, "W", rows, n_in, dt)
-    z, ldz = _NO_MATRIX if Z is None else _mat(Z, "Z", tokens, rows, dt)
-    dx, lddx = _NO_MATRIX if dX is None else _mat(dX, "dX", tokens, n_in, dt)
-    dw, lddw = _NO_MATRIX if dW is None else _mat(dW, "dW", rows, n_in, dw_dt)
-    a = occ_linear_grad_t(_mdtype(dY), OCC_F32 if dw_dt is torch.float32 else OCC_BF16, act, 0,
-                          tokens, n_in, out, dy, lddy, x, ldx, w, ldw, z, ldz, dx, lddx, dw, lddw,
-                          None if dbias is None else _vec(dbias, "dbias", rows))
-    call, size = _layer_calls(name)
-    keep, wp, wn = _workspace(size(a), ws, dY.device)
-    _check(name, call(a, OCC_GRAD_ACCUMULATE if accumulate else 0, wp, wn, _stream_of(dY, stream)))
+def _layer_bwd(name: str, gated: bool, dY, X, W, Z, act, dX, dW, dbias, accumulate, ws):
+    status = (_layers_module or _layers()).backward(
+        gated, dY, X, W, Z, act, dX, dW, dbias, OCC_GRAD_ACCUMULATE if accumulate else 0, ws)
+    if status:
+        raise OccError(name, status)
 
 
 def occ_linear_bwd(dY, X=None, W=None, Z=None, act: int = OCC_ACT_NONE, dX=None, dW=None,
@@ -710,14 +656,18 @@ def occ_linear_bwd(dY, X=None, W=None, Z=None, act: int = OCC_ACT_NONE, dX=None,
     Z is the stored pre-activation (not needed with OCC_ACT_NONE).  accumulate:
     dW and dbias are added to.  The gradient of R is dY itself.
     """
-    _layer_bwd("occ_linear_bwd", 1, dY, X, W, Z, act, dX, dW, dbias, accumulate, ws, stream)
+    if stream is not None:
+        return _on(stream, occ_linear_bwd, dY, X, W, Z, act, dX, dW, dbias, accumulate, ws)
+    _layer_bwd("occ_linear_bwd", False, dY, X, W, Z, act, dX, dW, dbias, accumulate, ws)
 
 
 def occ_gated_bwd(dY, X=None, W=None, Z=None, act: int = OCC_ACT_SILU, dX=None, dW=None,
                   dbias=None, accumulate: bool = False, ws=None, stream=None) -> None:
     """Gradients of occ_gated_fwd (W, dW and dbias hold both projections); as
     occ_linear_bwd, with Z = [G U] always needed."""
-    _layer_bwd("occ_gated_bwd", 2, dY, X, W, Z, act, dX, dW, dbias, accumulate, ws, stream)
+    if stream is not None:
+        return _on(stream, occ_gated_bwd, dY, X, W, Z, act, dX, dW, dbias, accumulate, ws)
+    _layer_bwd("occ_gated_bwd", True, dY, X, W, Z, act, dX, dW, dbias, accumulate, ws)
 
 
 def make_param(W, m, v, G=None, P=None, Q=None, W16=None, m_scale=None, v_scale=None,

@@ -211,3 +211,18 @@ def test_binding_refusals():
         optcc.make_param(w, torch.zeros(4, 301), w.clone(), G=w)
     with pytest.raises(TypeError):
         optcc.make_param(w.bfloat16(), w.clone(), w.clone(), G=w)
+
+
+def test_layers_need_tensors_on_a_gpu():
+    torch = pytest.importorskip("torch")
+    X, W, dY = torch.zeros(4, 8), torch.zeros(6, 8), torch.zeros(4, 6)
+    with pytest.raises(ValueError):
+        optcc.occ_linear_fwd(X, W)
+    with pytest.raises(ValueError):
+        optcc.occ_linear_bwd(dY, X, W, dX=torch.zeros(4, 8), dW=torch.zeros(6, 8))
+    with pytest.raises(TypeError):
+        optcc.occ_linear_fwd(X, W, R=1.0)
+    with pytest.raises(ValueError):
+        optcc.occ_linear_bwd(dY, X, W[0], dX=torch.zeros(4, 8))
+    with pytest.raises(TypeError):
+        optcc.occ_linear_bwd(dY.half(), X, W, dW=torch.zeros(6, 8))
