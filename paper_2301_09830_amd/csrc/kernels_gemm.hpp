@@ -193,6 +193,27 @@ __device__ __forceinline__ void st_quad(T* p, f32x4_t v, int left) {
     if (i < left) st_elem(p + i, v[i]);
 }
 
+// 16 bytes of a row, at any alignment; `left` elements of it are inside.
+template <class T>
+__device__ __forceinline__ f32x4_t ld_piece(const T* p, int left) {
+  constexpr int CH = 16 / sizeof(T);
+  if (left >= CH) {
+    if constexpr (sizeof(T) == 4) {
+      const f4u_t v = *(const f4u_t*)p;
+      return f32x4_t{v[0], v[1], v[2], v[3]};
+    } else {
+      const u4h_t v = *(const u4h_t*)p;
+      return f32x4_t{__uint_as_float(v[0]), __uint_as_float(v[1]), __uint_as_float(v[2]), __uint_as_float(v[3])};
+    }
+  }
+  T e[CH];
+#pragma unroll
+  for (int i = 0; i < CH; ++i) e[i] = i < left ? p[i] : (T)0;
+  f32x4_t r;
+  __builtin_memcpy(&r, e, 16);
+  return r;
+}
+
 // ----------------------------------------------------------------------------
 // the epilogue of the forward pass, shared by all forms of the product
 // ----------------------------------------------------------------------------
@@ -249,6 +270,14 @@ __device__ __forceinline__ void fwd_epilogue(const FwdEpi& e, int64_t m, int n, 
 // ----------------------------------------------------------------------------
 // tiled product
 // ----------------------------------------------------------------------------
+// dZ of a layer, made from dY and Z where it is loaded.  Z null: dZ = dY.
+struct DzSource {
+  const void* dY;
+  const void* Z;
+  int64_t ldy, ldz;
+  int32_t out, act, gated;
+};
+
 struct GemmArgs {
   const void* A;      // K contiguous: M x K; K strided: K x M
   const void* B;      // K contiguous: N x K; K strided: K x N
@@ -264,6 +293,7 @@ struct GemmArgs {
   int64_t plane_a, plane_b;   // fp32 as three bf16 planes: bytes from one to the next
   int32_t seg_tiles;          // K tiles of one pair of planes
   FwdEpi fwd;
+  DzSource dz;                // direct form: dz.Z, if given, in place of A
 };
 
 // fp32 operands on the bf16 matrix units: x = h + m + l, each the bf16 nearest
@@ -567,6 +597,114 @@ __device__ __forceinline__ void fwd_rows(const FwdEpi& e, int64_t M, int64_t m, 
   }
 }
 
+// One operand of the direct form: 64 rows, a piece of 16 bytes for each of 512
+// threads, through registers to the places of a tile that the DMA above fills.
+// Rows may lie at any alignment.  A source of dZ is turned into it on the way,
+// rounded to the layer's type as it would be if it were stored.
+template <class T, bool KS>
+struct DirectOperand {
+  static constexpr int CH = 16 / sizeof(T), KROW = 64 * sizeof(T);
+  struct Raw {
+    f32x4_t p[3];   // of the matrix or dY; of Z: gate, other projection
+  };
+  const T* base;
+  int64_t ld;
+  DzSource dz;
+  int at, kk, rows, k_end;   // at: the lane's row; K strided: first of its columns
+
+  template <class F>
+  __device__ __forceinline__ void init(const void* p, int64_t ld_, const DzSource& d, int rows_, int k_end_, int row0,
+                                       int wave, int lane, F&& row_of) {
+    base = (const T*)p;
+    ld = ld_;
+    dz = d;
+    rows = rows_;
+    k_end = k_end_;
+    if constexpr (KS) {
+      constexpr int LPR = KROW / 16;
+      const int k = wave * (64 / LPR) + lane / LPR;
+      kk = k;
+      at = row0 + ((lane % LPR) ^ Operand<64, true, sizeof(T), 8>::turn(k)) * CH;
+    } else {
+      kk = ((lane & 7) ^ (lane >> 3)) * CH;
+      at = row_of(wave * 8 + (lane >> 3));
+    }
+  }
+
+  __device__ __forceinline__ void place(int k0, int64_t& row, int& col, int& left) const {
+    row = KS ? k0 + kk : at;
+    col = KS ? at : k0 + kk;
+    left = KS ? (row < k_end ? rows - col : 0) : k_end - col;
+  }
+
+  __device__ __forceinline__ Raw fetch(int k0) const {
+    int64_t row;
+    int col, left;
+    place(k0, row, col, left);
+    Raw r = {};
+    if (!dz.Z) {
+      r.p[0] = ld_piece<T>(base + row * ld + col, left);
+      return r;
+    }
+    const T* const y = (const T*)dz.dY + row * dz.ldy;
+    const T* const z = (const T*)dz.Z + row * dz.ldz;
+    if (!dz.gated || col + CH <= dz.out) {
+      r.p[0] = ld_piece<T>(y + col, left);
+      r.p[1] = ld_piece<T>(z + col, left);
+      if (dz.gated) r.p[2] = ld_piece<T>(z + dz.out + col, left);
+    } else if (col >= dz.out) {
+      r.p[0] = ld_piece<T>(y + col - dz.out, left);
+      r.p[1] = ld_piece<T>(z + col - dz.out, left);
+    } else {   // columns of both projections
+      T e[3][CH];
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        const bool other = col + i >= dz.out;
+        const int c = col + i - (other ? dz.out : 0);
+        e[0][i] = i < left ? y[c] : (T)0;
+        e[1][i] = i < left ? z[c] : (T)0;
+        e[2][i] = i < left && !other ? z[dz.out + c] : (T)0;
+      }
+      __builtin_memcpy(r.p, e, 48);
+    }
+    return r;
+  }
+
+  // four elements from the i-th of a piece
+  static __device__ __forceinline__ f32x4_t quad(f32x4_t p, int i) {
+    if constexpr (sizeof(T) == 4) return p;
+    const uint32_t lo = __float_as_uint(p[2 * i]), hi = __float_as_uint(p[2 * i + 1]);
+    return f32x4_t{bf16_lo(lo), bf16_hi(lo), bf16_lo(hi), bf16_hi(hi)};
+  }
+
+  __device__ __forceinline__ f32x4_t finish(const Raw& r, int k0) const {
+    if (!dz.Z) return r.p[0];
+    int64_t row;
+    int col, left;
+    place(k0, row, col, left);
+    f32x4_t o;
+#pragma unroll
+    for (int i = 0; i < CH / 4; ++i) {
+      const f32x4_t dy = quad(r.p[0], i), z = quad(r.p[1], i);
+      f32x4_t a, da, d;
+      act_grad_quad(dz.act, z, a, da);
+      d = dy * da;
+      if (dz.gated) {
+        const f32x4_t u = quad(r.p[2], i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) d[k] = col + 4 * i + k >= dz.out ? dy[k] * a[k] : dy[k] * u[k] * da[k];
+      }
+      if constexpr (sizeof(T) == 4) {
+        o = d;
+      } else {
+        o[2 * i] = __uint_as_float(bf16_pack2(d[0], d[1]));
+        o[2 * i + 1] = __uint_as_float(bf16_pack2(d[2], d[3]));
+      }
+    }
+    return o;
+  }
+};
+
 // A form of the product: WM x WN waves, each 16 FA x 16 FB results, S stages
 // of K tiles in LDS.
 // S == 2 (256 x 256): the waves form two groups, one wave of each on every
@@ -574,8 +712,10 @@ __device__ __forceinline__ void fwd_rows(const FwdEpi& e, int64_t M, int64_t m, 
 // S == 4 (128 x 128 and 64 x 64): tiles are loaded three ahead, one barrier a
 // tile; two waves a SIMD, since one alone stands still while its loads are
 // issued (4096^3 bf16 at 128 x 128: 203 us on four waves, 151 on eight).
-template <int WM_, int WN_, int FA_, int FB_, int S_>
+// DIRECT: operands come through registers, two stages.
+template <int WM_, int WN_, int FA_, int FB_, int S_, bool DIRECT_ = false>
 struct Form {
+  static constexpr bool DIRECT = DIRECT_;
   static constexpr int WM = WM_, WN = WN_, FA = FA_, FB = FB_, S = S_;
   static constexpr int NW = WM * WN, BM = WM * FA * 16, BN = WN * FB * 16;
   static constexpr int LDS = S * (BM + BN) * kRowBytes;
@@ -583,6 +723,7 @@ struct Form {
 using Form256 = Form<2, 4, 8, 4, 2>;
 using Form128 = Form<2, 4, 4, 2, 4>;
 using Form64 = Form<4, 2, 1, 2, 4>;
+using FormDirect = Form<4, 2, 1, 2, 2, true>;
 
 // Block `block` of a product: all of its tile's K, or one part of it.  T: type
 // of the operands, TE: of the layer (fp32 on bf16 planes: T bf16, TE fp32).
@@ -590,7 +731,7 @@ template <class T, class TE, class F, bool AKS, bool BKS, int EP>
 __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_char* lds) {
   constexpr int ES = sizeof(T), S = F::S, NW = F::NW, WM = F::WM, WN = F::WN, FA = F::FA, FB = F::FB;
   constexpr int BM = F::BM, BN = F::BN;
-  constexpr bool PP = S == 2, SEG = sizeof(T) != sizeof(TE);
+  constexpr bool PP = S == 2 && !F::DIRECT, SEG = sizeof(T) != sizeof(TE);
   using OA = Operand<BM, AKS, ES, NW>;
   using OB = Operand<BN, BKS, ES, NW>;
   constexpr int STAGE = OA::BYTES + OB::BYTES;
@@ -614,11 +755,8 @@ __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_cha
   int in_a = SEG ? kt0 - pair_a * g.seg_tiles : kt0, in_b = in_a;
   const char* const A = (const char*)g.A;
   const char* const B = (const char*)g.B;
-  OA oa;
-  OB ob;
-  oa.init(SEG ? A + plane_of_a(pair_a) * g.plane_a : A, g.lda, g.M, m0, wave, lane, (int64_t)in_a * BK,
-          [&](int r) { return min(m0 + r, g.M - 1); });
-  ob.init(SEG ? B + plane_of_b(pair_b) * g.plane_b : B, g.ldb, g.N, n0, wave, lane, (int64_t)in_b * BK, [&](int r) {
+  auto row_of_a = [&](int r) { return min(m0 + r, g.M - 1); };
+  auto row_of_b = [&](int r) {
     if constexpr (EP == EP_GATED) {
       // each wave's columns: half of them the gate's, then the same of the other projection
       constexpr int TN = FB * 16;
@@ -627,7 +765,13 @@ __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_cha
     } else {
       return min(n0 + r, g.N - 1);
     }
-  });
+  };
+  OA oa;
+  OB ob;
+  if constexpr (!F::DIRECT) {
+    oa.init(SEG ? A + plane_of_a(pair_a) * g.plane_a : A, g.lda, g.M, m0, wave, lane, (int64_t)in_a * BK, row_of_a);
+    ob.init(SEG ? B + plane_of_b(pair_b) * g.plane_b : B, g.ldb, g.N, n0, wave, lane, (int64_t)in_b * BK, row_of_b);
+  }
   if constexpr (SEG) {   // plane 0
     oa.start -= plane_of_a(pair_a) * g.plane_a;
     ob.start -= plane_of_b(pair_b) * g.plane_b;
@@ -663,7 +807,52 @@ __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_cha
     }
   };
 
-  if constexpr (PP) {
+  if constexpr (F::DIRECT) {
+    // Three tiles' loads are in flight, in registers; a stage is written again
+    // behind the barrier that follows every wave's last read of it.
+    constexpr int D = 3;
+    DirectOperand<T, AKS> da;
+    DirectOperand<T, BKS> db;
+    da.init(g.A, g.lda, g.dz, g.M, g.ka, m0, wave, lane, row_of_a);
+    db.init(g.B, g.ldb, DzSource{}, g.N, g.kb, n0, wave, lane, row_of_b);
+    typename DirectOperand<T, AKS>::Raw xa[D];
+    typename DirectOperand<T, BKS>::Raw xb[D];
+#pragma unroll
+    for (int d = 0; d < D; ++d)
+      if (d < nk) {
+        xa[d] = da.fetch((kt0 + d) * BK);
+        xb[d] = db.fetch((kt0 + d) * BK);
+      }
+    typedef __attribute__((address_space(3))) f32x4_t lds_piece;
+    for (int k3 = 0; k3 < nk; k3 += D) {
+#pragma unroll
+      for (int d = 0; d < D; ++d) {
+        const int kt = k3 + d;
+        if (kt >= nk) continue;
+        lds_char* const p = lds + (kt & 1) * STAGE;
+        *(lds_piece*)(p + threadIdx.x * 16) = da.finish(xa[d], (kt0 + kt) * BK);
+        *(lds_piece*)(p + OA::BYTES + threadIdx.x * 16) = db.finish(xb[d], (kt0 + kt) * BK);
+        if (kt + D < nk) {
+          xa[d] = da.fetch((kt0 + kt + D) * BK);
+          xb[d] = db.fetch((kt0 + kt + D) * BK);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          f32x4_t fa[FA], fb[FB];
+#pragma unroll
+          for (int i = 0; i < FA; ++i) fa[i] = ra.template read_half<OA::KROW>(p, i, h);
+#pragma unroll
+          for (int i = 0; i < FB; ++i) fb[i] = rb.template read_half<OB::KROW>(p + OA::BYTES, i, h);
+#pragma unroll
+          for (int i = 0; i < FA; ++i)
+#pragma unroll
+            for (int j = 0; j < FB; ++j) acc[i][j] = mfma_half<ES>(fb[j], fa[i], acc[i][j]);
+        }
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // every wave's reads have ended
+  } else if constexpr (PP) {
     constexpr int HA = FA / 2, HB = FB / 2, Q1 = HA / 4, Q2 = HA / 2;
     Frag<ES> a0[HA], a1[HA], b0[HB], b1[HB];
     // fragments i0 .. i1 - 1 of a half
@@ -869,6 +1058,12 @@ template <class T, class TE, class F, int EP>
 __global__ __launch_bounds__(F::NW * 64, 2) void k_gemm(GemmArgs g) {
   __shared__ __attribute__((aligned(1024))) char sm[F::LDS];
   gemm_block<T, TE, F, false, false, EP>(g, blockIdx.x, (lds_char*)sm);
+}
+
+template <class T, int EP>
+__global__ __launch_bounds__(512, 4) void k_gemm_direct(GemmArgs g) {
+  __shared__ __attribute__((aligned(1024))) char sm[FormDirect::LDS];
+  gemm_block<T, T, FormDirect, false, false, EP>(g, blockIdx.x, (lds_char*)sm);
 }
 
 // Sum of the partial products of a split K, in split order, and the epilogue.

@@ -18,27 +18,6 @@ struct SkinnyArgs {
   FwdEpi fwd;
 };
 
-// 16 bytes of a row, at any alignment; `left` elements of it are inside.
-template <class T>
-__device__ __forceinline__ f32x4_t ld_piece(const T* p, int left) {
-  constexpr int CH = 16 / sizeof(T);
-  if (left >= CH) {
-    if constexpr (sizeof(T) == 4) {
-      const f4u_t v = *(const f4u_t*)p;
-      return f32x4_t{v[0], v[1], v[2], v[3]};
-    } else {
-      const u4h_t v = *(const u4h_t*)p;
-      return f32x4_t{__uint_as_float(v[0]), __uint_as_float(v[1]), __uint_as_float(v[2]), __uint_as_float(v[3])};
-    }
-  }
-  T e[CH];
-#pragma unroll
-  for (int i = 0; i < CH; ++i) e[i] = i < left ? p[i] : (T)0;
-  f32x4_t r;
-  __builtin_memcpy(&r, e, 16);
-  return r;
-}
-
 // One column of one token.
 template <class T, bool GATED>
 __device__ __forceinline__ void fwd_epilogue_one(const FwdEpi& e, int64_t m, int n, float z, float u) {
@@ -394,6 +373,8 @@ struct BiasArgs {
   float* dbias;
   int64_t width;
   int32_t strips, accumulate;
+  DzSource src;        // of the direct form, which has no parts
+  int32_t tokens;
 };
 
 // 64 columns a block of 512 threads: 8 threads a column add every 8th strip,
@@ -423,6 +404,70 @@ __device__ __forceinline__ void bias_block(const BiasArgs& g, int block, float* 
   g.dbias[n] = g.accumulate ? g.dbias[n] + s : s;
 }
 
+// Straight from dY and Z: 16 columns of dY a block of 512 threads, four of
+// them and every 128th row a thread, both projections together (64 columns and
+// every 32nd row: the backward pass of 991 x 1076 x 390 bf16 24 us, a chain of
+// loads; 14 this way).
+constexpr int BD_COLS = 16, BD_ROWS = 128;
+constexpr int BD_LDS = 2 * BD_ROWS * BD_COLS * 4;
+
+template <class T>
+__device__ __forceinline__ void bias_direct(const BiasArgs& g, int block, float* lds) {
+  constexpr int U = 4;   // rows whose loads are in flight together
+  const DzSource& d = g.src;
+  const int c = threadIdx.x % (BD_COLS / 4), r = threadIdx.x / (BD_COLS / 4);
+  const int n = block * BD_COLS + c * 4, left = d.out - n;
+  f32x4_t s0 = {}, s1 = {};
+  if (left > 0) {
+    for (int64_t m = r; m < g.tokens; m += U * BD_ROWS) {
+      f32x4_t dy[U], z[U], u[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int64_t row = min(m + i * BD_ROWS, (int64_t)g.tokens - 1);
+        dy[i] = ld_quad<T>((const T*)d.dY + row * d.ldy + n, left);
+        const T* const zr = (const T*)d.Z + row * d.ldz + n;
+        if (d.Z) z[i] = ld_quad<T>(zr, left);
+        if (d.gated) u[i] = ld_quad<T>(zr + d.out, left);
+      }
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        if (m + i * BD_ROWS >= g.tokens) continue;
+        f32x4_t a, da;
+        if (d.Z) act_grad_quad(d.act, z[i], a, da);
+        s0 += d.gated ? dy[i] * u[i] * da : d.Z ? dy[i] * da : dy[i];
+        if (d.gated) s1 += dy[i] * a;
+      }
+    }
+  }
+  f32x4_t* const part = (f32x4_t*)lds;
+  part[threadIdx.x] = s0;
+  if (d.gated) part[512 + threadIdx.x] = s1;
+  __syncthreads();
+  // 16 threads a column, 8 rows each, then their sums in order
+  constexpr int G = 16, PER = BD_ROWS / G;
+  const int col = threadIdx.x % BD_COLS, k = threadIdx.x / BD_COLS % G, half = threadIdx.x / (BD_COLS * G);
+  float s = 0.0f;
+  const float* const p = lds + (half * BD_ROWS + k * PER) * BD_COLS + col;
+  if (half == 0 || d.gated) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) s += p[i * BD_COLS];
+  }
+  __syncthreads();
+  lds[threadIdx.x] = s;
+  __syncthreads();
+  if (k || (half && !d.gated) || block * BD_COLS + col >= d.out) return;
+#pragma unroll
+  for (int i = 1; i < G; ++i) s += lds[threadIdx.x + i * BD_COLS];
+  const int64_t at = (int64_t)half * d.out + block * BD_COLS + col;
+  g.dbias[at] = g.accumulate ? g.dbias[at] + s : s;
+}
+
+template <class T>
+__device__ __forceinline__ void bias_any(const BiasArgs& g, int block, float* lds) {
+  if (g.part) bias_block(g, block, lds);
+  else bias_direct<T>(g, block, lds);
+}
+
 // The bias gradient, dX = dZ W and dW = dZ^T X in one launch: where one of the
 // products alone leaves CUs idle, or ends in a part of a round, the other's
 // blocks fill them.
@@ -439,8 +484,19 @@ __global__ __launch_bounds__(F::NW * 64, 2) void k_backward(BackwardArgs g) {
   if (b < g.dx_blocks) return gemm_block<T, TE, F, false, true, EP_STORE>(g.dx, b, (lds_char*)sm);
   b -= g.dx_blocks;
   if (b < g.dw_blocks) return gemm_block<T, TE, F, true, true, EP_STORE>(g.dw, b, (lds_char*)sm);
-  static_assert(F::NW == 8, "bias_block runs on eight waves");
-  bias_block(g.bias, b - g.dw_blocks, (float*)sm);
+  static_assert(F::NW == 8, "the bias blocks run on eight waves");
+  bias_any<TE>(g.bias, b - g.dw_blocks, (float*)sm);
+}
+
+// The same from dY and Z themselves, with no launch before it.
+template <class T>
+__global__ __launch_bounds__(512, 4) void k_backward_direct(BackwardArgs g) {
+  __shared__ __attribute__((aligned(1024))) char sm[FormDirect::LDS];
+  int b = blockIdx.x;
+  if (b < g.dx_blocks) return gemm_block<T, T, FormDirect, false, true, EP_STORE>(g.dx, b, (lds_char*)sm);
+  b -= g.dx_blocks;
+  if (b < g.dw_blocks) return gemm_block<T, T, FormDirect, true, true, EP_STORE>(g.dw, b, (lds_char*)sm);
+  bias_direct<T>(g.bias, b - g.dw_blocks, (float*)sm);
 }
 
 // Joins the parts of both products.
@@ -452,9 +508,10 @@ __global__ __launch_bounds__(256) void k_backward_join(GemmArgs dx, GemmArgs dw,
 }
 
 // dbias alone
+template <class T>
 __global__ __launch_bounds__(512) void k_bias(BiasArgs g) {
-  __shared__ float sm[512];
-  bias_block(g, blockIdx.x, sm);
+  __shared__ __attribute__((aligned(16))) float sm[BD_LDS / 4];
+  bias_any<T>(g, blockIdx.x, sm);
 }
 
 // Zeros where no token contributes to a gradient.

@@ -89,9 +89,8 @@ struct Product {
 
 // pair: columns come in pairs of rows of W (gated), so a tile makes half as many
 // planes: fp32 operands as bf16 planes, K once for each pair of them
-Product make_product(int64_t m, int64_t width, int64_t k, size_t es, Tile tile, int splits, bool pair, bool planes) {
+Product make_product(int64_t m, int64_t width, int64_t k, size_t es, const TileTimes& t, int splits, bool pair, bool planes) {
   Product p;
-  const TileTimes& t = kTiles[tile];
   p.tiles_m = div_up(m, t.side);
   p.tiles_n = pair ? div_up(width / 2, t.side / 2) : div_up(width, t.side);
   p.tiles_k = div_up(k, kRowBytes / (int64_t)es) * (planes ? kPairs : 1);
@@ -135,15 +134,15 @@ double launch_us(const Product& x, const Product& w, int64_t slots, bool halves)
   return full + x.block_us + (double)div_up(left - free, slots) * w.block_us;
 }
 
-// Up to two products of one launch, with the same tile.  m, width, k: of each
-// (m = 0: not there).
+// Up to two products of one launch, with the same of the given tiles.  m, width,
+// k: of each (m = 0: not there).
 ProductPlan plan_products(const int64_t (&m)[2], const int64_t (&width)[2], const int64_t (&k)[2], size_t es,
-                          bool pair, bool planes = false) {
+                          bool pair, bool planes = false, const TileTimes* tiles = kTiles, int num = TILE_NUM) {
   ProductPlan best;
   double best_us = INFINITY;
-  for (int t = 0; t < TILE_NUM; ++t) {
-    const bool halves = es == 4 && kTiles[t].resident > 1;
-    const int64_t slots = (int64_t)kCUs * (es == 4 ? 1 : kTiles[t].resident);
+  for (int t = 0; t < num; ++t) {
+    const bool halves = es == 4 && tiles[t].resident > 1;
+    const int64_t slots = (int64_t)kCUs * (es == 4 ? 1 : tiles[t].resident);
     Product of[2][kSplits];
     int n[2] = {0, 0};
     for (int i = 0; i < 2; ++i) {
@@ -152,7 +151,7 @@ ProductPlan plan_products(const int64_t (&m)[2], const int64_t (&width)[2], cons
         continue;
       }
       for (const int s : kSplitCounts) {
-        const Product p = make_product(m[i], width[i], k[i], es, (Tile)t, s, pair, planes);
+        const Product p = make_product(m[i], width[i], k[i], es, tiles[t], s, pair, planes);
         if (p.splits != s || (s > 1 && p.k_per_split < 4) || !product_fits(p)) break;
         of[i][n[i]++] = p;
         if (p.blocks() > 2 * slots) break;   // parts of K would only add work
@@ -175,6 +174,23 @@ ProductPlan plan_products(const int64_t (&m)[2], const int64_t (&width)[2], cons
     }
   }
   return best;
+}
+
+// The direct form: 64 x 64 tiles whose operands come through registers, at any
+// alignment, dZ made on the way by every block that reads it.  No launch
+// before the products, but more work in each of their K tiles: two resident
+// blocks 0.50 us in bf16, 1.17 with relu, 1.87 with gelu, 1.02 to 1.31 with
+// rows off 16 bytes (the tiles above: 0.42), bound by the VALU, so that a block
+// alone takes half of it.  Linear backward, bf16: 94 x 768 x 64 with gelu 8.2 us,
+// with dZ made before the products 12.7; 4293 x 463 x 663 with relu 131 us
+// against 29.
+ProductPlan plan_direct(const int64_t (&m)[2], const int64_t (&width)[2], const int64_t (&k)[2], size_t es, bool pair,
+                        bool dz, bool act, bool off_pieces) {
+  const bool costly = dz && act;   // more than a comparison an element
+  const bool back = m[1] || dz;
+  const TileTimes t = {64, 1, 0.30 + (costly ? 0.65 : dz ? 0.35 : 0.0) + (off_pieces ? (back ? 0.4 : 0.1) : 0.0),
+                       0.56 + (costly ? 0.4 : dz ? 0.2 : 0.0) + (off_pieces ? (back ? 0.15 : 0.06) : 0.0), 3.0};
+  return plan_products(m, width, k, es, pair, false, &t, 1);
 }
 
 void set_tiles(GemmArgs& g, const Product& p, char* part) {
@@ -260,9 +276,19 @@ double few_us(int64_t tokens, int64_t n_in, int64_t out, size_t es, bool gated, 
 // us of the copy of an operand that the tiled product cannot take in place
 double copy_us(int64_t rows, int64_t cols, size_t es) { return 3.0 + 2.0 * (double)rows * (double)cols * (double)es / 6e6; }
 
+// us of the launch that makes dZ, sums bias strips or copies operands:
+// `elements` read and written
+double prep_us(double elements, size_t es) { return elements > 0.0 ? 5.0 + elements * (double)es / 5e6 : 0.0; }
+
+// Up to kBiasTokens the bias gradient is summed from dY and Z themselves, in
+// blocks beside the products' (a rule on the tokens alone, so that its order
+// does not depend on what else a call makes).
+constexpr int64_t kBiasTokens = 1024;
+
 struct FwdPlan {
   bool few = false, copy_x = false, copy_w = false;
   bool planes = false;   // fp32 on the bf16 matrix units
+  bool direct = false;   // operands as they lie, through registers
   size_t x_off = 0, w_off = 0, part_off = 0, bytes = 0;
   ProductPlan prod;
 };
@@ -289,16 +315,26 @@ occ_status_t plan_fwd(const occ_linear_t& l, bool gated, FwdPlan& f) {
   f.copy_w = needs_copy(l.W, l.ldw, l.in, es);
   f.prod = plan_products({l.tokens, 0}, {wide, 0}, {l.in, 0}, es, gated);
   if (!f.prod.fits) return OCC_E_SHAPE;
+  const double copies = f.copy_x || f.copy_w ? copy_us(l.tokens * f.copy_x + wide * f.copy_w, l.in, es) : 0.0;
+  double tiled = f.prod.us + copies;
+  if (copies > 0.0) {
+    const ProductPlan p = plan_direct({l.tokens, 0}, {wide, 0}, {l.in, 0}, es, gated, false, false, true);
+    if (p.fits && p.us < tiled) {
+      f.prod = p;
+      tiled = p.us;
+      f.direct = true;
+      f.copy_x = f.copy_w = false;
+    }
+  }
   if (l.tokens <= kFewTokens) {
-    const double tiled = f.prod.us + (f.copy_w ? copy_us(wide, l.in, es) : 0.0);
-    f.few = few_us(l.tokens, l.in, l.out, es, gated, !f.copy_w) <= tiled;
+    f.few = few_us(l.tokens, l.in, l.out, es, gated, !needs_copy(l.W, l.ldw, l.in, es)) <= tiled;
     if (f.few) return OCC_OK;
   }
   if (l.dtype == OCC_F32) {
     const ProductPlan p = plan_products({l.tokens, 0}, {wide, 0}, {l.in, 0}, 2, gated, true);
-    const double copies = f.copy_x || f.copy_w ? copy_us(l.tokens * f.copy_x + wide * f.copy_w, l.in, es) : 0.0;
-    if (p.fits && p.us + 3.0 + planes_us((double)(l.tokens + wide) * (double)l.in) < f.prod.us + copies) {
+    if (p.fits && p.us + 3.0 + planes_us((double)(l.tokens + wide) * (double)l.in) < tiled) {
       f.prod = p;
+      f.direct = false;
       f.planes = f.copy_x = f.copy_w = true;
     }
   }
@@ -374,7 +410,7 @@ occ_status_t run_fwd(const occ_linear_t& l, const FwdPlan& f, char* ws, hipStrea
   OCC_TRY((run_prep<T, GATED>(prep, s)));
   g.M = (int32_t)l.tokens;
   g.N = (int32_t)l.out;
-  g.ka = g.kb = (int32_t)ldp;
+  g.ka = g.kb = (int32_t)(f.direct ? l.in : ldp);
   g.fwd = e;
   set_tiles(g, f.prod.x, ws + f.part_off);
   constexpr int EP = GATED ? EP_GATED : EP_FWD;
@@ -389,7 +425,11 @@ occ_status_t run_fwd(const occ_linear_t& l, const FwdPlan& f, char* ws, hipStrea
       }
     });
   };
-  if (f.planes) {
+  if (f.direct) {
+    OCC_TRY(launch(GATED ? "gated_fwd" : "linear_fwd", s, [&] {
+      hipLaunchKernelGGL((k_gemm_direct<T, EP>), grid, block, 0, s, g);
+    }));
+  } else if (f.planes) {
     g.seg_tiles = (int32_t)(f.prod.x.tiles_k / kPairs);
     OCC_TRY(product(uint16_t{}));
   } else {
@@ -439,6 +479,8 @@ occ_status_t forward(const occ_linear_t* lp, void* ws, size_t ws_bytes, occ_stre
 struct BwdPlan {
   bool has_dz = false;    // dZ is made (else it is dY)
   bool planes = false;    // fp32 on the bf16 matrix units
+  bool direct = false;    // operands as they lie, dZ made where it is loaded
+  bool strip_bias = false;   // bias sums by strips of rows, beside dZ
   bool copy_dy = false, copy_x = false, copy_w = false;
   int64_t strip = 0, strips = 0;
   size_t dz_off = 0, bias_off = 0, x_off = 0, w_off = 0, dx_part = 0, dw_part = 0, bytes = 0;
@@ -469,42 +511,58 @@ occ_status_t plan_bwd(const occ_linear_grad_t& l, bool gated, BwdPlan& f) {
   const bool prod = l.dX || l.dW;
   const bool act = gated || l.act != OCC_ACT_NONE;
   f.has_dz = act && prod;
+  f.strip_bias = l.dbias && l.tokens > kBiasTokens;
   if (prod) {
     f.copy_dy = !act && needs_copy(l.dY, l.lddy, l.out, es);
     f.copy_w = l.dX && needs_copy(l.W, l.ldw, l.in, es);
     f.copy_x = l.dW && needs_copy(l.X, l.ldx, l.in, es);
     const int64_t m[2] = {l.dX ? l.tokens : 0, l.dW ? wide : 0}, width[2] = {l.in, l.in}, k[2] = {wide, l.tokens};
     f.prod = plan_products(m, width, k, es, false);
+    if (!f.prod.fits) return OCC_E_SHAPE;
+    const double x = l.dW ? (double)l.tokens * (double)l.in : 0.0, w = l.dX ? (double)wide * (double)l.in : 0.0;
+    const double dz = (double)l.tokens * (double)wide, dy = (double)l.tokens * (double)l.out;
+    const double copied = (f.copy_x ? x : 0.0) + (f.copy_w ? w : 0.0) + (f.copy_dy ? dz : 0.0);
+    double us = f.prod.us + prep_us((act ? dy + 2.0 * dz : f.strip_bias ? dy : 0.0) + 2.0 * copied, es);
+    if (us > f.prod.us && !f.strip_bias) {
+      const bool off_pieces = copied > 0.0 || (act && (needs_copy(l.dY, l.lddy, l.out, es) || needs_copy(l.Z, l.ldz, wide, es)));
+      const ProductPlan p = plan_direct(m, width, k, es, false, act, gated || l.act != OCC_ACT_RELU, off_pieces);
+      // each product reads dY and Z for itself
+      const double all = p.us + (act ? (dy + dz) * (double)es * ((l.dX ? 1 : 0) + (l.dW ? 1 : 0)) / 6e6 : 0.0);
+      if (p.fits && all < us) {
+        f.prod = p;
+        us = all;
+        f.direct = true;
+        f.has_dz = f.copy_dy = f.copy_x = f.copy_w = false;
+      }
+    }
     if (l.dtype == OCC_F32) {
       const ProductPlan p = plan_products(m, width, k, 2, false, true);
-      const double x = l.dW ? (double)l.tokens * (double)l.in : 0.0, w = l.dX ? (double)wide * (double)l.in : 0.0;
-      const double dz = (double)l.tokens * (double)wide;
-      const double copied = (f.copy_x ? x : 0.0) + (f.copy_w ? w : 0.0) + (f.copy_dy ? dz : 0.0);
-      const double copies = copied > 0.0 && !act ? copy_us(1, (int64_t)copied, es) : copied * 8.0 / 6e6;
-      // dZ itself is written in either form
-      if (p.fits && p.us + 3.0 + planes_us(x + w + (act ? 0.2 : 1.0) * dz) < f.prod.us + copies) {
+      // dZ, if it is made, is written as planes in place of fp32
+      const double planes = 3.0 + planes_us(x + w + dz) + (act || f.strip_bias ? dy * 4.0 / 5e6 : 0.0);
+      if (p.fits && p.us + planes < us) {
         f.prod = p;
         f.planes = true;
+        f.direct = false;
+        f.has_dz = act;
         f.copy_x = l.dW;
         f.copy_w = l.dX;
         f.copy_dy = !act;
       }
     }
-    if (!f.prod.fits) return OCC_E_SHAPE;
   }
   const size_t os = f.planes ? 2 : es, np = f.planes ? kPlanes : 1;   // of operands in the workspace
   f.ldd = piece_ld(wide, os);
   Carve c;
   if (f.has_dz || f.copy_dy) f.dz_off = c.take((size_t)l.tokens * f.ldd * os * np);
-  if (f.has_dz || l.dbias) {
+  if (f.has_dz || f.strip_bias) {
     // enough blocks to fill the chip several times, whole groups of rows in
     // each; fewer, longer strips where their sums have to be added
-    const int64_t across = div_up(l.out, DZ_LANES * 4), most = l.dbias ? 2048 : 8192;
+    const int64_t across = div_up(l.out, DZ_LANES * 4), most = f.strip_bias ? 2048 : 8192;
     const int64_t down = std::max<int64_t>(1, std::min<int64_t>(div_up(most, across), div_up(l.tokens, DZ_ROWS)));
     f.strip = up(div_up(l.tokens, down), DZ_ROWS);
     f.strips = div_up(l.tokens, f.strip);
     if (across * f.strips >= ((int64_t)1 << 30)) return OCC_E_SHAPE;
-    if (l.dbias) f.bias_off = c.take((size_t)f.strips * wide * 4);
+    if (f.strip_bias) f.bias_off = c.take((size_t)f.strips * wide * 4);
   }
   if (f.copy_w) f.w_off = c.take((size_t)wide * piece_ld(l.in, os) * os * np);
   if (f.copy_x) f.x_off = c.take((size_t)l.tokens * piece_ld(l.in, os) * os * np);
@@ -527,7 +585,7 @@ occ_status_t run_bwd(const occ_linear_grad_t& l, const BwdPlan& f, bool accumula
     d.ldz = l.ldz;
     d.dZ = f.has_dz ? ws + f.dz_off : nullptr;
     d.ldd = f.ldd;
-    d.bias_part = l.dbias ? (float*)(ws + f.bias_off) : nullptr;
+    d.bias_part = f.strip_bias ? (float*)(ws + f.bias_off) : nullptr;
     d.tokens = (int32_t)l.tokens;
     d.out = (int32_t)l.out;
     d.act = l.act;
@@ -536,6 +594,14 @@ occ_status_t run_bwd(const occ_linear_grad_t& l, const BwdPlan& f, bool accumula
     d.plane = f.planes && f.has_dz ? l.tokens * f.ldd : 0;
     prep.dz_blocks = (int32_t)(d.across * f.strips);
   }
+  DzSource src{};
+  src.dY = l.dY;
+  src.ldy = l.lddy;
+  src.Z = act ? l.Z : nullptr;
+  src.ldz = l.ldz;
+  src.out = (int32_t)l.out;
+  src.act = l.act;
+  src.gated = GATED;
   const void* dz = l.dY;
   int64_t ldd = l.lddy;
   if (f.has_dz || f.copy_dy) {
@@ -571,6 +637,7 @@ occ_status_t run_bwd(const occ_linear_grad_t& l, const BwdPlan& f, bool accumula
     g.C = l.dX;
     g.ldc = l.lddx;
     g.stream = stream && rows_on_lines(l.dX, l.lddx, l.in, sizeof(T));
+    g.dz = src;
     set_tiles(g, f.prod.x, ws + f.dx_part);
     a.dx_blocks = (int32_t)f.prod.x.blocks();
   }
@@ -591,24 +658,30 @@ occ_status_t run_bwd(const occ_linear_grad_t& l, const BwdPlan& f, bool accumula
     g.c_f32 = l.dw_dtype == OCC_F32;
     g.accumulate = accumulate;
     g.stream = stream && rows_on_lines(l.dW, l.lddw, l.in, elem_size(l.dw_dtype));
+    g.dz = src;
     set_tiles(g, f.prod.w, ws + f.dw_part);
     a.dw_blocks = (int32_t)f.prod.w.blocks();
   }
   int64_t bias_blocks = 0;
   if (l.dbias) {
-    a.bias.part = (const float*)(ws + f.bias_off);
+    a.bias.part = f.strip_bias ? (const float*)(ws + f.bias_off) : nullptr;
     a.bias.dbias = l.dbias;
     a.bias.width = wide;
     a.bias.strips = (int32_t)f.strips;
     a.bias.accumulate = accumulate;
-    bias_blocks = div_up(wide, 64);
+    a.bias.src = src;
+    a.bias.tokens = (int32_t)l.tokens;
+    bias_blocks = f.strip_bias ? div_up(wide, 64) : div_up(l.out, BD_COLS);
   }
   const int64_t blocks = (int64_t)a.dx_blocks + a.dw_blocks + bias_blocks;
   if (!a.dx_blocks && !a.dw_blocks)
     return launch("layer_bias", s, [&] {
-      hipLaunchKernelGGL(k_bias, dim3((unsigned)bias_blocks), dim3(512), 0, s, a.bias);
+      hipLaunchKernelGGL((k_bias<T>), dim3((unsigned)bias_blocks), dim3(512), 0, s, a.bias);
     });
   const dim3 grid((unsigned)blocks), block(512);
+  auto direct = [&] {
+    return launch("layer_bwd", s, [&] { hipLaunchKernelGGL((k_backward_direct<T>), grid, block, 0, s, a); });
+  };
   auto products = [&](auto operand) {
     using TI = decltype(operand);
     return launch("layer_bwd", s, [&] {
@@ -619,7 +692,8 @@ occ_status_t run_bwd(const occ_linear_grad_t& l, const BwdPlan& f, bool accumula
       }
     });
   };
-  if (f.planes) OCC_TRY(products(uint16_t{}));
+  if (f.direct) OCC_TRY(direct());
+  else if (f.planes) OCC_TRY(products(uint16_t{}));
   else OCC_TRY(products(T{}));
   const unsigned jx = l.dX && a.dx.splits > 1 ? join_blocks(a.dx) : 0;
   const unsigned jw = l.dW && a.dw.splits > 1 ? join_blocks(a.dw) : 0;
