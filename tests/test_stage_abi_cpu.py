@@ -91,7 +91,7 @@ def test_backward_refusals(L, change, code):
 
 
 def test_workspaces(L):
-    g = grad()
+    g = grad(tokens=50000)
     need = L.occ_linear_bwd_workspace_bytes(ctypes.byref(g))
     assert need > 0 and need % 256 == 0
     assert L.occ_gated_bwd_workspace_bytes(ctypes.byref(g)) > need
@@ -104,8 +104,12 @@ def test_workspaces(L):
     # invalid arguments have no workspace; few tokens need none
     assert L.occ_linear_bwd_workspace_bytes(ctypes.byref(grad(out=0))) == 0
     assert L.occ_linear_fwd_workspace_bytes(ctypes.byref(layer(tokens=4))) == 0
-    # rows off 16 bytes are copied
-    a, b = layer(), layer(X=BASE + 2)
+    # a small layer takes its operands as they lie
+    assert L.occ_linear_fwd_workspace_bytes(ctypes.byref(layer(X=BASE + 2))) == 0
+    assert L.occ_linear_bwd_workspace_bytes(ctypes.byref(grad())) == 0
+    # in a large one, rows off 16 bytes are copied
+    large = dict(tokens=8192, in_=2048, out=2048, ldx=2048, ldw=2048, ldr=2048, ldy=2048, ldz=2048)
+    a, b = layer(**large), layer(**large, X=BASE + 2)
     assert L.occ_linear_fwd_workspace_bytes(ctypes.byref(b)) > \
         L.occ_linear_fwd_workspace_bytes(ctypes.byref(a))
 
