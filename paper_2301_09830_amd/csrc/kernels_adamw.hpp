@@ -36,31 +36,36 @@ struct AdamTensor {
   void* v;
   float* m_scale;       // 8-bit moments: rows x ceil(cols / 256)
   float* v_scale;
-  int64_t ldg;
-  int32_t rows, cols, rank;
-  int32_t block0;       // first block of this tensor in the launch
+  int64_t ldg;          // of G; of factors: their rank
+  int32_t rows, cols;
   float keep;
   uint32_t key;         // of the tensor's random bits
 };
 
-constexpr int kAdamTensors = 30;   // of one launch: their descriptors are kernel arguments
+// Tensors of one launch.  Their descriptors are kernel arguments, 4 KB of them.
+constexpr int kAdamTensors = 40;
 
 struct AdamArgs {
   AdamTensor t[kAdamTensors];
-  int32_t count;
+  int32_t start[kAdamTensors];   // first block of each tensor; behind the last one INT_MAX
   float b1, c1, b2, c2;   // c1 = 1 - b1, c2 = 1 - b2
   float a, c, eps;
   const float* grad_scale;   // device scalar, or null
   const uint32_t* flags;     // device word, or null: FLAG 1 set = leave everything as it is
 };
+static_assert(sizeof(AdamArgs) <= 4096, "kernel arguments");
 
+// The tensor of a block: which eight, then which of them, so that it waits
+// for the arguments' memory twice (a step of 56 tensors, 6.3M elements, 20.9 us;
+// by halves, 30 tensors a launch, 28.5).
 __device__ __forceinline__ int adam_tensor(const AdamArgs& g, int b) {
-  int lo = 0, hi = g.count - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (g.t[mid].block0 <= b) lo = mid; else hi = mid - 1;
-  }
-  return lo;
+  int n = 0;
+#pragma unroll
+  for (int i = 8; i < kAdamTensors; i += 8) n += g.start[i] <= b ? 8 : 0;
+  const int32_t* const p = g.start + n;
+#pragma unroll
+  for (int i = 1; i < 8; ++i) n += p[i] <= b ? 1 : 0;
+  return n;
 }
 
 // sqrt(x) to nearest: the hardware's result (1 ulp) against its neighbours, by
@@ -187,10 +192,11 @@ __device__ __forceinline__ f32x4_t ld_grad(const AdamTensor& t, int64_t e, int l
 template <class TG, bool NT>
 __global__ __launch_bounds__(256) void k_adamw32(AdamArgs g) {
   if (g.flags && (*g.flags & 1u)) return;
-  const AdamTensor& t = g.t[adam_tensor(g, blockIdx.x)];
+  const int index = adam_tensor(g, blockIdx.x);
+  const AdamTensor& t = g.t[index];
   const float scale = g.grad_scale ? *g.grad_scale : 1.0f;
   const int64_t total = (int64_t)t.rows * t.cols;
-  const int64_t e = (int64_t)((int)blockIdx.x - t.block0) * AD_BLOCK + threadIdx.x * 4;
+  const int64_t e = (int64_t)((int)blockIdx.x - g.start[index]) * AD_BLOCK + threadIdx.x * 4;
   if (e >= total) return;
   const int left = (int)min((int64_t)4, total - e);
   float* const M = (float*)t.m + e;
@@ -207,8 +213,9 @@ __global__ __launch_bounds__(256) void k_adamw32(AdamArgs g) {
 // ----------------------------------------------------------------------------
 // stored gradients, 8-bit moments: a wave takes runs of 256 columns
 // ----------------------------------------------------------------------------
-// Two runs a wave (403M elements on bf16 gradients, 16 bytes each, 1.21 ms =
-// 5.4 TB/s; four runs 1.20 ms, but 61 against 55 us for 12.6M elements).
+// Two runs a wave (403M elements on bf16 gradients, 16 bytes each, 1.14 ms =
+// 5.7 TB/s; four runs are as fast, but 10 % slower for 12.6M elements).  Bound
+// by memory, closely followed by the instructions of the two encodings.
 constexpr int AD8_RUNS = 2;                    // runs of a wave
 constexpr int AD8_BLOCK = 4 * AD8_RUNS;        // runs of a block
 
@@ -281,12 +288,13 @@ struct Adam8Run {
 template <class TG, bool NT>
 __global__ __launch_bounds__(256) void k_adamw8(AdamArgs g) {
   if (g.flags && (*g.flags & 1u)) return;
-  const AdamTensor& t = g.t[adam_tensor(g, blockIdx.x)];
+  const int index = adam_tensor(g, blockIdx.x);
+  const AdamTensor& t = g.t[index];
   const float scale = g.grad_scale ? *g.grad_scale : 1.0f;
   const int lane = threadIdx.x & 63;
   const int per_row = (t.cols + kRun - 1) / kRun;
   const int64_t runs = (int64_t)t.rows * per_row;
-  const int64_t r0 = (int64_t)((int)blockIdx.x - t.block0) * AD8_BLOCK + wave_id() * AD8_RUNS;
+  const int64_t r0 = (int64_t)((int)blockIdx.x - g.start[index]) * AD8_BLOCK + wave_id() * AD8_RUNS;
   if (r0 >= runs) return;
   int64_t row = runs >> 31 ? r0 / per_row : (int64_t)((uint32_t)r0 / (uint32_t)per_row);
   int b = (int)(r0 - row * per_row);
@@ -320,7 +328,7 @@ __global__ __launch_bounds__(256) void k_adamw8(AdamArgs g) {
 // 64 columns at a time they are turned through LDS, so that W and the moments
 // are read and written in runs of 256 bytes of a row (16 runs of 64 bytes at a
 // power of two apart meet in one memory channel: 2.8 ms for the 403M elements
-// of eight layers of width 2048 at rank 32, 2.1 ms this way).  The first
+// of eight layers of width 2048 at rank 32, 1.99 ms this way, 5.3 TB/s).  The first
 // columns' W and moments are asked for before the products, each next 64
 // columns' while the present ones are worked on.
 constexpr int ADF_WAVES = 8;
@@ -338,6 +346,7 @@ template <int BITS, bool NT, bool FULL>
 __device__ __forceinline__ void adamw_factors(const AdamArgs& g, const AdamTensor& t, int rb, int run, int per_row,
                                               f32x4_t* qs, f32x4_t (*turn)[16 * 16]) {
   const float scale = g.grad_scale ? *g.grad_scale : 1.0f;
+  const int rank = (int)t.ldg;
   const int wave = wave_id(), lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
   const int row0 = rb * ADF_ROWS + wave * 16;
   const int c0 = run * kRun;
@@ -376,7 +385,7 @@ __device__ __forceinline__ void adamw_factors(const AdamArgs& g, const AdamTenso
   f32x4_t acc[16];
 #pragma unroll
   for (int f = 0; f < 16; ++f) acc[f] = f32x4_t{};
-  const float* const prow = t.P + (int64_t)min(row0 + i, t.rows - 1) * t.rank;
+  const float* const prow = t.P + (int64_t)min(row0 + i, t.rows - 1) * rank;
   // thread: pieces of 4 ranks of rows threadIdx / 8 + 64 u of the run's Q
   constexpr int QN = kRun * ADF_RANKS / 4 / (ADF_WAVES * 64);
   const int qr = threadIdx.x >> 3, qc = threadIdx.x & 7;
@@ -384,14 +393,14 @@ __device__ __forceinline__ void adamw_factors(const AdamArgs& g, const AdamTenso
   auto load_q = [&](int k) {
 #pragma unroll
     for (int u = 0; u < QN; ++u)
-      qn[u] = ld_quad<float>(t.Q + (int64_t)min(c0 + qr + u * (ADF_WAVES * 8), t.cols - 1) * t.rank + k + 4 * qc,
-                             t.rank - k - 4 * qc);
+      qn[u] = ld_quad<float>(t.Q + (int64_t)min(c0 + qr + u * (ADF_WAVES * 8), t.cols - 1) * rank + k + 4 * qc,
+                             rank - k - 4 * qc);
   };
   load_q(0);
-  for (int k = 0; k < t.rank; k += ADF_RANKS) {
+  for (int k = 0; k < rank; k += ADF_RANKS) {
     f32x4_t pv[2];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) pv[s] = ld_quad<float>(prow + k + 16 * s + 4 * q, t.rank - k - 16 * s - 4 * q);
+    for (int s = 0; s < 2; ++s) pv[s] = ld_quad<float>(prow + k + 16 * s + 4 * q, rank - k - 16 * s - 4 * q);
     if (k) __syncthreads();
 #pragma unroll
     for (int u = 0; u < QN; ++u) {
@@ -399,10 +408,10 @@ __device__ __forceinline__ void adamw_factors(const AdamArgs& g, const AdamTenso
       qs[r * 8 + (qc ^ (r & 7))] = qn[u];
     }
     __syncthreads();
-    if (k + ADF_RANKS < t.rank) load_q(k + ADF_RANKS);
+    if (k + ADF_RANKS < rank) load_q(k + ADF_RANKS);
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      if (k + 16 * s >= t.rank) continue;
+      if (k + 16 * s >= rank) continue;
 #pragma unroll
       for (int f = 0; f < 16; ++f) {
         const f32x4_t qv = qs[(16 * f + i) * 8 + ((4 * s + q) ^ (i & 7))];
@@ -491,9 +500,10 @@ __global__ __launch_bounds__(ADF_WAVES * 64) void k_adamw_factors(AdamArgs g) {
   if (g.flags && (*g.flags & 1u)) return;
   __shared__ f32x4_t qs[kRun * ADF_RANKS / 4];
   __shared__ f32x4_t turn[ADF_WAVES][16 * 16];
-  const AdamTensor& t = g.t[adam_tensor(g, blockIdx.x)];
+  const int index = adam_tensor(g, blockIdx.x);
+  const AdamTensor& t = g.t[index];
   const int per_row = (t.cols + kRun - 1) / kRun;
-  const int b = (int)blockIdx.x - t.block0;
+  const int b = (int)blockIdx.x - g.start[index];
   const int rb = b / per_row, run = b - rb * per_row;
   if ((rb + 1) * ADF_ROWS <= t.rows && (run + 1) * kRun <= t.cols)
     adamw_factors<BITS, NT, true>(g, t, rb, run, per_row, qs, turn);
