@@ -56,7 +56,7 @@ struct AdamArgs {
 static_assert(sizeof(AdamArgs) <= 4096, "kernel arguments");
 
 // The tensor of a block: which eight, then which of them, so that it waits
-// for the arguments' memory twice (a step of 56 tensors, 6.3M elements, 20.9 us;
+// for the arguments' memory twice (a step of 70 tensors, 3.1M elements, 20.9 us;
 // by halves, 30 tensors a launch, 28.5).
 __device__ __forceinline__ int adam_tensor(const AdamArgs& g, int b) {
   int n = 0;

@@ -402,3 +402,47 @@ def test_fp32_planes_of_the_largest_values():
     y, _, by, _ = forward64(X[keep], W, None, 0, None, False)
     within(Y[keep], y, by, "Y")
     assert torch.isnan(Y[9]).all()
+
+
+# Small layers take their operands as they lie (no workspace); larger ones make
+# dZ and aligned copies first.  Above 1024 tokens the bias gradient is summed in
+# strips.  Both sides at odd widths, where pieces of 16 bytes end inside rows and
+# gated ones hold columns of both projections.
+FORMS = [(1024, 65, 131), (1025, 65, 131), (1024, 7, 1), (1025, 3, 2), (90, 1531, 37),
+         (1300, 1021, 1535), (2500, 517, 1999)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("size", FORMS, ids=lambda s: "x".join(map(str, s)))
+def test_forms_of_the_products(size, gated, dtype):
+    run_backward(*size, dtype, act=3, gated=gated, seed=sum(size))
+    run_backward(*size, dtype, act=1, gated=gated, pad=3, shift=1, accumulate=True)
+    if not gated:
+        run_backward(*size, dtype, act=0, gated=False, pad=1)
+    run_forward(*size, dtype, act=4, gated=gated, pad=1, shift=3)
+
+
+def test_workspaces_of_both_forms():
+    def need(tokens, width):
+        a = optcc.occ_linear_grad_t(optcc.OCC_BF16, optcc.OCC_BF16, 2, 0, tokens, width, width, 4096,
+                                    width, 4096, width, 4096, width, 4096, width, 4096, width, 4096,
+                                    width, None)
+        return optcc.lib().occ_linear_bwd_workspace_bytes(a)
+    assert need(64, 64) == 0 and need(2500, 2048) >= 2500 * 2048 * 2
+
+
+@pytest.mark.parametrize("tokens", [40, 1500])
+def test_infinities_behind_an_edge_do_not_count(tokens):
+    """What lies between the rows of every operand is NaN (rand), and a zero
+    gradient times a finite act' is zero: no NaN reaches a result."""
+    for gated in (False, True):
+        g = gen(9)
+        wide = 2 * 37 if gated else 37
+        dY = rand(g, tokens, 37, torch.bfloat16, 0.0, pad=5, shift=1)
+        X, W = rand(g, tokens, 41, torch.bfloat16, pad=7), rand(g, wide, 41, torch.bfloat16, pad=3)
+        Z = rand(g, tokens, wide, torch.bfloat16, 50.0, pad=9, shift=3)
+        dX, dW = torch.full_like(X, 7.0), torch.full_like(W, 7.0)
+        db = torch.full((wide,), 7.0, device="cuda")
+        (optcc.occ_gated_bwd if gated else optcc.occ_linear_bwd)(dY, X, W, Z=Z, act=2, dX=dX, dW=dW, dbias=db)
+        assert not dX.any() and not dW.any() and not db.any()
