@@ -11,7 +11,7 @@
 // it is read from LDS (ds_read_b64_tr_b16, or single words for fp32).  Pieces
 // of 16 bytes are exchanged within a row (on the global side of the DMA, so
 // that LDS is written in order) such that the lanes of a read meet no bank
-// twice (no conflict cycles counted in any form).
+// twice (no conflict cycles counted in the products).
 //
 // Bound by the matrix units and what keeps them fed: bf16 8192^3 runs forward
 // at 1510 TFLOP/s, both gradients at 1330 (K strided takes twice the LDS reads
