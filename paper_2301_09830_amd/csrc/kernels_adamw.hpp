@@ -331,6 +331,8 @@ __global__ __launch_bounds__(256) void k_adamw8(AdamArgs g) {
 // of eight layers of width 2048 at rank 32, 1.99 ms this way, 5.3 TB/s).  The first
 // columns' W and moments are asked for before the products, each next 64
 // columns' while the present ones are worked on.
+// With fp32 moments, which have no runs, a block may take 64 columns (NJ = 1):
+// twice the waves a SIMD, and four times the blocks where there are few.
 constexpr int ADF_WAVES = 8;
 constexpr int ADF_ROWS = 16 * ADF_WAVES;
 constexpr int ADF_RANKS = 32;
@@ -341,16 +343,18 @@ struct AdamPiece {   // 4 rows x 4 columns of a lane, 4 rows apart
   uint32_t cm[4], cv[4];
 };
 
-// Rows 128 rb .. and run `run` of a tensor.  FULL: all of them are there.
-template <int BITS, bool NT, bool FULL>
+// Rows 128 rb .. and columns 64 NJ run .. of a tensor.  FULL: all of them are there.
+template <int BITS, bool NT, bool FULL, int NJ>
 __device__ __forceinline__ void adamw_factors(const AdamArgs& g, const AdamTensor& t, int rb, int run, int per_row,
                                               f32x4_t* qs, f32x4_t (*turn)[16 * 16]) {
+  constexpr int COLS = 64 * NJ;
+  static_assert(BITS == 32 || COLS == kRun, "scales of whole runs");
   const float scale = g.grad_scale ? *g.grad_scale : 1.0f;
   const int rank = (int)t.ldg;
   const int wave = wave_id(), lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
   const int row0 = rb * ADF_ROWS + wave * 16;
-  const int c0 = run * kRun;
-  const int cols_left = FULL ? kRun : t.cols - c0;
+  const int c0 = run * COLS;
+  const int cols_left = FULL ? COLS : t.cols - c0;
   auto left_of = [&](int row, int j) { return FULL ? 4 : row < t.rows ? cols_left - 64 * j - 4 * i : 0; };
 
   // rows row0 + 4 k + q, columns c0 + 64 j + 4 i of piece j
@@ -382,12 +386,12 @@ __device__ __forceinline__ void adamw_factors(const AdamArgs& g, const AdamTenso
     }
   }
 
-  f32x4_t acc[16];
+  f32x4_t acc[4 * NJ];
 #pragma unroll
-  for (int f = 0; f < 16; ++f) acc[f] = f32x4_t{};
+  for (int f = 0; f < 4 * NJ; ++f) acc[f] = f32x4_t{};
   const float* const prow = t.P + (int64_t)min(row0 + i, t.rows - 1) * rank;
   // thread: pieces of 4 ranks of rows threadIdx / 8 + 64 u of the run's Q
-  constexpr int QN = kRun * ADF_RANKS / 4 / (ADF_WAVES * 64);
+  constexpr int QN = COLS * ADF_RANKS / 4 / (ADF_WAVES * 64);
   const int qr = threadIdx.x >> 3, qc = threadIdx.x & 7;
   f32x4_t qn[QN];
   auto load_q = [&](int k) {
@@ -413,7 +417,7 @@ __device__ __forceinline__ void adamw_factors(const AdamArgs& g, const AdamTenso
     for (int s = 0; s < 2; ++s) {
       if (k + 16 * s >= rank) continue;
 #pragma unroll
-      for (int f = 0; f < 16; ++f) {
+      for (int f = 0; f < 4 * NJ; ++f) {
         const f32x4_t qv = qs[(16 * f + i) * 8 + ((4 * s + q) ^ (i & 7))];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -423,11 +427,11 @@ __device__ __forceinline__ void adamw_factors(const AdamArgs& g, const AdamTenso
   }
 
   float tm[4] = {}, tv[4] = {};
-  f32x4_t ms[BITS == 8 ? 4 : 1][4], roots[BITS == 8 ? 4 : 1][4];
+  f32x4_t ms[BITS == 8 ? NJ : 1][4], roots[BITS == 8 ? NJ : 1][4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
+  for (int j = 0; j < NJ; ++j) {
     if (64 * j >= cols_left) continue;
-    if (j < 3 && 64 * (j + 1) < cols_left) load(next, j + 1);
+    if (j < NJ - 1 && 64 * (j + 1) < cols_left) load(next, j + 1);
 #pragma unroll
     for (int f = 0; f < 4; ++f) turn[wave][i * 16 + ((4 * f + q) ^ i)] = acc[4 * j + f];
     __builtin_amdgcn_wave_barrier();
@@ -467,7 +471,7 @@ __device__ __forceinline__ void adamw_factors(const AdamArgs& g, const AdamTenso
         roots[j][k] = root;
       }
     }
-    now = next;
+    if constexpr (NJ > 1) now = next;
   }
   if constexpr (BITS == 8) {
 #pragma unroll
@@ -477,7 +481,7 @@ __device__ __forceinline__ void adamw_factors(const AdamArgs& g, const AdamTenso
       const float im = (1.0f / tm[k]) * 448.0f, iv = (1.0f / tv[k]) * 448.0f;
       const int row = row0 + 4 * k + q;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < NJ; ++j) {
         if (64 * j >= cols_left) continue;
         const int64_t e = (int64_t)row * t.cols + c0 + 64 * j + 4 * i;
         const int left = left_of(row, j);
@@ -495,20 +499,21 @@ __device__ __forceinline__ void adamw_factors(const AdamArgs& g, const AdamTenso
   }
 }
 
-template <int BITS, bool NT>
+template <int BITS, bool NT, int NJ>
 __global__ __launch_bounds__(ADF_WAVES * 64) void k_adamw_factors(AdamArgs g) {
   if (g.flags && (*g.flags & 1u)) return;
-  __shared__ f32x4_t qs[kRun * ADF_RANKS / 4];
+  constexpr int COLS = 64 * NJ;
+  __shared__ f32x4_t qs[COLS * ADF_RANKS / 4];
   __shared__ f32x4_t turn[ADF_WAVES][16 * 16];
   const int index = adam_tensor(g, blockIdx.x);
   const AdamTensor& t = g.t[index];
-  const int per_row = (t.cols + kRun - 1) / kRun;
+  const int per_row = (t.cols + COLS - 1) / COLS;
   const int b = (int)blockIdx.x - g.start[index];
   const int rb = b / per_row, run = b - rb * per_row;
-  if ((rb + 1) * ADF_ROWS <= t.rows && (run + 1) * kRun <= t.cols)
-    adamw_factors<BITS, NT, true>(g, t, rb, run, per_row, qs, turn);
+  if ((rb + 1) * ADF_ROWS <= t.rows && (run + 1) * COLS <= t.cols)
+    adamw_factors<BITS, NT, true, NJ>(g, t, rb, run, per_row, qs, turn);
   else
-    adamw_factors<BITS, NT, false>(g, t, rb, run, per_row, qs, turn);
+    adamw_factors<BITS, NT, false, NJ>(g, t, rb, run, per_row, qs, turn);
 }
 
 }  // namespace occ

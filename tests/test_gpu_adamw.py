@@ -308,3 +308,25 @@ def test_repeats_streams_and_graphs():
         torch.cuda.synchronize()
         for x, y, z in zip(buffers(a), buffers(b), buffers(c)):
             assert torch.equal(x, y) and torch.equal(x, z)
+
+
+@pytest.mark.parametrize("shift", [0, 1])
+def test_factors_of_many_whole_runs(shift):
+    """Enough blocks of 256 columns for the wide form, its last rows ragged; on
+    and off 64 bytes."""
+    s = State(8262, 16384, 32, "factors", seed=shift, shift=shift, rank=20)
+    ref = s.reference(step=3)
+    print(f"adamw 8262x16384 factors shift {shift}", flush=True)
+    optcc.occ_adamw_step([s.param()], LR, 3, B1, B2, EPS)
+    check(s, ref, f"wide, shift {shift}")
+
+
+@pytest.mark.parametrize("grads", ["f32", "bf16", "factors"])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_more_than_the_caches_hold(bits, grads):
+    """Streams past the caches: 14.6M elements whose rows start on 64 bytes."""
+    s = State(12301, 1184, bits, grads, seed=bits, rank=40)
+    ref = s.reference(step=3)
+    print(f"adamw 12301x1184 {bits} {grads}", flush=True)
+    optcc.occ_adamw_step([s.param()], LR, 3, B1, B2, EPS)
+    check(s, ref, f"streams {bits} {grads}")
