@@ -90,6 +90,14 @@ struct Call {
     return (float*)t->data_ptr();
   }
 
+  // The caller's workspace: its bytes are counted, so there are no gaps in it.
+  const at::Tensor* workspace(const at::Tensor* t, const char* name) const {
+    if (!t) return nullptr;
+    if (!t->is_contiguous()) refuse(PyExc_ValueError, "%s must be contiguous", name);
+    if (t->device() != device) refuse(PyExc_ValueError, "%s lies on another device", name);
+    return t;
+  }
+
   occ_stream_t stream() const {
     if (!device.is_cuda()) refuse(PyExc_ValueError, "%s", "the tensors must lie on a GPU");
     PyObject* const index = PyLong_FromLong(device.index());
@@ -161,8 +169,9 @@ PyObject* forward(PyObject*, PyObject* const* v, Py_ssize_t n) {
     a.R = c(tensor(v[5], "R"), "R", tokens, out, a.ldr);
     a.Z = c(tensor(v[7], "Z"), "Z", tokens, rows, a.ldz);
     a.bias = c.vector(tensor(v[3], "bias"), "bias", rows);
+    const at::Tensor* const given = c.workspace(tensor(v[8], "ws"), "ws");
     const occ_stream_t s = c.stream();
-    const Workspace ws(lib.fwd_size[gated](&a), tensor(v[8], "ws"), X.device());
+    const Workspace ws(lib.fwd_size[gated](&a), given, X.device());
     return PyLong_FromLong(lib.fwd[gated](&a, ws.p, ws.bytes, s));
   });
 }
@@ -198,8 +207,9 @@ PyObject* backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
     a.dX = c(dX, "dX", tokens, in, a.lddx);
     a.dW = c(dW, "dW", rows, in, wide, a.lddw);
     a.dbias = c.vector(dbias, "dbias", rows);
+    const at::Tensor* const given = c.workspace(tensor(v[10], "ws"), "ws");
     const occ_stream_t s = c.stream();
-    const Workspace ws(lib.bwd_size[gated](&a), tensor(v[10], "ws"), dY.device());
+    const Workspace ws(lib.bwd_size[gated](&a), given, dY.device());
     return PyLong_FromLong(lib.bwd[gated](&a, flags, ws.p, ws.bytes, s));
   });
 }
