@@ -690,6 +690,8 @@ def make_param(W, m, v, G=None, P=None, Q=None, W16=None, m_scale=None, v_scale=
             raise ValueError(f"{name} must hold {n} contiguous values")
         return t.data_ptr()
 
+    given = {"W": W, "m": m, "v": v, "G": G, "P": P, "Q": Q, "W16": W16, "m_scale": m_scale,
+             "v_scale": v_scale}
     a = occ_param_t()
     a.rows, a.cols = rows, cols
     a.W = whole(W, "W", rows * cols, torch.float32)
@@ -718,6 +720,11 @@ def make_param(W, m, v, G=None, P=None, Q=None, W16=None, m_scale=None, v_scale=
         a.m_scale = whole(m_scale, "m_scale", n, torch.float32)
         a.v_scale = whole(v_scale, "v_scale", n, torch.float32)
     a.decay = float(decay)
+    for name, t in given.items():
+        if t is not None and t.device != W.device:
+            raise ValueError(f"{name} lies on another device than W")
+    if not W.is_cuda:
+        raise ValueError("the tensors must lie on a GPU")
     return a
 
 
@@ -735,6 +742,9 @@ def occ_adamw_step(params, lr: float, step: int, beta1: float = 0.9, beta2: floa
     CUDA tensor of one value; flags: int32 CUDA tensor of one value."""
     if not isinstance(params, ctypes.Array):
         params = make_params(params)
+    for name, t in (("grad_scale", grad_scale), ("flags", flags)):
+        if t is not None and not t.is_cuda:
+            raise ValueError(f"{name} must lie on a GPU")
     h = occ_adamw_t(lr, beta1, beta2, eps, step, seed & 0xFFFFFFFF, 0,
                     None if grad_scale is None else _vec(grad_scale, "grad_scale", 1), None)
     if flags is not None:

@@ -32,3 +32,50 @@ def test_workspace_must_be_a_tensor():
     for call in layer_calls(4096):
         with pytest.raises(TypeError, match="ws must be a tensor"):
             call()
+
+
+# --- the optimizer's tensors ---------------------------------------------------
+class OnGpu(torch.Tensor):
+    """A host tensor that says it lies on a GPU, for checks that never read it."""
+    is_cuda = True
+    device = torch.device("cuda", 0)
+
+
+def gpu(*shape, dtype=torch.float32):
+    return torch.zeros(*shape, dtype=dtype).as_subclass(OnGpu)
+
+
+def tensors(rows=6, cols=300, bits=8, factors=False, make=gpu):
+    """The arguments of make_param."""
+    state = torch.uint8 if bits == 8 else torch.float32
+    t = {"W": make(rows, cols), "m": make(rows, cols, dtype=state),
+         "v": make(rows, cols, dtype=state), "W16": make(rows, cols, dtype=torch.bfloat16)}
+    if factors:
+        t["P"], t["Q"] = make(rows, 4), make(cols, 4)
+    else:
+        t["G"] = make(rows, cols)
+    if bits == 8:
+        t["m_scale"], t["v_scale"] = make(rows, 2), make(rows, 2)
+    return t
+
+
+@pytest.mark.parametrize("factors", [False, True])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_parameters_lie_on_one_gpu(bits, factors):
+    optcc.make_param(**tensors(bits=bits, factors=factors))
+    for name in tensors(bits=bits, factors=factors):
+        t = tensors(bits=bits, factors=factors)
+        t[name] = torch.zeros_like(t[name].as_subclass(torch.Tensor))      # on the host
+        with pytest.raises(ValueError, match="another device"):
+            optcc.make_param(**t)
+    with pytest.raises(ValueError, match="must lie on a GPU"):
+        optcc.make_param(**tensors(bits=bits, factors=factors, make=torch.zeros))
+
+
+def test_scale_and_flags_lie_on_a_gpu():
+    """A list of no tensors is refused by the library, after the binding's checks."""
+    none = (optcc.occ_param_t * 0)()
+    with pytest.raises(ValueError, match="grad_scale must lie on a GPU"):
+        optcc.occ_adamw_step(none, 1e-3, 1, grad_scale=torch.ones(1))
+    with pytest.raises(ValueError, match="flags must lie on a GPU"):
+        optcc.occ_adamw_step(none, 1e-3, 1, flags=torch.zeros(1, dtype=torch.int32))
