@@ -681,21 +681,24 @@ def make_param(W, m, v, G=None, P=None, Q=None, W16=None, m_scale=None, v_scale=
         raise ValueError("W must be 1-D or 2-D")
     rows, cols = shape
 
-    def whole(t, name, n, *dtypes):
+    def whole(t, name, of, *dtypes):   # flat, or a matrix of this shape
         if t is None:
             return None
+        n = of[0] * of[1]
         if t.dtype not in dtypes:
             raise TypeError(f"{name} must be {' or '.join(map(str, dtypes))}")
         if t.numel() != n or not t.is_contiguous():
             raise ValueError(f"{name} must hold {n} contiguous values")
+        if t.dim() == 2 and 1 not in t.shape and tuple(t.shape) != of:
+            raise ValueError(f"{name} must be {of[0]} x {of[1]}")
         return t.data_ptr()
 
     given = {"W": W, "m": m, "v": v, "G": G, "P": P, "Q": Q, "W16": W16, "m_scale": m_scale,
              "v_scale": v_scale}
     a = occ_param_t()
     a.rows, a.cols = rows, cols
-    a.W = whole(W, "W", rows * cols, torch.float32)
-    a.W16 = whole(W16, "W16", rows * cols, torch.bfloat16)
+    a.W = whole(W, "W", shape, torch.float32)
+    a.W16 = whole(W16, "W16", shape, torch.bfloat16)
     if G is not None:
         if P is not None or Q is not None:
             raise ValueError("give G, or P and Q")
@@ -704,21 +707,24 @@ def make_param(W, m, v, G=None, P=None, Q=None, W16=None, m_scale=None, v_scale=
             raise ValueError(f"G must be {rows} x {cols}")
         a.G, a.ldg, a.g_dtype = G2.data_ptr(), _ld(G2, "G"), _mdtype(G2)
     elif P is not None and Q is not None:
+        if P.dim() != 2 or Q.dim() != 2 or P.shape[0] != rows or Q.shape[0] != cols \
+                or P.shape[1] != Q.shape[1]:
+            raise ValueError("P must be rows x rank and Q cols x rank")
         a.rank = P.shape[1]
-        a.P = whole(P, "P", rows * a.rank, torch.float32)
-        a.Q = whole(Q, "Q", cols * a.rank, torch.float32)
+        a.P = whole(P, "P", (rows, a.rank), torch.float32)
+        a.Q = whole(Q, "Q", (cols, a.rank), torch.float32)
     else:
         raise ValueError("give G, or P and Q")
     codes = (torch.float8_e4m3fn, torch.uint8)
     a.state_bits = 8 if m.dtype in codes else 32
     kinds = codes if a.state_bits == 8 else (torch.float32,)
-    a.m, a.v = whole(m, "m", rows * cols, *kinds), whole(v, "v", rows * cols, *kinds)
+    a.m, a.v = whole(m, "m", shape, *kinds), whole(v, "v", shape, *kinds)
     if a.state_bits == 8:
         if m_scale is None or v_scale is None:
             raise ValueError("8-bit moments need m_scale and v_scale")
-        n = rows * (-(-cols // OCC_SCALE_RUN))
-        a.m_scale = whole(m_scale, "m_scale", n, torch.float32)
-        a.v_scale = whole(v_scale, "v_scale", n, torch.float32)
+        runs = (rows, -(-cols // OCC_SCALE_RUN))
+        a.m_scale = whole(m_scale, "m_scale", runs, torch.float32)
+        a.v_scale = whole(v_scale, "v_scale", runs, torch.float32)
     a.decay = float(decay)
     for name, t in given.items():
         if t is not None and t.device != W.device:

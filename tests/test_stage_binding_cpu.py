@@ -79,3 +79,29 @@ def test_scale_and_flags_lie_on_a_gpu():
         optcc.occ_adamw_step(none, 1e-3, 1, grad_scale=torch.ones(1))
     with pytest.raises(ValueError, match="flags must lie on a GPU"):
         optcc.occ_adamw_step(none, 1e-3, 1, flags=torch.zeros(1, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("change", [
+    {"Q": (4, 300)}, {"P": (4, 6)}, {"P": (6, 5)}, {"Q": (300, 5)}, {"Q": (1200,)}, {"P": (24,)},
+    {"m": (300, 6)}, {"v": (300, 6)}, {"W16": (300, 6)}, {"m_scale": (2, 6)}, {"v_scale": (3, 4)}],
+    ids=str)
+def test_shapes_are_checked_not_counts(change):
+    """As many contiguous values in another shape mean another order: P^T, Q^T,
+    moments of the transposed weight."""
+    t = tensors(factors=True)
+    for name, shape in change.items():
+        t[name] = gpu(*shape, dtype=t[name].dtype)
+    with pytest.raises(ValueError):
+        optcc.make_param(**t)
+
+
+def test_flat_states_of_a_matrix_are_taken():
+    """The order of the values is the matrix's: so are rank = rows and cols."""
+    t = tensors(factors=True)
+    for name in ("m", "v", "W16", "m_scale", "v_scale"):
+        t[name] = t[name].view(-1)
+    assert optcc.make_param(**t).rank == 4
+    t["P"], t["Q"] = gpu(6, 6), gpu(300, 6)
+    assert optcc.make_param(**t).rank == 6
+    v = {k: x.view(-1) for k, x in tensors(rows=1).items()}      # a vector
+    assert optcc.make_param(**v).cols == 300
