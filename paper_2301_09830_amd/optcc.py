@@ -674,7 +674,9 @@ def make_param(W, m, v, G=None, P=None, Q=None, W16=None, m_scale=None, v_scale=
                decay: float = 0.0) -> occ_param_t:
     """One tensor of occ_adamw_step: float32 W (a matrix, or a vector), its
     gradient G (float32 or bfloat16) or the factors P and Q of one, and its
-    moments: float32, or float8_e4m3fn / uint8 codes with their scales."""
+    moments: float32, or float8_e4m3fn / uint8 codes with their scales.  The
+    result holds their addresses, and the tensors themselves so that they live
+    as long as it does."""
     torch = _torch()
     shape = (1, W.shape[0]) if W.dim() == 1 else tuple(W.shape)
     if len(shape) != 2:
@@ -731,13 +733,17 @@ def make_param(W, m, v, G=None, P=None, Q=None, W16=None, m_scale=None, v_scale=
             raise ValueError(f"{name} lies on another device than W")
     if not W.is_cuda:
         raise ValueError("the tensors must lie on a GPU")
+    a._tensors = tuple(given.values())   # they live as long as their addresses are held
     return a
 
 
 def make_params(params):
-    """The array occ_adamw_step takes, made once and kept while the tensors live."""
+    """The array occ_adamw_step takes, made once.  It keeps the tensors alive:
+    a tensor replaced in the program needs a new array."""
     items = list(params)
-    return (occ_param_t * len(items))(*items)
+    array = (occ_param_t * len(items))(*items)
+    array._params = items   # the structures are copied, what they keep is not
+    return array
 
 
 def occ_adamw_step(params, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.95,

@@ -1,6 +1,9 @@
 """What the Python binding of the stage operators refuses before a kernel sees
 it, and what it keeps alive.  Host checks: no GPU."""
 
+import gc
+import weakref
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -105,3 +108,20 @@ def test_flat_states_of_a_matrix_are_taken():
     assert optcc.make_param(**t).rank == 6
     v = {k: x.view(-1) for k, x in tensors(rows=1).items()}      # a vector
     assert optcc.make_param(**v).cols == 300
+
+
+def test_parameters_keep_their_tensors():
+    """Temporaries given to make_param live as long as the list of parameters."""
+    t = tensors()
+    gone = [weakref.ref(x) for x in t.values()]
+    p = optcc.make_param(**t)
+    del t
+    gc.collect()
+    assert all(r() is not None for r in gone)
+    array = optcc.make_params(q for q in [p])
+    del p
+    gc.collect()
+    assert all(r() is not None for r in gone)
+    del array
+    gc.collect()
+    assert all(r() is None for r in gone)
