@@ -7,6 +7,7 @@
 // The functions of liboptcc.so are handed over by address (setup), so that
 // this module and the rest of the binding use one loaded library.
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "optcc.h"
@@ -171,7 +172,9 @@ PyObject* forward(PyObject*, PyObject* const* v, Py_ssize_t n) {
     a.bias = c.vector(tensor(v[3], "bias"), "bias", rows);
     const at::Tensor* const given = c.workspace(tensor(v[8], "ws"), "ws");
     const occ_stream_t s = c.stream();
-    const Workspace ws(lib.fwd_size[gated](&a), given, X.device());
+    // a default stream's handle is null: it is the current GPU's
+    const c10::DeviceGuard current(c.device);
+    const Workspace ws(lib.fwd_size[gated](&a), given, c.device);
     return PyLong_FromLong(lib.fwd[gated](&a, ws.p, ws.bytes, s));
   });
 }
@@ -209,7 +212,9 @@ PyObject* backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
     a.dbias = c.vector(dbias, "dbias", rows);
     const at::Tensor* const given = c.workspace(tensor(v[10], "ws"), "ws");
     const occ_stream_t s = c.stream();
-    const Workspace ws(lib.bwd_size[gated](&a), given, dY.device());
+    // a default stream's handle is null: it is the current GPU's
+    const c10::DeviceGuard current(c.device);
+    const Workspace ws(lib.bwd_size[gated](&a), given, c.device);
     return PyLong_FromLong(lib.bwd[gated](&a, flags, ws.p, ws.bytes, s));
   });
 }

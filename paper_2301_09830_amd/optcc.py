@@ -13,6 +13,7 @@ is cols x rank, contiguous.  Work is enqueued on torch's current stream.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import re
@@ -743,6 +744,10 @@ def make_params(params):
     items = list(params)
     array = (occ_param_t * len(items))(*items)
     array._params = items   # the structures are copied, what they keep is not
+    devices = {p._tensors[0].device for p in items if hasattr(p, "_tensors")}
+    if len(devices) > 1:
+        raise ValueError("the tensors lie on different GPUs")
+    array._device = devices.pop() if devices else None
     return array
 
 
@@ -754,17 +759,26 @@ def occ_adamw_step(params, lr: float, step: int, beta1: float = 0.9, beta2: floa
     CUDA tensor of one value; flags: int32 CUDA tensor of one value."""
     if not isinstance(params, ctypes.Array):
         params = make_params(params)
+    device = getattr(params, "_device", None)   # None: structures of addresses alone
     for name, t in (("grad_scale", grad_scale), ("flags", flags)):
-        if t is not None and not t.is_cuda:
+        if t is None:
+            continue
+        if not t.is_cuda:
             raise ValueError(f"{name} must lie on a GPU")
+        if device is not None and t.device != device:
+            raise ValueError(f"{name} lies on another device than the tensors")
     h = occ_adamw_t(lr, beta1, beta2, eps, step, seed & 0xFFFFFFFF, 0,
                     None if grad_scale is None else _vec(grad_scale, "grad_scale", 1), None)
     if flags is not None:
         if flags.numel() != 1 or flags.element_size() != 4:
             raise ValueError("flags must be one 32-bit word")
         h.flags = flags.data_ptr()
-    _check("occ_adamw_step", lib().occ_adamw_step(params, len(params), ctypes.byref(h),
-                                                  _stream(stream)))
+    cuda = _torch().cuda
+    # a default stream's handle is null: it is the current GPU's
+    other = device is not None and device.index != cuda.current_device()
+    with cuda.device(device) if other else contextlib.nullcontext():
+        status = lib().occ_adamw_step(params, len(params), ctypes.byref(h), _stream(stream))
+    _check("occ_adamw_step", status)
 
 
 def occ_profile_begin() -> None:

@@ -125,3 +125,77 @@ def test_parameters_keep_their_tensors():
     del array
     gc.collect()
     assert all(r() is None for r in gone)
+
+
+# --- the GPU that a call runs on -----------------------------------------------
+class OnGpu1(OnGpu):
+    device = torch.device("cuda", 1)
+
+
+class Library:
+    """Takes the place of the library and notes the stream of each call."""
+
+    def __init__(self):
+        self.calls = []
+
+    def occ_adamw_step(self, params, count, hyper, stream):
+        self.calls.append((count, stream))
+        return 0
+
+
+@pytest.mark.parametrize("stream", [None, "given"])
+def test_adamw_runs_on_its_tensors_gpu(monkeypatch, stream):
+    """The default stream of every GPU has the same null handle and means the
+    current one, so the tensors' GPU has to be current."""
+    at, seen, fake = [0], [], Library()
+
+    class Device:
+        def __init__(self, device):
+            self.to, self.back = device.index, at[0]
+
+        def __enter__(self):
+            at[0] = self.to
+
+        def __exit__(self, *_):
+            at[0] = self.back
+
+    class Stream:
+        cuda_stream = 5
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: at[0])
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: seen.append(i) or 0,
+                        raising=False)
+    real = fake.occ_adamw_step
+    fake.occ_adamw_step = lambda *a: real(*a[:3], (at[0], a[3]))
+    monkeypatch.setattr(optcc, "lib", lambda: fake)
+    given = Stream() if stream else None
+    handle = 5 if stream else 0
+    for kind, index in ((OnGpu, 0), (OnGpu1, 1)):
+        def make(*shape, dtype=torch.float32):
+            return torch.zeros(*shape, dtype=dtype).as_subclass(kind)
+        p = optcc.make_param(**tensors(make=make))
+        optcc.occ_adamw_step([p], 1e-3, 1, stream=given, flags=make(1))
+        assert fake.calls.pop() == (1, (index, handle)) and at == [0]
+        assert given or seen.pop() == index
+        other = OnGpu1 if index == 0 else OnGpu
+        with pytest.raises(ValueError, match="another device"):
+            optcc.occ_adamw_step([p], 1e-3, 1, grad_scale=torch.ones(1).as_subclass(other))
+        with pytest.raises(ValueError, match="different GPUs"):
+            optcc.make_params([p, optcc.make_param(**tensors(make=lambda *s, dtype=torch.float32:
+                              torch.zeros(*s, dtype=dtype).as_subclass(other)))])
+
+
+@pytest.mark.gpu
+@pytest.mark.skipif(torch.cuda.device_count() < 2, reason="needs two GPUs")
+def test_layers_run_on_their_tensors_gpu():
+    """Tensors of the second GPU while the first one is current."""
+    X, W = torch.randn(100, 64, device="cuda:1"), torch.randn(32, 64, device="cuda:1")
+    assert torch.cuda.current_device() == 0
+    Y = optcc.occ_linear_fwd(X, W)
+    dX = torch.empty_like(X)
+    optcc.occ_linear_bwd(Y, W=W, dX=dX)
+    torch.cuda.synchronize(1)
+    assert torch.cuda.current_device() == 0
+    for got, want in ((Y, X.double() @ W.double().t()), (dX, Y.double() @ W.double())):
+        assert torch.allclose(got.double(), want, rtol=1e-4, atol=1e-3)
