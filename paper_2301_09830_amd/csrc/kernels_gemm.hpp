@@ -24,6 +24,7 @@
 #include <stdint.h>
 
 #include "device.hpp"
+#include "layer_tiles.hpp"
 
 namespace occ {
 
@@ -307,7 +308,6 @@ struct GemmArgs {
 // nine products of two such sums hold the product to 2^-25 (those left out are
 // m l, l m and l l), less than its rounding to fp32.  The product runs over K
 // once for each pair, the small ones first.
-constexpr int kPlanes = 3, kPairs = 6;
 
 // plane of pair p: A takes l h m m h h, B takes h l m h m h
 __device__ __forceinline__ int plane_of_a(int p) { return (0x052 >> (2 * p)) & 3; }
@@ -330,8 +330,6 @@ template <int EP>
 __device__ __forceinline__ int64_t part_width(const GemmArgs& g) {
   return (int64_t)((g.N + 3) & ~3) * (EP == EP_GATED ? 2 : 1);
 }
-
-constexpr int kRowBytes = 128;   // of a row of K in a tile: 64 bf16 or 32 fp32
 
 // Offsets at or above this are out of range of the buffer descriptors below;
 // such a lane of a DMA writes zeros.

@@ -258,9 +258,6 @@ __device__ __forceinline__ void st_planes(uint16_t* p, int64_t plane, f32x4_t v,
   }
 }
 
-constexpr int DZ_LANES = 32;   // threads along a row, 4 columns each
-constexpr int DZ_ROWS = 8;     // rows at a time
-
 template <class T, bool GATED>
 __device__ __forceinline__ void dz_block(const DzArgs& g, int block) {
   __shared__ f32x4_t part[GATED ? 2 : 1][DZ_ROWS][DZ_LANES];
