@@ -19,7 +19,13 @@ constexpr size_t kWsAlign = 256;        // of the workspace and of each region i
 constexpr size_t kWsHeader = 256;       // the compressor's numeric flags, left alone
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;
 constexpr int64_t kMaxWidth = (int64_t)1 << 24;   // of in and out
-constexpr int64_t kMaxRowBytes = (int64_t)1 << 26;  // 32 rows are addressed in 31 bits
+constexpr int64_t kMaxRowBytes = (int64_t)1 << 26;  // of a caller's operand
+// The rows of an operand that a wave brings into LDS are addressed from the
+// first of them in 31 bits: 32 rows with the 256 x 256 tile, 16 and 8 with the
+// others.  So the larger tile takes rows of up to 2^26 bytes (bf16 layers, and
+// fp32 ones as planes), the smaller ones of 2^27: dZ of a gated fp32 layer.
+static_assert(kMaxRowBytes * 32 <= (int64_t)1 << 31 && 2 * kMaxWidth * 2 * 32 <= (int64_t)1 << 31 &&
+              2 * kMaxWidth * 4 * 16 <= (int64_t)1 << 31, "offsets of a wave's rows");
 
 inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
 inline int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -51,12 +57,14 @@ enum Tile { TILE_256, TILE_128, TILE_64, TILE_NUM };
 struct TileTimes {
   int side;
   int resident;                    // blocks a CU that do not slow each other down (bf16)
-  double k_bf16, k_f32, fixed;     // us; K tiles of all resident blocks
+  double k_bf16, k_f32, fixed;     // us; K tiles of all resident blocks.  k_f32 0: not for fp32
 };
 // bf16: 8192 x 8192 x K, slope and intercept; 128 and 64: one round at K = 4096.
-// fp32 is bound by the matrix unit in each (256 x 256 x 32 in 16384 clocks), so
-// two resident blocks share its time.
-constexpr TileTimes kTiles[TILE_NUM] = {{256, 1, 1.38, 7.9, 13.0}, {128, 1, 0.57, 2.0, 4.0}, {64, 2, 0.42, 0.58, 3.0}};
+// fp32 is bound by the matrix unit in each (128 x 128 x 32 in 4096 clocks), so
+// two resident blocks share its time.  Products that would fill 256 x 256 tiles
+// run on bf16 planes (of 3000 layers up to 8192 tokens and widths two preferred
+// that tile in fp32).
+constexpr TileTimes kTiles[TILE_NUM] = {{256, 1, 1.38, 0.0, 13.0}, {128, 1, 0.57, 2.0, 4.0}, {64, 2, 0.42, 0.58, 3.0}};
 constexpr double kJoinUs = 6.0, kJoinBytesPerUs = 5e6;
 constexpr int kCUs = 256;
 constexpr int kSplits = 8;
@@ -126,6 +134,7 @@ inline ProductPlan plan_products(const int64_t (&m)[2], const int64_t (&width)[2
   ProductPlan best;
   double best_us = INFINITY;
   for (int t = 0; t < num; ++t) {
+    if (es == 4 && tiles[t].k_f32 == 0.0) continue;
     const bool halves = es == 4 && tiles[t].resident > 1;
     const int64_t slots = (int64_t)kCUs * (es == 4 ? 1 : tiles[t].resident);
     Product of[2][kSplits];

@@ -40,3 +40,28 @@ def test_every_layer_has_a_plan_whose_parts_cover_k(exe):
         wide = p["form"] == "planes" or c["dtype"] == "bf16"
         assert p["x_tiles_k"] == -(-k // (64 if wide else 32)) * (6 if p["form"] == "planes" else 1)
         assert 1 <= p["x_splits"] <= p["x_tiles_k"]
+
+
+def test_offsets_within_a_wave_stay_in_31_bits(exe):
+    """A wave's rows of an operand (an eighth of the tile's) are addressed from
+    the first of them by a 32-bit offset below 2^31: also those of the dZ that a
+    gated fp32 layer makes, up to 2^27 bytes wide.  Where the native fp32 product
+    took 256 x 256 tiles, 32 such rows passed 2^31."""
+    all_of = list(draws(6000, kinds=("bwd",), dtypes=("f32",)))
+    rng = random.Random(2)
+    all_of += [dict(kind="bwd", dtype="f32", tokens=rng.choice((128, 256, 300, 513, 1024, 2048, 4096)),
+                    n_in=rng.choice((64, 256, 300, 1024, 2048)), act=4, gated=True,
+                    out=rng.randint(8 << 20, 16 << 20), dw=rng.random() < 0.5) for _ in range(300)]
+    # weight gradients of few tokens, which used to take that form
+    all_of += [dict(kind="bwd", dtype="f32", tokens=t, n_in=k, out=n, act=4, gated=True, dx=False)
+               for t, k, n in ((4, 7322, 8024), (17, 139, 8640027), (2, 6910, 2434027))]
+    used = set()
+    for c, p in zip(all_of, plans(exe, [case(**c) for c in all_of])):
+        if p["status"]:
+            continue
+        size = 2 if p["form"] == "planes" else 4
+        if p["form"] != "direct" and p["made"]:
+            assert p["tile"] // 8 * p["ldd"] * size <= 1 << 31, (c, p)
+        used.add((p["form"], p["tile"]))
+    assert ("tiled", 256) not in used
+    assert {("tiled", 128), ("tiled", 64), ("planes", 256), ("direct", 64)} <= used
