@@ -70,6 +70,9 @@ constexpr int kCUs = 256;
 constexpr int kSplits = 8;
 constexpr int kSplitCounts[kSplits] = {1, 2, 3, 4, 6, 8, 12, 16};
 constexpr double kMaxPartBytes = 512e6;
+// A launch holds fewer than 2^32 threads: of blocks of 512, those of the
+// products and, beside them, of the bias gradient (16 columns or more each).
+constexpr int64_t kMaxBlocks = (((int64_t)1 << 32) - 1) / 512 - kMaxWidth / 16;
 
 // One product of m x width results over k: its blocks with a tile and a split.
 struct Product {
@@ -98,14 +101,13 @@ inline Product make_product(int64_t m, int64_t width, int64_t k, size_t es, cons
 }
 
 inline bool product_fits(const Product& p) {
-  return p.tiles_m * p.tiles_n < ((int64_t)1 << 26) && p.tiles_k < ((int64_t)1 << 24) &&
-         (double)p.part_bytes <= kMaxPartBytes;
+  return p.blocks() <= kMaxBlocks && p.tiles_k < ((int64_t)1 << 28) && (double)p.part_bytes <= kMaxPartBytes;
 }
 
 struct ProductPlan {
   Tile tile = TILE_256;
   Product x, w;   // of the backward pass; the forward pass has x alone
-  double us = 0.0;
+  double us = INFINITY;
   bool fits = false;
 };
 
@@ -132,7 +134,6 @@ inline double launch_us(const Product& x, const Product& w, int64_t slots, bool 
 inline ProductPlan plan_products(const int64_t (&m)[2], const int64_t (&width)[2], const int64_t (&k)[2], size_t es,
                           bool pair, bool planes = false, const TileTimes* tiles = kTiles, int num = TILE_NUM) {
   ProductPlan best;
-  double best_us = INFINITY;
   for (int t = 0; t < num; ++t) {
     if (es == 4 && tiles[t].k_f32 == 0.0) continue;
     const bool halves = es == 4 && tiles[t].resident > 1;
@@ -154,10 +155,10 @@ inline ProductPlan plan_products(const int64_t (&m)[2], const int64_t (&width)[2
     for (int x = 0; x < n[0]; ++x) {
       for (int w = 0; w < n[1]; ++w) {
         const Product &px = of[0][x], &pw = of[1][w];
+        if (px.blocks() + pw.blocks() > kMaxBlocks) continue;
         const double parts = (double)(px.part_bytes + pw.part_bytes);
         const double us = launch_us(px, pw, slots, halves) + (parts > 0.0 ? kJoinUs + parts / kJoinBytesPerUs : 0.0);
-        if (us < best_us) {
-          best_us = us;
+        if (us < best.us) {
           best.tile = (Tile)t;
           best.x = px;
           best.w = pw;
@@ -260,7 +261,6 @@ inline occ_status_t plan_fwd(const occ_linear_t& l, bool gated, FwdPlan& f) {
   f.copy_x = needs_copy(l.X, l.ldx, l.in, es);
   f.copy_w = needs_copy(l.W, l.ldw, l.in, es);
   f.prod = plan_products({l.tokens, 0}, {wide, 0}, {l.in, 0}, es, gated);
-  if (!f.prod.fits) return OCC_E_SHAPE;
   const double copies = f.copy_x || f.copy_w ? copy_us(l.tokens * f.copy_x + wide * f.copy_w, l.in, es) : 0.0;
   double tiled = f.prod.us + copies;
   if (copies > 0.0) {
@@ -284,6 +284,7 @@ inline occ_status_t plan_fwd(const occ_linear_t& l, bool gated, FwdPlan& f) {
       f.planes = f.copy_x = f.copy_w = true;
     }
   }
+  if (!f.prod.fits) return OCC_E_SHAPE;
   Carve c;
   const size_t row = f.planes ? (size_t)piece_ld(l.in, 2) * 2 * kPlanes : (size_t)piece_ld(l.in, es) * es;
   if (f.copy_x) f.x_off = c.take((size_t)l.tokens * row);
@@ -338,7 +339,6 @@ inline occ_status_t plan_bwd(const occ_linear_grad_t& l, bool gated, BwdPlan& f)
     f.copy_x = l.dW && needs_copy(l.X, l.ldx, l.in, es);
     const int64_t m[2] = {l.dX ? l.tokens : 0, l.dW ? wide : 0}, width[2] = {l.in, l.in}, k[2] = {wide, l.tokens};
     f.prod = plan_products(m, width, k, es, false);
-    if (!f.prod.fits) return OCC_E_SHAPE;
     const double x = l.dW ? (double)l.tokens * (double)l.in : 0.0, w = l.dX ? (double)wide * (double)l.in : 0.0;
     const double dz = (double)l.tokens * (double)wide, dy = (double)l.tokens * (double)l.out;
     const double copied = (f.copy_x ? x : 0.0) + (f.copy_w ? w : 0.0) + (f.copy_dy ? dz : 0.0);
@@ -369,6 +369,7 @@ inline occ_status_t plan_bwd(const occ_linear_grad_t& l, bool gated, BwdPlan& f)
         f.copy_dy = !act;
       }
     }
+    if (!f.prod.fits) return OCC_E_SHAPE;
   }
   const size_t os = f.planes ? 2 : es, np = f.planes ? kPlanes : 1;   // of operands in the workspace
   f.ldd = piece_ld(wide, os);

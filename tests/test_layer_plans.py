@@ -65,3 +65,34 @@ def test_offsets_within_a_wave_stay_in_31_bits(exe):
         used.add((p["form"], p["tile"]))
     assert ("tiled", 256) not in used
     assert {("tiled", 128), ("tiled", 64), ("planes", 256), ("direct", 64)} <= used
+
+
+def test_launches_stay_within_the_largest_grid(exe):
+    """A launch holds fewer than 2^32 threads in a dimension: layers of any
+    number of tokens that the interface admits get tiles large enough for that
+    (512 threads a block, the bias gradient's blocks among them), or are refused
+    by the plan before anything is enqueued."""
+    rng = random.Random(3)
+    top = (1 << 30) - 1
+    all_of = []
+    for _ in range(600):
+        width = rng.choice((1, 7, 16, 64, 100, 128, 300, 1024))
+        c = dict(kind=rng.choice(("fwd", "bwd")), dtype=rng.choice(("bf16", "f32")),
+                 tokens=rng.choice((top, 1 << 29, rng.randint(1 << 27, top))), n_in=width,
+                 out=rng.choice((1, 16, 64, width)), act=rng.randint(1, 4), gated=rng.random() < 0.3,
+                 shift=rng.choice((0, 1)), dx=rng.random() < 0.8)
+        all_of.append(c)
+    # few tokens and huge weights
+    all_of += [dict(kind="bwd", dtype="bf16", tokens=3, n_in=1 << 24, out=1 << w, act=0, dx=False)
+               for w in (9, 12, 13, 14, 16, 20)]
+    taken = 0
+    for c, p in zip(all_of, plans(exe, [case(**c) for c in all_of])):
+        if p["status"]:     # the call's matrices alone pass the memory of a GPU
+            size = 2 if c["dtype"] == "bf16" else 4
+            rows = c["n_in"] * (1 if c["kind"] == "fwd" else 1 + c.get("dx", True)) + c["out"]
+            assert size * (c["tokens"] * rows + c["out"] * c["n_in"]) > 288e9, c
+            continue
+        taken += 1
+        bias = -(-c["out"] * (2 if c.get("gated") else 1) // 16)
+        assert (p["x_blocks"] + p["w_blocks"] + bias) * 512 < 1 << 32, (c, p)
+    assert taken >= 300
