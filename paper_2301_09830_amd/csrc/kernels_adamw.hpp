@@ -47,7 +47,7 @@ constexpr int kAdamTensors = 40;
 
 struct AdamArgs {
   AdamTensor t[kAdamTensors];
-  int32_t start[kAdamTensors];   // first block of each tensor; behind the last one INT_MAX
+  int32_t start[kAdamTensors];   // first block of each tensor (negative: earlier launches took some); behind the last one INT_MAX
   float b1, c1, b2, c2;   // c1 = 1 - b1, c2 = 1 - b2
   float a, c, eps;
   const float* grad_scale;   // device scalar, or null

@@ -405,6 +405,9 @@ AdamKind kind_of(const occ_param_t& p) {
 // 39M at rank 128 275 against 229, and rows of 1817 2.15 ms against 1.95.
 constexpr int64_t kNarrowBlocks = 4096;
 
+// A launch holds fewer than 2^32 threads, 512 or 256 a block.
+constexpr int64_t kMaxAdamBlocks = (((int64_t)1 << 32) - 1) / 512;
+
 // narrow: factors in blocks of 64 columns
 int64_t adam_blocks(const occ_param_t& p, bool narrow) {
   const int64_t per_row = div_up(p.cols, kRun);
@@ -531,28 +534,32 @@ occ_status_t adamw(const occ_param_t* params, int count, const occ_adamw_t* h, h
       const occ_param_t& p = params[j];
       if (kind_of(p) != kind || (far && streams(p)) != nt) continue;
       const int64_t nb = adam_blocks(p, narrow);
-      if (in == kAdamTensors || blocks + nb >= kMaxTokens) {
-        OCC_TRY(launch_adam(kind, nt, narrow, a, in, blocks, s));
-        in = 0;
-        blocks = 0;
+      // a tensor of more blocks than a launch has left is taken in parts
+      for (int64_t done = 0, take; done < nb; done += take) {
+        if (in == kAdamTensors || blocks == kMaxAdamBlocks) {
+          OCC_TRY(launch_adam(kind, nt, narrow, a, in, blocks, s));
+          in = 0;
+          blocks = 0;
+        }
+        take = std::min(nb - done, kMaxAdamBlocks - blocks);
+        a.start[in] = (int32_t)(blocks - done);
+        AdamTensor& t = a.t[in++];
+        t.W = p.W;
+        t.W16 = (uint16_t*)p.W16;
+        t.G = p.G;
+        t.P = p.P;
+        t.Q = p.Q;
+        t.m = p.m;
+        t.v = p.v;
+        t.m_scale = p.m_scale;
+        t.v_scale = p.v_scale;
+        t.ldg = p.G ? p.ldg : p.rank;
+        t.rows = (int32_t)p.rows;
+        t.cols = (int32_t)p.cols;
+        t.keep = (float)(1.0 - h->lr * (double)p.decay);
+        t.key = (h->seed + (uint32_t)j * 0x6A09E667u) * 0xBB67AE85u;
+        blocks += take;
       }
-      a.start[in] = (int32_t)blocks;
-      AdamTensor& t = a.t[in++];
-      t.W = p.W;
-      t.W16 = (uint16_t*)p.W16;
-      t.G = p.G;
-      t.P = p.P;
-      t.Q = p.Q;
-      t.m = p.m;
-      t.v = p.v;
-      t.m_scale = p.m_scale;
-      t.v_scale = p.v_scale;
-      t.ldg = p.G ? p.ldg : p.rank;
-      t.rows = (int32_t)p.rows;
-      t.cols = (int32_t)p.cols;
-      t.keep = (float)(1.0 - h->lr * (double)p.decay);
-      t.key = (h->seed + (uint32_t)j * 0x6A09E667u) * 0xBB67AE85u;
-      blocks += nb;
     }
     if (in) OCC_TRY(launch_adam(kind, nt, narrow, a, in, blocks, s));
   }
