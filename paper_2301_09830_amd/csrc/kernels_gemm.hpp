@@ -342,7 +342,9 @@ __device__ __forceinline__ i32x4_t make_rsrc(uintptr_t p) {
 
 // 64 lanes x 16 bytes from memory to LDS at `lds` + 16 * lane.  Written as
 // assembly so that the compiler does not wait for it before LDS reads of
-// other stages; the kernels below wait themselves.  No register is written.
+// other stages; the kernels below wait themselves.  No register is written but
+// m0, which is reserved: it cannot be named as clobbered, and the compiler sets
+// it before each use of its own (these kernels have none).
 __device__ __forceinline__ void dma16(i32x4_t rsrc, uint32_t voff, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :: "s"(lds), "v"(voff), "s"(rsrc));
@@ -893,7 +895,7 @@ __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_cha
       load_a(1);
     }
     read_a(a0, 0, 0, 0, HA);
-    if (wave >= NW / 2) asm volatile("s_barrier" ::: "memory");
+    if (wave >= NW / 2) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     // The quarters of the wave's results, in an order that needs one new half
     // operand each; the reads are spread so that each run of matrix
     // instructions covers the same number of them.  Loads of tile t + 1 end
@@ -917,7 +919,7 @@ __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_cha
       if (kt + 2 < nk) load_a(st);
       multiply(a1, b0, 1, 0);
     }
-    if (wave < NW / 2) asm volatile("s_barrier" ::: "memory");
+    if (wave < NW / 2) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
   } else {
     constexpr int NI = OA::NI + OB::NI;   // loads of a tile, in flight together
     struct Half {
@@ -968,7 +970,7 @@ __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_cha
       }
       multiply(h1);
     }
-    asm volatile("s_barrier" ::: "memory");   // every wave's reads have ended
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // every wave's reads have ended
   }
 
   // The results go through LDS, so that the epilogue runs along whole rows of
