@@ -53,6 +53,13 @@ int32_t layer_type(const at::Tensor& t, const char* name) {
   refuse(PyExc_TypeError, "%s must be float32 or bfloat16", name);
 }
 
+// An activation's number; one that 32 bits do not hold is none of them.
+int32_t activation(PyObject* o) {
+  const long act = PyLong_AsLong(o);
+  if (PyErr_Occurred()) throw Refused{};
+  return act == (int32_t)act ? (int32_t)act : -1;
+}
+
 struct Call {
   at::ScalarType dtype;
   at::Device device;
@@ -158,8 +165,7 @@ PyObject* forward(PyObject*, PyObject* const* v, Py_ssize_t n) {
     if (gated && rows % 2) refuse(PyExc_ValueError, "%s must hold the rows of both projections", "W");
     occ_linear_t a;
     a.dtype = layer_type(X, "X");
-    a.act = (int32_t)PyLong_AsLong(v[4]);
-    if (PyErr_Occurred()) throw Refused{};
+    a.act = activation(v[4]);
     const Call c{X.scalar_type(), X.device()};
     a.tokens = tokens;
     a.in = in;
@@ -196,7 +202,7 @@ PyObject* backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
     const Call c{dY.scalar_type(), dY.device()};
     const at::ScalarType wide = dW && dW->scalar_type() == at::kFloat ? at::kFloat : c.dtype;
     a.dw_dtype = wide == at::kFloat ? OCC_F32 : OCC_BF16;
-    a.act = (int32_t)PyLong_AsLong(v[5]);
+    a.act = activation(v[5]);
     const uint32_t flags = (uint32_t)PyLong_AsUnsignedLong(v[9]);
     if (PyErr_Occurred()) throw Refused{};
     a.reserved = 0;
