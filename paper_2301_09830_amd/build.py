@@ -67,13 +67,16 @@ def layers_command(out: str = LAYERS) -> list:
 
 
 def build(verbose: bool = False) -> str:
-    """Compile liboptcc.so for gfx950 and the binding of the layers next to
-    this file; returns the library's path."""
+    """Compile liboptcc.so for gfx950 and, where torch is installed, the binding
+    of the layers next to this file; returns the library's path."""
     tmp = LIB + ".tmp"
     objects = [LIB + f".{i}.o" for i in range(len(SOURCES))]
     steps = [[c for c in compile_command(o, src) if c != "-shared"] + ["-c"]
              for o, src in zip(objects, SOURCES)]
-    steps.append(layers_command(LAYERS + ".tmp"))
+    try:
+        steps.append(layers_command(LAYERS + ".tmp"))
+    except ImportError:   # no torch: the library alone, for programs of its C interface
+        pass
     try:
         procs = [subprocess.Popen(cmd, stdout=subprocess.DEVNULL, stderr=subprocess.PIPE, text=True)
                  for cmd in steps]
@@ -86,7 +89,8 @@ def build(verbose: bool = False) -> str:
         for o in objects:
             if os.path.exists(o):
                 os.remove(o)
-    os.replace(LAYERS + ".tmp", LAYERS)
+    if len(steps) > len(SOURCES):
+        os.replace(LAYERS + ".tmp", LAYERS)
     os.replace(tmp, LIB)
     return LIB
 
