@@ -39,7 +39,7 @@ int main() {
       FwdPlan f;
       std::printf("status %d", check_fwd(&a, gated) ? 2 : plan_fwd(a, gated, f));
       std::printf(" form %s tile %d bytes %zu", f.few ? "few" : f.planes ? "planes" : f.direct ? "direct" : "tiled",
-                  f.few ? 0 : kTiles[f.prod.tile].side, f.bytes);
+                  f.few ? 0 : f.direct ? 64 : kTiles[f.prod.tile].side, f.bytes);
       product("x", f.prod.x);
       product("w", f.prod.w);
     } else {

@@ -6,6 +6,7 @@ import random
 import pytest
 
 from layer_plans import AVAILABLE, case, compile_plans, plans
+from stage_forms import FORMS, SINGLE
 
 pytestmark = pytest.mark.skipif(not AVAILABLE, reason="g++ or the HIP headers not available")
 
@@ -96,3 +97,43 @@ def test_launches_stay_within_the_largest_grid(exe):
         bias = -(-c["out"] * (2 if c.get("gated") else 1) // 16)
         assert (p["x_blocks"] + p["w_blocks"] + bias) * 512 < 1 << 32, (c, p)
     assert taken >= 300
+
+
+def test_the_gpu_tests_reach_the_forms_they_name(exe):
+    """tests/test_gpu_layer_forms.py runs these layers."""
+    cases = [case(kind, dtype, *size, act=4 if gated else 2, gated=gated)
+             for kind, dtype, gated, _, _, _, size in FORMS]
+    for (kind, dtype, gated, form, tile, parts, size), p in zip(FORMS, plans(exe, cases)):
+        split = p["x_splits"] > 1 or (kind == "bwd" and p["w_splits"] > 1)
+        assert (p["status"], p["form"], p["tile"]) == (0, form, tile), (kind, dtype, size, p)
+        assert form == "few" or split == parts, (kind, dtype, size, p)
+
+
+def test_no_form_is_left_out(exe):
+    """What 20000 random layers take, the listed ones take too."""
+    listed = {(kind, dtype, gated, form, tile) for kind, dtype, gated, form, tile, _, _ in FORMS}
+    all_of = [c for c in draws(20000, seed=4) if c["pad"] == 0 and c["shift"] == 0]
+    taken = {}
+    for c, p in zip(all_of, plans(exe, [case(**c) for c in all_of])):
+        key = (c["kind"], c["dtype"], c["gated"], p["form"], p["tile"])
+        taken[key] = taken.get(key, 0) + 1
+    assert not {k: n for k, n in taken.items() if k not in listed and n > 2}
+
+
+def test_layers_of_the_plane_tests_take_planes(exe):
+    sizes = [(2048, 1030, 3000), (1500, 2304, 2200), (3001, 2047, 1533), (4096, 256, 4096),
+             (4096, 520, 4096)]
+    cases = [case("fwd", "f32", *s, act=0, gated=g) for s in sizes for g in (False, True)]
+    cases += [case("bwd", "f32", *s, act=0) for s in [(520, 4096, 4096), (4096, 4096, 520)]]
+    assert {p["form"] for p in plans(exe, cases)} == {"planes"}
+    cases = [case("fwd", "f32", *s, act=0) for s in [(200, 520, 130), (1003, 1023, 2047)]]
+    cases += [case("bwd", "f32", *s, act=0) for s in [(517, 1000, 1500), (300, 200, 100)]]
+    assert "planes" not in {p["form"] for p in plans(exe, cases)}
+
+
+def test_the_requested_outputs_enter_the_plan(exe):
+    for dtype, act, size, single, what in SINGLE:
+        both, one = plans(exe, [case("bwd", dtype, *size, act=act, db=False),
+                                case("bwd", dtype, *size, act=act, db=False, dx=single == "dX",
+                                     dw=single == "dW")])
+        assert both[what] != one[what], (dtype, size)
