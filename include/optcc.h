@@ -285,7 +285,9 @@ occ_status_t occ_get_flags(void* ws, uint32_t* flags_out, int clear, occ_stream_
  * matrices with leading dimensions, any alignment (rows that start on 16 bytes
  * and hold whole 16-byte pieces select the fastest forms), host-side checks,
  * work enqueued on `stream`.  Results are deterministic: no atomics, and sums
- * in an order that sizes and alignment alone decide.
+ * in an order that a call's sizes, types, alignment and the outputs that it asks
+ * for decide.  (A backward call plans its products together: dX or dW asked for
+ * alone may sum in another order, or on other units, than beside the other.)
  * ------------------------------------------------------------------------- */
 
 /* Activation functions: z; max(z, 0); z Phi(z); the tanh form
@@ -312,7 +314,9 @@ typedef enum {
  * in and out at most 2^24.
  * fp32 products of some size run on the bf16 matrix units, each operand as the
  * sum of three bf16 values: a product is then off by at most 2^-25 of itself
- * before it is added in fp32.  A non-finite input makes its row NaN there. */
+ * before it is added in fp32 (operands of 2^-99 and more; of smaller ones the
+ * parts below 2^-126 are lost).  There every result that an infinite or NaN
+ * operand enters is NaN, also where the fp32 units would give an infinity. */
 typedef struct {
   int32_t dtype; /* occ_dtype_t */
   int32_t act;   /* occ_act_t */

@@ -96,3 +96,26 @@ def test_fp32_layers_are_fp32_in_norm(kind, size, units):
     optcc.occ_linear_bwd(dY, X, W, dX=dX, dW=dW)
     near(dX, dY.double() @ w, n)
     near(dW, dY.double().t() @ x, t)
+
+
+def test_planes_of_the_smallest_operands():
+    """Operands of 2^-99 keep their 2^-25: their planes end above 2^-126."""
+    g = gen(41)
+    X, W = rand(g, 4096, 520, torch.float32), rand(g, 4096, 520, torch.float32, 2.0 ** 40)
+    X.copy_(torch.copysign(X.abs().frac() + 1, X) * 2.0 ** -99)
+    want = X.double() @ W.double().t()
+    error = float((optcc.occ_linear_fwd(X, W).double() - want).norm() / want.norm())
+    assert error <= ((520 / 24) ** 0.5 + 1) * 2.0 ** -24
+
+
+def test_planes_of_infinities():
+    """A non-finite operand makes every result that it enters NaN, and no other."""
+    g = gen(42)
+    X, W = rand(g, 4096, 520, torch.float32), rand(g, 4096, 520, torch.float32)
+    X[9, 100], X[77, 519], W[5, 3] = float("inf"), float("nan"), float("-inf")
+    Y = optcc.occ_linear_fwd(X, W)
+    rows = torch.ones(4096, dtype=torch.bool, device="cuda")
+    cols = rows.clone()
+    rows[[9, 77]], cols[5] = False, False
+    assert torch.isnan(Y[~rows]).all() and torch.isnan(Y[:, ~cols]).all()
+    assert torch.isfinite(Y[rows][:, cols]).all()
