@@ -2,13 +2,21 @@
 it, and what it keeps alive.  Host checks: no GPU."""
 
 import gc
+import os
 import weakref
 
 import pytest
 
 torch = pytest.importorskip("torch")
 
+from paper_2301_09830_amd import build as buildmod  # noqa: E402
 from paper_2301_09830_amd import optcc  # noqa: E402
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    if not (os.path.exists(buildmod.LIB) and os.path.exists(buildmod.LAYERS)):
+        buildmod.build()
 
 
 # --- a workspace given by the caller -----------------------------------------
