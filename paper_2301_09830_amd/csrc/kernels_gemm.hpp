@@ -114,7 +114,7 @@ __device__ __forceinline__ void act_grad_quad(int act, f32x4_t z, f32x4_t& a, f3
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         a[i] = z[i] > 0.0f || z[i] != z[i] ? z[i] : 0.0f;
-        da[i] = z[i] > 0.0f ? 1.0f : 0.0f;
+        da[i] = z[i] > 0.0f ? 1.0f : z[i] != z[i] ? z[i] : 0.0f;
       }
       break;
     case ACT_GELU:

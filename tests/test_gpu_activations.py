@@ -34,3 +34,23 @@ def test_gelu_is_as_good_as_its_roundings(tokens):
     for got, want, size in ((y, x * phi, (x * phi).abs()), (d, phi + slope, phi + slope.abs())):
         off = (got.double().cpu() - want).abs() / (u * size).clamp_min(2.0 ** -126)
         assert float(off.max()) <= 1, (float(off.max()), float(x[off.argmax()]))
+
+
+@pytest.mark.parametrize("act", range(1, 5))
+@pytest.mark.parametrize("tokens", [40, 3000], ids=["direct", "made first"])
+def test_derivatives_of_nan_are_nan(act, tokens):
+    """A pre-activation that is not a number is not one in the gradients either:
+    none of them hides it behind a zero."""
+    g = torch.Generator(device="cuda").manual_seed(act)
+    for gated in (False, True):
+        n, wide = 72, 144 if gated else 72
+        dY, X = (torch.randn(tokens, c, generator=g, device="cuda") for c in (n, 56))
+        W, Z = torch.randn(wide, 56, generator=g, device="cuda"), torch.randn(tokens, wide, generator=g, device="cuda")
+        Z[3, 5] = float("nan")
+        dX, dW, db = torch.empty_like(X), torch.empty_like(W), torch.empty(wide, device="cuda")
+        (optcc.occ_gated_bwd if gated else optcc.occ_linear_bwd)(dY, X, W, Z=Z, act=act, dX=dX,
+                                                                 dW=dW, dbias=db)
+        assert torch.isnan(dX[3]).all() and torch.isnan(dW[5]).all() and torch.isnan(db[5])
+        assert torch.isnan(dX).any(1).sum() == 1
+        # with a gate, u act'(z) and act(z) are both not a number
+        assert int(torch.isnan(db).sum()) == (2 if gated else 1)
