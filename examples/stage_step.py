@@ -1,4 +1,4 @@
-"""Training steps of one pipeline stage on the library's calls alone.
+"""Training steps of one pipeline stage: its layers, compressor and optimizer.
 
 The stage holds a feed-forward block and a gated one, each with its residual:
 
@@ -11,7 +11,8 @@ next stage, as factors (occ_step by the sender, occ_decompress_ex here),
 backward (occ_linear_bwd, occ_gated_bwd), compression of the weight gradients
 (occ_step_batched_noalloc; between data-parallel ranks the factors would be
 averaged here), and AdamW straight from those factors (occ_adamw_step), with
-fp32 weights, their bf16 copies and 8-bit moments.
+fp32 weights, their bf16 copies and 8-bit moments.  The residuals' gradients
+are added with torch.
 
     python examples/stage_step.py [--steps 60] [--hidden 512] [--tokens 1024]
 """

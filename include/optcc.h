@@ -418,7 +418,8 @@ typedef struct {
 /* Hyperparameters of a step.  step counts from 1.  seed selects the random
  * bits that the 8-bit codes are rounded with: another one each step, the same
  * one on every data-parallel rank; a code depends on seed, the tensor's place
- * in the list and the element's place in the tensor only.
+ * in the list and the element's place in the tensor only.  These are values of
+ * the call: a graph that holds it repeats its step and seed.
  *   grad_scale  device scalar that multiplies every gradient (a clipping
  *               coefficient, 1 / loss scale), or NULL
  *   flags       device word, e.g. flags_out of occ_step_batched_noalloc, or

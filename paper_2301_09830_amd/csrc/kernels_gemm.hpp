@@ -16,8 +16,8 @@
 // Bound by the matrix units and what keeps them fed: bf16 8192^3 runs forward
 // at 1510 TFLOP/s, both gradients at 1330 (K strided takes twice the LDS reads
 // for the same instructions), with the units busy 60 to 67 % of the time; 8192 x
-// 4096 x 16384 with GELU and Z stored 806 us, 1360 TFLOP/s; fp32 4096^3, on bf16
-// planes, 215.
+// 4096 x 16384 with GELU and Z stored 806 to 949 us on different boards, 1160 to
+// 1360 TFLOP/s; fp32 4096^3, on bf16 planes, 215.
 #pragma once
 
 #include <hip/hip_runtime.h>

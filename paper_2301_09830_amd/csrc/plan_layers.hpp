@@ -229,7 +229,9 @@ inline double prep_us(double elements, size_t es) { return elements > 0.0 ? 5.0 
 
 // Up to kBiasTokens the bias gradient is summed from dY and Z themselves, in
 // blocks beside the products' (a rule on the tokens alone, so that its order
-// does not depend on what else a call makes).
+// does not depend on what else a call makes).  bf16, 2048 x 2048, strips and
+// direct: 512 tokens 24 and 21 us, 1024 tokens 29 and 26, 2048 tokens 48 and 50;
+// with GELU 27 and 27, 33 and 35, 53 and 66.
 constexpr int64_t kBiasTokens = 1024;
 
 struct FwdPlan {
