@@ -23,7 +23,8 @@ constexpr int64_t kMaxRowBytes = (int64_t)1 << 26;  // of a caller's operand
 // The rows of an operand that a wave brings into LDS are addressed from the
 // first of them in 31 bits: 32 rows with the 256 x 256 tile, 16 and 8 with the
 // others.  So the larger tile takes rows of up to 2^26 bytes (bf16 layers, and
-// fp32 ones as planes), the smaller ones of 2^27: dZ of a gated fp32 layer.
+// fp32 ones as planes), the smaller ones of 2^27: dZ of a gated fp32 layer
+// (largest_tile).
 static_assert(kMaxRowBytes * 32 <= (int64_t)1 << 31 && 2 * kMaxWidth * 2 * 32 <= (int64_t)1 << 31 &&
               2 * kMaxWidth * 4 * 16 <= (int64_t)1 << 31, "offsets of a wave's rows");
 
@@ -57,14 +58,12 @@ enum Tile { TILE_256, TILE_128, TILE_64, TILE_NUM };
 struct TileTimes {
   int side;
   int resident;                    // blocks a CU that do not slow each other down (bf16)
-  double k_bf16, k_f32, fixed;     // us; K tiles of all resident blocks.  k_f32 0: not for fp32
+  double k_bf16, k_f32, fixed;     // us; K tiles of all resident blocks
 };
 // bf16: 8192 x 8192 x K, slope and intercept; 128 and 64: one round at K = 4096.
-// fp32 is bound by the matrix unit in each (128 x 128 x 32 in 4096 clocks), so
-// two resident blocks share its time.  Products that would fill 256 x 256 tiles
-// run on bf16 planes (of 3000 layers up to 8192 tokens and widths two preferred
-// that tile in fp32).
-constexpr TileTimes kTiles[TILE_NUM] = {{256, 1, 1.38, 0.0, 13.0}, {128, 1, 0.57, 2.0, 4.0}, {64, 2, 0.42, 0.58, 3.0}};
+// fp32 is bound by the matrix unit in each (256 x 256 x 32 in 16384 clocks), so
+// two resident blocks share its time.
+constexpr TileTimes kTiles[TILE_NUM] = {{256, 1, 1.38, 7.9, 13.0}, {128, 1, 0.57, 2.0, 4.0}, {64, 2, 0.42, 0.58, 3.0}};
 constexpr double kJoinUs = 6.0, kJoinBytesPerUs = 5e6;
 constexpr int kCUs = 256;
 constexpr int kSplits = 8;
@@ -129,13 +128,13 @@ inline double launch_us(const Product& x, const Product& w, int64_t slots, bool 
   return full + x.block_us + (double)div_up(left - free, slots) * w.block_us;
 }
 
-// Up to two products of one launch, with the same of the given tiles.  m, width,
-// k: of each (m = 0: not there).
+// Up to two products of one launch, with the same of the given tiles, from the
+// first-th on.  m, width, k: of each (m = 0: not there).
 inline ProductPlan plan_products(const int64_t (&m)[2], const int64_t (&width)[2], const int64_t (&k)[2], size_t es,
-                          bool pair, bool planes = false, const TileTimes* tiles = kTiles, int num = TILE_NUM) {
+                                 bool pair, bool planes = false, int first = TILE_256,
+                                 const TileTimes* tiles = kTiles, int num = TILE_NUM) {
   ProductPlan best;
-  for (int t = 0; t < num; ++t) {
-    if (es == 4 && tiles[t].k_f32 == 0.0) continue;
+  for (int t = first; t < num; ++t) {
     const bool halves = es == 4 && tiles[t].resident > 1;
     const int64_t slots = (int64_t)kCUs * (es == 4 ? 1 : tiles[t].resident);
     Product of[2][kSplits];
@@ -185,7 +184,7 @@ inline ProductPlan plan_direct(const int64_t (&m)[2], const int64_t (&width)[2],
   const bool back = m[1] || dz;
   const TileTimes t = {64, 1, 0.30 + (costly ? 0.65 : dz ? 0.35 : 0.0) + (off_pieces ? (back ? 0.4 : 0.1) : 0.0),
                        0.56 + (costly ? 0.4 : dz ? 0.2 : 0.0) + (off_pieces ? (back ? 0.15 : 0.06) : 0.0), 3.0};
-  return plan_products(m, width, k, es, pair, false, &t, 1);
+  return plan_products(m, width, k, es, pair, false, 0, &t, 1);
 }
 
 // us to write an operand as planes: 4 bytes of each element are read, 6 written
@@ -327,6 +326,13 @@ inline occ_status_t check_bwd(const occ_linear_grad_t* l, bool gated) {
   return OCC_OK;
 }
 
+// Largest tile for a layer whose dZ is `wide` columns of es bytes.  (In fp32 the
+// 256 x 256 tile is taken where K is short and results are many, bound by their
+// stores: dW alone of 30 x 4096 x 16384 85 us, with 128 x 128 tiles 93.)
+inline int largest_tile(int64_t wide, size_t es) {
+  return piece_ld(wide, es) * (int64_t)es > kMaxRowBytes ? TILE_128 : TILE_256;
+}
+
 inline occ_status_t plan_bwd(const occ_linear_grad_t& l, bool gated, BwdPlan& f) {
   if (l.tokens == 0) return OCC_OK;
   const size_t es = elem_size(l.dtype);
@@ -340,7 +346,7 @@ inline occ_status_t plan_bwd(const occ_linear_grad_t& l, bool gated, BwdPlan& f)
     f.copy_w = l.dX && needs_copy(l.W, l.ldw, l.in, es);
     f.copy_x = l.dW && needs_copy(l.X, l.ldx, l.in, es);
     const int64_t m[2] = {l.dX ? l.tokens : 0, l.dW ? wide : 0}, width[2] = {l.in, l.in}, k[2] = {wide, l.tokens};
-    f.prod = plan_products(m, width, k, es, false);
+    f.prod = plan_products(m, width, k, es, false, false, largest_tile(wide, es));
     const double x = l.dW ? (double)l.tokens * (double)l.in : 0.0, w = l.dX ? (double)wide * (double)l.in : 0.0;
     const double dz = (double)l.tokens * (double)wide, dy = (double)l.tokens * (double)l.out;
     const double copied = (f.copy_x ? x : 0.0) + (f.copy_w ? w : 0.0) + (f.copy_dy ? dz : 0.0);

@@ -152,9 +152,7 @@ occ_status_t run_fwd(const occ_linear_t& l, const FwdPlan& f, char* ws, hipStrea
     using TI = decltype(operand);
     return launch(GATED ? "gated_fwd" : "linear_fwd", s, [&] {
       switch (f.prod.tile) {
-        case TILE_256:   // of 2-byte operands alone
-          if constexpr (sizeof(TI) == 2) hipLaunchKernelGGL((k_gemm<TI, T, Form256, EP>), grid, block, 0, s, g);
-          break;
+        case TILE_256: hipLaunchKernelGGL((k_gemm<TI, T, Form256, EP>), grid, block, 0, s, g); break;
         case TILE_128: hipLaunchKernelGGL((k_gemm<TI, T, Form128, EP>), grid, block, 0, s, g); break;
         default: hipLaunchKernelGGL((k_gemm<TI, T, Form64, EP>), grid, block, 0, s, g); break;
       }
@@ -322,9 +320,7 @@ occ_status_t run_bwd(const occ_linear_grad_t& l, const BwdPlan& f, bool accumula
     using TI = decltype(operand);
     return launch("layer_bwd", s, [&] {
       switch (f.prod.tile) {
-        case TILE_256:   // of 2-byte operands alone
-          if constexpr (sizeof(TI) == 2) hipLaunchKernelGGL((k_backward<TI, T, Form256>), grid, block, 0, s, a);
-          break;
+        case TILE_256: hipLaunchKernelGGL((k_backward<TI, T, Form256>), grid, block, 0, s, a); break;
         case TILE_128: hipLaunchKernelGGL((k_backward<TI, T, Form128>), grid, block, 0, s, a); break;
         default: hipLaunchKernelGGL((k_backward<TI, T, Form64>), grid, block, 0, s, a); break;
       }

@@ -7,7 +7,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from paper_2301_09830_amd import optcc  # noqa: E402
-from stage_forms import FORMS, SINGLE, STREAMS  # noqa: E402
+from stage_forms import ALONE, FORMS, SINGLE, STREAMS  # noqa: E402
 from stage_ref import backward64, within  # noqa: E402
 from test_gpu_layers import gen, rand, run_backward, run_forward  # noqa: E402
 
@@ -33,6 +33,19 @@ def test_results_past_the_caches(case):
         run_forward(*size, dtype, 4 if gated else 2, gated)
     else:
         run_backward(*size, dtype, 4 if gated else 0, gated, accumulate=not gated)
+
+
+@pytest.mark.parametrize("dtype,act,gated,form,tile,size,output", ALONE)
+def test_forms_of_a_gradient_alone(dtype, act, gated, form, tile, size, output):
+    g = gen(7)
+    t, k, n = size
+    wide, dt = 2 * n if gated else n, torch.float32
+    dY = rand(g, t, n, dt)
+    X, W = (rand(g, t, k, dt), None) if output == "dW" else (None, rand(g, n, k, dt, n ** -0.5))
+    Z = rand(g, t, wide, dt) if act else None
+    got = torch.empty((wide, k) if output == "dW" else (t, k), device="cuda")
+    (optcc.occ_gated_bwd if gated else optcc.occ_linear_bwd)(dY, X, W, Z=Z, act=act, **{output: got})
+    within(got, *backward64(dY, X, W, Z, act, gated)[output], output)
 
 
 @pytest.mark.parametrize("dtype,act,size,single,what", SINGLE)

@@ -6,7 +6,7 @@ import random
 import pytest
 
 from layer_plans import AVAILABLE, case, compile_plans, plans
-from stage_forms import FORMS, SINGLE
+from stage_forms import ALONE, FORMS, SINGLE
 
 pytestmark = pytest.mark.skipif(not AVAILABLE, reason="g++ or the HIP headers not available")
 
@@ -46,8 +46,7 @@ def test_every_layer_has_a_plan_whose_parts_cover_k(exe):
 def test_offsets_within_a_wave_stay_in_31_bits(exe):
     """A wave's rows of an operand (an eighth of the tile's) are addressed from
     the first of them by a 32-bit offset below 2^31: also those of the dZ that a
-    gated fp32 layer makes, up to 2^27 bytes wide.  Where the native fp32 product
-    took 256 x 256 tiles, 32 such rows passed 2^31."""
+    gated fp32 layer makes, up to 2^27 bytes wide, 32 of which would pass it."""
     all_of = list(draws(6000, kinds=("bwd",), dtypes=("f32",)))
     rng = random.Random(2)
     all_of += [dict(kind="bwd", dtype="f32", tokens=rng.choice((128, 256, 300, 513, 1024, 2048, 4096)),
@@ -64,7 +63,6 @@ def test_offsets_within_a_wave_stay_in_31_bits(exe):
         if p["form"] != "direct" and p["made"]:
             assert p["tile"] // 8 * p["ldd"] * size <= 1 << 31, (c, p)
         used.add((p["form"], p["tile"]))
-    assert ("tiled", 256) not in used
     assert {("tiled", 128), ("tiled", 64), ("planes", 256), ("direct", 64)} <= used
 
 
@@ -107,6 +105,10 @@ def test_the_gpu_tests_reach_the_forms_they_name(exe):
         split = p["x_splits"] > 1 or (kind == "bwd" and p["w_splits"] > 1)
         assert (p["status"], p["form"], p["tile"]) == (0, form, tile), (kind, dtype, size, p)
         assert form == "few" or split == parts, (kind, dtype, size, p)
+    for dtype, act, gated, form, tile, size, output in ALONE:
+        p, = plans(exe, [case("bwd", dtype, *size, act=act, gated=gated, dx=output == "dX",
+                              dw=output == "dW", db=False)])
+        assert (p["status"], p["form"], p["tile"]) == (0, form, tile), (size, p)
 
 
 def test_no_form_is_left_out(exe):
