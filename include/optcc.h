@@ -61,6 +61,9 @@ extern "C" {
 #define OCC_ABI_VERSION 2
 #define OCC_MAX_RANK 128
 #define OCC_MAX_ITERS 64
+#define OCC_MAX_EXPERTS 1024 /* of a layer of experts */
+#define OCC_MAX_CHOICES 32   /* experts of a token */
+#define OCC_MAX_TEACHER 1024 /* entries of a teacher's list */
 
 typedef void* occ_stream_t; /* a hipStream_t */
 
@@ -84,7 +87,8 @@ typedef enum { OCC_F32 = 0, OCC_BF16 = 1 } occ_dtype_t;
 /* sticky numeric flags, read with occ_get_flags; OCC_F_BAD_ROWS: the row list
  * of occ_step_rows was not strictly increasing inside [0, rows) (the results
  * of that call are then unspecified, but no memory outside the arguments is
- * touched) */
+ * touched).  The calls on experts' rows and on a teacher's list raise it in a
+ * word of the caller's, where they say so. */
 enum { OCC_F_NONFINITE = 1u, OCC_F_RANK_DEFICIENT = 2u, OCC_F_BAD_ROWS = 4u };
 
 /* call flags for occ_step / occ_step_batched */
@@ -443,6 +447,175 @@ typedef struct {
  * run of 256).  No workspace; nothing is copied to the device by itself. */
 occ_status_t occ_adamw_step(const occ_param_t* params, int count, const occ_adamw_t* h,
                             occ_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Layers of experts: each token goes to k of the experts, each of which is a
+ * linear or gated layer of its own.
+ *   occ_route_fwd   the choice of the experts, and the plan of their rows
+ *   occ_dispatch    the tokens' rows in the experts' order
+ *   occ_experts_*   the layers on those rows
+ *   occ_combine     the experts' rows back in the tokens' order, weighted
+ * A plan: entry t k + j is the j-th choice of token t; `order` lists the entries
+ * expert by expert, those of an expert by token; `offsets` (experts + 1 values)
+ * says where each expert's begin, and its last value how many there are;
+ * `slots` gives each entry's place in `order`, -1 for a choice that is none.
+ * Offsets, order and slots are DEVICE arrays of int32.  The host does not read
+ * them: values that fit no plan raise OCC_F_BAD_ROWS in *flags (a device word
+ * that the caller owns and clears, or NULL), and no memory outside the
+ * arguments is touched.
+ * ------------------------------------------------------------------------- */
+
+/* Router.  Of each token's logits the k largest, in falling order, the lower
+ * index first among equals (0 and -0 are equal); -inf and NaN are never chosen,
+ * and a token with fewer than k others has index -1 and weight 0 in the places
+ * left.  Weights (fp32): renorm 1, the softmax over the chosen logits; renorm 0,
+ * the softmax over all the experts at the chosen ones.  A NaN among a token's
+ * logits makes its weights NaN.  Results of one call depend on its arguments
+ * alone: no atomics on floating values, and a stable order.
+ * index, weights and slots are tokens x k, order holds tokens k values (those
+ * behind offsets[experts] are left alone). */
+typedef struct {
+  int32_t dtype; /* occ_dtype_t of the logits (and of their gradient) */
+  int32_t k;     /* 1 .. OCC_MAX_CHOICES, at most experts */
+  int32_t renorm;
+  int32_t reserved;
+  int64_t tokens, experts; /* tokens k < 2^30, experts <= OCC_MAX_EXPERTS */
+  const void* logits;      /* tokens x experts */
+  int64_t ldl;
+  int32_t* index;
+  float* weights;
+  int32_t* offsets;
+  int32_t* order;
+  int32_t* slots;
+} occ_route_t;
+
+size_t occ_route_fwd_workspace_bytes(const occ_route_t* r);
+occ_status_t occ_route_fwd(const occ_route_t* r, void* ws, size_t ws_bytes, occ_stream_t stream);
+
+/* Gradient of the logits (tokens x experts, of their type, all of it written)
+ * from dweights (fp32, tokens x k), with index and weights as occ_route_fwd left
+ * them.  With s the sum of w dw over a token's choices:
+ *   renorm 1   w (dw - s) at the chosen, 0 elsewhere (logits may be NULL)
+ *   renorm 0   -p s at every expert, p their softmax, and w dw more at the chosen
+ * dweights of a choice that is none are not looked at.  dlogits may be the
+ * logits. */
+occ_status_t occ_route_bwd(const occ_route_t* r, const float* dweights, void* dlogits, int64_t ldd,
+                           occ_stream_t stream);
+
+/* The plan that rows are exchanged by: tokens x width on one side, rows x width
+ * on the other (rows: what order holds, at least offsets[experts]). */
+typedef struct {
+  int32_t dtype; /* occ_dtype_t of all matrices */
+  int32_t k;
+  int64_t tokens, experts, rows, width;
+  const int32_t* offsets; /* occ_dispatch */
+  const int32_t* order;   /* occ_dispatch, occ_combine_bwd */
+  const int32_t* slots;   /* occ_combine, occ_combine_bwd */
+  uint32_t* flags;        /* may be NULL */
+} occ_exchange_t;
+
+/* Xs[s] = X[order[s] / k] for s < offsets[experts]; rows behind are left alone.
+ * Its gradient is occ_combine of dXs without weights. */
+occ_status_t occ_dispatch(const occ_exchange_t* x, const void* X, int64_t ldx, void* Xs, int64_t ldxs,
+                          occ_stream_t stream);
+
+/* Y[t] = sum over j of weights[t][j] Ys[slots[t][j]] + R[t], summed in fp32 in
+ * the order of j, rounded once.  weights (fp32) NULL: ones; R may be NULL, or Y.
+ * A slot of -1 adds nothing, whatever its weight; one of `rows` or more raises
+ * OCC_F_BAD_ROWS and adds nothing. */
+occ_status_t occ_combine(const occ_exchange_t* x, const float* weights, const void* Ys, int64_t ldys, const void* R,
+                         int64_t ldr, void* Y, int64_t ldy, occ_stream_t stream);
+
+/* dYs[slots[t][j]] = weights[t][j] dY[t] and dweights[t][j] = <dY[t],
+ * Ys[slots[t][j]]> (fp32); either may be NULL.  An entry without a row has
+ * dweights 0; rows of dYs that no entry has are left alone.  An entry whose
+ * place in order does not name it raises OCC_F_BAD_ROWS and counts as without. */
+occ_status_t occ_combine_bwd(const occ_exchange_t* x, const float* weights, const void* dY, int64_t lddy,
+                             const void* Ys, int64_t ldys, void* dYs, int64_t lddys, float* dweights,
+                             occ_stream_t stream);
+
+/* The layers.  l is the layer of the first expert: l.tokens counts all rows of
+ * X, R, Z and Y (of dY, Z, X and dX), of which those from offsets[e] on up to
+ * offsets[e + 1] belong to expert e; rows outside are neither read for a result
+ * nor written.  Weights of expert e begin stride_w elements after those of
+ * expert e - 1 (dW: stride_dw), biases follow each other: experts x out (gated:
+ * experts x 2 out), contiguous.  An expert may have no rows: its dW and dbias
+ * are zero (or left, when accumulating).  Offsets out of 0 .. l.tokens are taken as
+ * the nearer end, and one that falls as the largest before it; either raises
+ * OCC_F_BAD_ROWS.  All else is as in occ_linear_fwd and its companions; the order
+ * of a sum depends on the number of rows and experts, and of dbias on offsets. */
+typedef struct {
+  occ_linear_t l;
+  int64_t experts; /* 1 .. OCC_MAX_EXPERTS */
+  int64_t stride_w;
+  const int32_t* offsets;
+  uint32_t* flags; /* may be NULL */
+} occ_experts_t;
+
+typedef struct {
+  occ_linear_grad_t l;
+  int64_t experts;
+  int64_t stride_w, stride_dw;
+  const int32_t* offsets;
+  uint32_t* flags;
+} occ_experts_grad_t;
+
+size_t occ_experts_linear_fwd_workspace_bytes(const occ_experts_t* l);
+size_t occ_experts_gated_fwd_workspace_bytes(const occ_experts_t* l);
+size_t occ_experts_linear_bwd_workspace_bytes(const occ_experts_grad_t* l);
+size_t occ_experts_gated_bwd_workspace_bytes(const occ_experts_grad_t* l);
+
+occ_status_t occ_experts_linear_fwd(const occ_experts_t* l, void* ws, size_t ws_bytes, occ_stream_t stream);
+occ_status_t occ_experts_gated_fwd(const occ_experts_t* l, void* ws, size_t ws_bytes, occ_stream_t stream);
+occ_status_t occ_experts_linear_bwd(const occ_experts_grad_t* l, unsigned flags, void* ws, size_t ws_bytes,
+                                    occ_stream_t stream);
+occ_status_t occ_experts_gated_bwd(const occ_experts_grad_t* l, unsigned flags, void* ws, size_t ws_bytes,
+                                   occ_stream_t stream);
+
+/* Loss of the last stage: a token's logits s over the vocabulary against the
+ * teacher's k largest logits t, at columns i, and against a label:
+ *   p = softmax(t / T) over the list, q = softmax(s / T), c = softmax(s)
+ *   loss = scale [alpha T^2 sum p (log p - log q_i) + (1 - alpha) (-log c_label)]
+ *   dS_j = scale [alpha T (q_j - p_j) + (1 - alpha) (c_j - [j = label])]
+ * (a column listed twice has both its p).  A list entry with a negative index, or
+ * a teacher's logit of -inf, is masked; a token whose entries all are has no
+ * first part, one whose label is negative (or labels NULL) no second.  With
+ * neither, or with scale 0, the loss is 0 and the gradient a row of zeros, and the
+ * token's logits are not looked at.  An index or label of `vocab` or more counts
+ * as masked and raises OCC_F_BAD_ROWS.  alpha 1 leaves labels, alpha 0 the list
+ * out of account.
+ *   occ_distill_fwd   loss (fp32, a token each); lse, if given, receives the
+ *                     logarithms of the two softmaxes' sums (tokens x 2: at T, at
+ *                     1; 0 for a part that a token has not); dS, if given, the
+ *                     gradient of the sum of the losses, in the same pass
+ *   occ_distill_bwd   dS from lse (loss is not looked at); scale carries the
+ *                     gradient of each loss: the forward's scale times it
+ * dS has the type of S and may be S.  Sums are held in fp32, dS is rounded once;
+ * from lse, itself rounded to fp32, it is |lse| 2^-24 less exact. */
+typedef struct {
+  int32_t dtype;   /* occ_dtype_t of S and dS */
+  int32_t t_dtype; /* occ_dtype_t of the teacher's logits */
+  int64_t tokens, vocab; /* vocab <= 2^24 */
+  const void* S;
+  int64_t lds;
+  int32_t k; /* 0 .. OCC_MAX_TEACHER */
+  int32_t reserved;
+  const int32_t* index; /* tokens x k */
+  int64_t ldi;
+  const void* teacher;  /* tokens x k */
+  int64_t ldt;
+  const int32_t* labels; /* a token each, or NULL */
+  const float* scale;    /* a token each, or NULL: ones */
+  float temperature, alpha; /* T > 0; alpha 0 .. 1 */
+  float* loss;
+  float* lse;
+  void* dS;
+  int64_t ldds;
+  uint32_t* flags; /* may be NULL */
+} occ_distill_t;
+
+occ_status_t occ_distill_fwd(const occ_distill_t* d, occ_stream_t stream);
+occ_status_t occ_distill_bwd(const occ_distill_t* d, occ_stream_t stream);
 
 /* Per-kernel timing with HIP events, for benchmarks.  Between
  * occ_profile_begin and occ_profile_end every kernel the library launches is

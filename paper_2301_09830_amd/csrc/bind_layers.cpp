@@ -1,4 +1,5 @@
-// Python binding of the layers (occ_linear_*, occ_gated_*): from tensors to
+// Python binding of the layers (occ_linear_*, occ_gated_*; in bind_experts.hpp
+// those of experts, the router, the exchange and the loss): from tensors to
 // the structures of include/optcc.h and one call, in native code, since a call
 // of a small layer takes the host longer than the GPU: a forward call of a
 // small bf16 layer 3.8 us, a backward call (two launches) 8.1; the same checks
@@ -9,6 +10,8 @@
 #include <ATen/ATen.h>
 #include <c10/core/DeviceGuard.h>
 #include <torch/csrc/autograd/python_variable.h>
+
+#include <cstring>
 
 #include "optcc.h"
 
@@ -246,10 +249,27 @@ PyObject* setup(PyObject*, PyObject* const* v, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
+}  // namespace
+
+#include "bind_experts.hpp"
+
+namespace {
+
+#define FAST(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
+
 PyMethodDef methods[] = {
     {"forward", (PyCFunction)(void (*)(void))forward, METH_FASTCALL, nullptr},
     {"backward", (PyCFunction)(void (*)(void))backward, METH_FASTCALL, nullptr},
     {"setup", (PyCFunction)(void (*)(void))setup, METH_FASTCALL, nullptr},
+    FAST(experts_forward),
+    FAST(experts_backward),
+    FAST(route_forward),
+    FAST(route_backward),
+    FAST(dispatch),
+    FAST(combine),
+    FAST(combine_backward),
+    FAST(distill),
+    FAST(setup_experts),
     {nullptr, nullptr, 0, nullptr},
 };
 

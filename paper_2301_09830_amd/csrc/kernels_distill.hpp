@@ -1,0 +1,428 @@
+// Loss of a language model's logits against a teacher's top logits and the
+// labels, with its gradient.  For a token with logits s, temperature T and
+// weight alpha, with the teacher's k entries t at columns i:
+//
+//   p = softmax(t / T) over the entries, q = softmax(s / T), c = softmax(s)
+//   loss = scale [alpha T^2 sum p (log p - log q_i) + (1 - alpha) (-log c_label)]
+//   ds_j = scale [alpha T (q_j - p_j) + (1 - alpha) (c_j - [j = label])]
+//
+// Bound by memory: the loss with its gradient reads every logit once and
+// writes it once, the row held in registers in between.
+#pragma once
+
+#include "kernels_route.hpp"
+
+namespace occ {
+
+constexpr int DL_ENTRIES = 1024;   // of a teacher's list
+
+struct DistillArgs {
+  const void* S;          // tokens x vocab
+  int64_t lds;
+  const int32_t* index;   // tokens x k
+  const void* teacher;    // tokens x k
+  int64_t ldi, ldt;
+  const int32_t* labels;  // may be null
+  const float* scale;     // may be null
+  float* loss;
+  float* lse;             // tokens x 2: at the temperature, at 1; may be null
+  void* dS;               // may be null
+  int64_t ldd;
+  uint32_t* flags;
+  int32_t vocab, k, teacher_bf16;
+  float temperature, alpha;
+  int32_t stream;         // dS bypasses the caches
+};
+
+// One token's entries, in LDS.  Those out of the vocabulary are masked, and
+// those that name a column for the second time are added to its first entry.
+template <int N>
+struct DistillToken {
+  int32_t index[N + 1];   // the label's entry is behind the teacher's
+  float p[N + 1], s[N + 1];
+};
+
+// Sum (or maximum) over a block of NW waves, in every thread.
+template <int NW, class F>
+__device__ __forceinline__ float block_reduce(float x, float* lds, F&& f) {
+#pragma unroll
+  for (int s = 32; s; s >>= 1) x = f(x, __shfl_xor(x, s));
+  if constexpr (NW == 1) return x;
+  __syncthreads();   // the last use of lds has ended
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+  __syncthreads();
+  x = lds[0];
+#pragma unroll
+  for (int w = 1; w < NW; ++w) x = f(x, lds[w]);
+  return x;
+}
+
+// NaN wins.
+__device__ __forceinline__ float max_nan(float a, float b) { return a != a || a > b ? a : b; }
+
+template <int NW>
+__device__ __forceinline__ float block_max(float x, float* lds) {
+  return block_reduce<NW>(x, lds, [](float a, float b) { return max_nan(a, b); });
+}
+
+template <int NW>
+__device__ __forceinline__ float block_sum(float x, float* lds) {
+  return block_reduce<NW>(x, lds, [](float a, float b) { return a + b; });
+}
+
+// A token's part in the loss, the same in all threads.
+struct DistillRow {
+  float scale;
+  bool soft, hard;    // has entries; has a label
+  float entropy;      // sum of p log p
+};
+
+// Reads the entries and their logits, makes p.  Returns with the block in step.
+template <class T, int NW>
+__device__ __forceinline__ DistillRow distill_entries(const DistillArgs& g, int64_t token, DistillToken<DL_ENTRIES>& e,
+                                                      float* lds) {
+  constexpr int NT = NW * 64;
+  DistillRow r;
+  r.scale = g.scale ? g.scale[token] : 1.0f;
+  const int label = g.labels && g.alpha != 1.0f ? g.labels[token] : -1;
+  r.hard = r.scale != 0.0f && label >= 0 && label < g.vocab;
+  r.soft = false;
+  r.entropy = 0.0f;
+  bool bad = label >= g.vocab;
+  if (r.scale == 0.0f) return r;
+  const T* const row = (const T*)g.S + token * g.lds;
+  const float inv = 1.0f / g.temperature;
+  float top = -INFINITY;
+  if (g.alpha != 0.0f)
+    for (int j = threadIdx.x; j < g.k; j += NT) {
+      const int i = g.index[token * g.ldi + j];
+      const bool in = i >= 0 && i < g.vocab;
+      bad |= i >= g.vocab;
+      float t = -INFINITY;
+      if (in) {   // what stands at a masked entry is not looked at
+        t = g.teacher_bf16 ? ld_elem<uint16_t>((const uint16_t*)g.teacher + token * g.ldt + j)
+                           : ((const float*)g.teacher)[token * g.ldt + j];
+        t *= inv;
+      }
+      const bool live = in && t != -INFINITY;
+      e.index[j] = live ? i : -1;
+      e.p[j] = t;
+      e.s[j] = live ? ld_elem<T>(row + i) : 0.0f;
+      top = max_nan(top, t);
+    }
+  if (threadIdx.x == 0) {
+    e.index[g.k] = r.hard ? label : -1;
+    e.s[g.k] = r.hard ? ld_elem<T>(row + label) : 0.0f;
+  }
+  if (__ballot(bad) && (threadIdx.x & 63) == 0 && g.flags) atomicOr(g.flags, kBadRows);
+  top = block_max<NW>(top, lds);
+  r.soft = g.k && g.alpha != 0.0f && top != -INFINITY;
+  if (r.soft) {
+    float sum = 0.0f, plog = 0.0f;
+    for (int j = threadIdx.x; j < g.k; j += NT) sum += exp_f(e.p[j] - top);
+    sum = block_sum<NW>(sum, lds);
+    const float log_sum = logf(sum), part = 1.0f / sum;
+    for (int j = threadIdx.x; j < g.k; j += NT) {
+      const float d = e.p[j] - top, p = exp_f(d) * part;
+      plog += p > 0.0f || p != p ? p * (d - log_sum) : 0.0f;
+      e.p[j] = p;
+    }
+    r.entropy = block_sum<NW>(plog, lds);
+  }
+  __syncthreads();
+  return r;
+}
+
+// The loss from a row's statistics: m its maximum, z and z1 the sums of
+// exp((s - m) / T) and exp(s - m).
+template <int NW>
+__device__ __forceinline__ void distill_loss(const DistillArgs& g, int64_t token, const DistillRow& r,
+                                             const DistillToken<DL_ENTRIES>& e, float m, float z, float z1,
+                                             float* lds) {
+  const float inv = 1.0f / g.temperature, log_z = logf(z), log_1 = logf(z1);
+  float cross = 0.0f;   // -sum p log q
+  if (r.soft) {
+    for (int j = threadIdx.x; j < g.k; j += NW * 64) {
+      const float p = e.p[j];
+      if (p > 0.0f || p != p) cross += p * (log_z - (e.s[j] - m) * inv);
+    }
+    cross = block_sum<NW>(cross, lds);
+  }
+  if (threadIdx.x) return;
+  float loss = 0.0f;
+  if (r.soft) loss = g.alpha * g.temperature * g.temperature * (r.entropy + cross);
+  if (r.hard) loss += (1.0f - g.alpha) * (log_1 - (e.s[g.k] - m));
+  g.loss[token] = r.scale * loss;
+  if (g.lse) {
+    g.lse[2 * token] = r.soft ? m * inv + log_z : 0.0f;
+    g.lse[2 * token + 1] = r.hard ? m + log_1 : 0.0f;
+  }
+}
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// Exponentials of a row: e^((s - m) / T), or e^(s - m) for the labels alone or
+// at T = 1, and both where a token has entries and a label at another
+// temperature (`two`).  m is the row's maximum, subtracted before anything is
+// multiplied, so that rows of the type's lowest values stay exact; from stored
+// logarithms m is 0 and oa, ob hold them, in powers of two.
+struct DistillExp {
+  float m, ka, kb, oa, ob;
+  bool two;
+  __device__ __forceinline__ DistillExp(const DistillArgs& g, const DistillRow& r, float top) {
+    m = top;
+    ka = r.soft ? kLog2e / g.temperature : kLog2e;
+    kb = kLog2e;
+    oa = ob = 0.0f;
+    two = r.soft && r.hard && g.temperature != 1.0f;
+  }
+  __device__ __forceinline__ float a(float s) const { return __builtin_amdgcn_exp2f(__builtin_fmaf(s - m, ka, -oa)); }
+  __device__ __forceinline__ float b(float s) const { return __builtin_amdgcn_exp2f(__builtin_fmaf(s - m, kb, -ob)); }
+};
+
+// Factors of the exponentials in the gradient.
+struct DistillGrad {
+  float fa, fb;
+  __device__ __forceinline__ DistillGrad(const DistillArgs& g, const DistillRow& r, bool two, float z, float z1) {
+    const float soft = r.soft ? r.scale * g.alpha * g.temperature / z : 0.0f;
+    const float hard = r.hard ? r.scale * (1.0f - g.alpha) / z1 : 0.0f;
+    fa = two ? soft : soft + hard;
+    fb = two ? hard : 0.0f;
+  }
+};
+
+// A piece of a row, -inf behind its end.
+template <class T>
+__device__ __forceinline__ f32x4_t row_piece(const T* row, int c, int vocab) {
+  constexpr int CH = 16 / sizeof(T);
+  if (c + CH <= vocab) return ld_piece<T>(row + c, CH);
+  const uint32_t low = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+  f32x4_t v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(low);
+  if (c >= vocab) return v;
+  T e[CH];
+  __builtin_memcpy(e, &v, 16);
+#pragma unroll
+  for (int i = 0; i < CH; ++i)
+    if (c + i < vocab) e[i] = row[c + i];
+  __builtin_memcpy(&v, e, 16);
+  return v;
+}
+
+template <class T>
+__device__ __forceinline__ f32x4_t grad_piece(f32x4_t v, const DistillExp& x, const DistillGrad& d) {
+  constexpr int CH = 16 / sizeof(T);
+  float e[CH];
+  widen<T>(v, e);
+  if (x.two) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) e[i] = __builtin_fmaf(d.fb, x.b(e[i]), d.fa * x.a(e[i]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) e[i] = d.fa * x.a(e[i]);
+  }
+  return narrow<T>(e);
+}
+
+template <class T, bool NT>
+__device__ __forceinline__ void st_row_piece(T* p, f32x4_t v, int left) {
+  constexpr int CH = 16 / sizeof(T);
+  if constexpr (NT) {
+    if (left >= CH) return __builtin_nontemporal_store(v, (f32x4_t*)p);
+  }
+  st_piece<T>(p, v, left);
+}
+
+// The columns of the entries, once the rest of the row is stored: the first
+// entry of a column takes off what all of the same column hold.
+template <class T, int NW>
+__device__ __forceinline__ void store_entries(const DistillArgs& g, int64_t token, const DistillRow& r,
+                                              const DistillToken<DL_ENTRIES>& e, const DistillExp& x,
+                                              const DistillGrad& d) {
+  // another thread has stored to the same place: its store has to be done
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  const float soft = r.scale * g.alpha * g.temperature, hard = r.scale * (1.0f - g.alpha);
+  const int n = g.k + 1;
+  for (int j = threadIdx.x; j < n; j += NW * 64) {
+    const int at = e.index[j];
+    if (at < 0 || (j < g.k && !r.soft)) continue;
+    float off = 0.0f;
+    bool first = true;
+    if (r.soft)
+      for (int i = 0; i < g.k; ++i) {
+        if (e.index[i] != at) continue;
+        first = first && i >= j;
+        off += e.p[i];
+      }
+    if (!first) continue;
+    off *= soft;
+    if (r.hard && e.index[g.k] == at) off += hard;
+    const float s = e.s[j];
+    float v = d.fa * x.a(s);
+    if (x.two) v = __builtin_fmaf(d.fb, x.b(s), v);
+    st_elem((T*)g.dS + token * g.ldd + at, v - off);
+  }
+}
+
+template <class T, int NW>
+__device__ __forceinline__ void zero_row(const DistillArgs& g, int64_t token) {
+  constexpr int CH = 16 / sizeof(T);
+  T* const row = (T*)g.dS + token * g.ldd;
+  for (int c = threadIdx.x * CH; c < g.vocab; c += NW * 64 * CH) st_piece<T>(row + c, f32x4_t{}, g.vocab - c);
+}
+
+// A token that has no part in the loss: its logits are not read.
+template <class T, int NW>
+__device__ __forceinline__ void ignored_token(const DistillArgs& g, int64_t token) {
+  if (threadIdx.x == 0) {
+    if (g.loss) g.loss[token] = 0.0f;
+    if (g.lse) g.lse[2 * token] = g.lse[2 * token + 1] = 0.0f;
+  }
+  if (g.dS) zero_row<T, NW>(g, token);
+}
+
+// A token a block, its row in the registers of NW waves, VPT pieces of 16 bytes
+// a thread: one pass over memory.
+template <class T, int NW, int VPT, bool NT>
+__global__ __launch_bounds__(NW * 64, 4) void k_distill(DistillArgs g) {
+  constexpr int CH = 16 / sizeof(T), STEP = NW * 64 * CH;
+  __shared__ DistillToken<DL_ENTRIES> e;
+  __shared__ float lds[NW];
+  const int64_t token = blockIdx.x;
+  const T* const row = (const T*)g.S + token * g.lds;
+  const int c0 = threadIdx.x * CH;
+  f32x4_t v[VPT];
+  if (!g.scale || g.scale[token] != 0.0f) {   // on its way while the entries are read
+#pragma unroll
+    for (int p = 0; p < VPT; ++p) v[p] = row_piece<T>(row, c0 + p * STEP, g.vocab);
+  }
+  const DistillRow r = distill_entries<T, NW>(g, token, e, lds);
+  if (!r.soft && !r.hard) return ignored_token<T, NW>(g, token);
+  float m = -INFINITY;
+#pragma unroll
+  for (int p = 0; p < VPT; ++p) {
+    float f[CH];
+    widen<T>(v[p], f);
+#pragma unroll
+    for (int i = 0; i < CH; ++i) m = fmaxf(m, f[i]);
+  }
+  m = block_reduce<NW>(m, lds, [](float a, float b) { return fmaxf(a, b); });
+  const DistillExp x(g, r, m);
+  float z = 0.0f, z1 = 0.0f;
+#pragma unroll
+  for (int p = 0; p < VPT; ++p) {
+    float f[CH];
+    widen<T>(v[p], f);
+    if (x.two) {
+#pragma unroll
+      for (int i = 0; i < CH; ++i) z1 += x.b(f[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < CH; ++i) z += x.a(f[i]);
+  }
+  z = block_sum<NW>(z, lds);
+  z1 = x.two ? block_sum<NW>(z1, lds) : z;
+  distill_loss<NW>(g, token, r, e, m, z, z1, lds);
+  if (!g.dS) return;
+  const DistillGrad d(g, r, x.two, z, z1);
+  T* const out = (T*)g.dS + token * g.ldd;
+#pragma unroll
+  for (int p = 0; p < VPT; ++p) {
+    const int c = c0 + p * STEP;
+    if (c < g.vocab) st_row_piece<T, NT>(out + c, grad_piece<T>(v[p], x, d), g.vocab - c);
+  }
+  store_entries<T, NW>(g, token, r, e, x, d);
+}
+
+// Rows that the registers of a block do not hold: the maximum and the sums in
+// one pass, kept together, then the gradient from a second one, which finds
+// the row in the memory-side cache.
+template <class T>
+__global__ __launch_bounds__(1024) void k_distill_long(DistillArgs g) {
+  constexpr int NW = 16, CH = 16 / sizeof(T), STEP = NW * 64 * CH, U = 4;
+  __shared__ DistillToken<DL_ENTRIES> e;
+  __shared__ float lds[NW];
+  const int64_t token = blockIdx.x;
+  const DistillRow r = distill_entries<T, NW>(g, token, e, lds);
+  if (!r.soft && !r.hard) return ignored_token<T, NW>(g, token);
+  const T* const row = (const T*)g.S + token * g.lds;
+  const DistillExp unit(g, r, 0.0f);   // its factors alone
+  float m = -INFINITY, z = 0.0f, z1 = 0.0f;
+  for (int c0 = threadIdx.x * CH; c0 < g.vocab; c0 += U * STEP) {
+    f32x4_t v[U];
+    float f[U][CH], top = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = row_piece<T>(row, c0 + u * STEP, g.vocab);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      widen<T>(v[u], f[u]);
+#pragma unroll
+      for (int i = 0; i < CH; ++i) top = fmaxf(top, f[u][i]);
+    }
+    const float by = top == -INFINITY ? 0.0f : top;   // only -inf (or NaN) so far
+    z *= __builtin_amdgcn_exp2f(unit.ka * (m - by));
+    if (unit.two) z1 *= __builtin_amdgcn_exp2f(unit.kb * (m - by));
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        z += __builtin_amdgcn_exp2f(unit.ka * (f[u][i] - by));
+        if (unit.two) z1 += __builtin_amdgcn_exp2f(unit.kb * (f[u][i] - by));
+      }
+    m = top;
+  }
+  const float all = block_reduce<NW>(m, lds, [](float a, float b) { return fmaxf(a, b); });
+  const float own = m == -INFINITY && z == 0.0f ? 0.0f : m - all;   // a thread without a column has nothing to add
+  z = block_sum<NW>(z * __builtin_amdgcn_exp2f(unit.ka * own), lds);
+  z1 = unit.two ? block_sum<NW>(z1 * __builtin_amdgcn_exp2f(unit.kb * own), lds) : z;
+  if (all == -INFINITY) z = z1 = NAN;
+  distill_loss<NW>(g, token, r, e, all, z, z1, lds);
+  if (!g.dS) return;
+  const DistillExp x(g, r, all);
+  const DistillGrad d(g, r, x.two, z, z1);
+  T* const out = (T*)g.dS + token * g.ldd;
+  for (int c0 = threadIdx.x * CH; c0 < g.vocab; c0 += U * STEP) {
+    f32x4_t v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = row_piece<T>(row, c0 + u * STEP, g.vocab);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int c = c0 + u * STEP;
+      if (c < g.vocab) st_piece<T>(out + c, grad_piece<T>(v[u], x, d), g.vocab - c);
+    }
+  }
+  store_entries<T, NW>(g, token, r, e, x, d);
+}
+
+// The gradient from the stored logarithms of the sums.
+template <class T, int NW, bool NT>
+__global__ __launch_bounds__(NW * 64) void k_distill_bwd(DistillArgs g) {
+  constexpr int CH = 16 / sizeof(T), STEP = NW * 64 * CH, U = 4;
+  __shared__ DistillToken<DL_ENTRIES> e;
+  __shared__ float lds[NW];
+  const int64_t token = blockIdx.x;
+  const float soft = g.lse[2 * token], hard = g.lse[2 * token + 1];
+  const DistillRow r = distill_entries<T, NW>(g, token, e, lds);
+  if (!r.soft && !r.hard) return zero_row<T, NW>(g, token);
+  DistillExp x(g, r, 0.0f);
+  x.oa = kLog2e * (r.soft ? soft : hard);
+  x.ob = kLog2e * hard;
+  const DistillGrad d(g, r, x.two, 1.0f, 1.0f);
+  const T* const row = (const T*)g.S + token * g.lds;
+  T* const out = (T*)g.dS + token * g.ldd;
+  for (int c0 = threadIdx.x * CH; c0 < g.vocab; c0 += U * STEP) {
+    f32x4_t v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = row_piece<T>(row, c0 + u * STEP, g.vocab);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int c = c0 + u * STEP;
+      if (c < g.vocab) st_row_piece<T, NT>(out + c, grad_piece<T>(v[u], x, d), g.vocab - c);
+    }
+  }
+  store_entries<T, NW>(g, token, r, e, x, d);
+}
+
+}  // namespace occ

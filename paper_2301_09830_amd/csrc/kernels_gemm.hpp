@@ -738,10 +738,10 @@ using Form128 = Form<2, 4, 4, 2, 4>;
 using Form64 = Form<4, 2, 1, 2, 4>;
 using FormDirect = Form<4, 2, 1, 2, 2, true>;
 
-// Block `block` of a product: all of its tile's K, or one part of it.  T: type
+// Tile (tm, tn) of a product: all of its K, or part `split` of it.  T: type
 // of the operands, TE: of the layer (fp32 on bf16 planes: T bf16, TE fp32).
 template <class T, class TE, class F, bool AKS, bool BKS, int EP>
-__device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_char* lds) {
+__device__ __forceinline__ void gemm_tile(const GemmArgs& g, int tm, int tn, int split, lds_char* lds) {
   constexpr int ES = sizeof(T), S = F::S, NW = F::NW, WM = F::WM, WN = F::WN, FA = F::FA, FB = F::FB;
   constexpr int BM = F::BM, BN = F::BN;
   constexpr bool PP = S == 2 && !F::DIRECT, SEG = sizeof(T) != sizeof(TE);
@@ -752,11 +752,6 @@ __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_cha
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
   const int wave = wave_id(), lane = threadIdx.x & 63;
   const int wm = wave / WN, wn = wave % WN;
-  int tm, tn;
-  const int per_split = g.tiles_m * g.tiles_n;
-  const int t = xcd_order(block, per_split * g.splits);
-  const int split = t / per_split;
-  band_tile(t - split * per_split, g.tiles_m, g.tiles_n, tm, tn);
   const int kt0 = split * g.k_per_split;
   const int nk = min(g.k_per_split, g.tiles_k - kt0);
   const int m0 = tm * BM;
@@ -1065,6 +1060,17 @@ __device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_cha
       }
     }
   }
+}
+
+// Block `block` of a product.
+template <class T, class TE, class F, bool AKS, bool BKS, int EP>
+__device__ __forceinline__ void gemm_block(const GemmArgs& g, int block, lds_char* lds) {
+  const int per_split = g.tiles_m * g.tiles_n;
+  const int t = xcd_order(block, per_split * g.splits);
+  const int split = t / per_split;
+  int tm, tn;
+  band_tile(t - split * per_split, g.tiles_m, g.tiles_n, tm, tn);
+  gemm_tile<T, TE, F, AKS, BKS, EP>(g, tm, tn, split, lds);
 }
 
 template <class T, class TE, class F, int EP>

@@ -50,10 +50,10 @@ __device__ __forceinline__ float wave_sum(float x) {
 constexpr int DOT_WAVES = 4;
 
 template <class T, int NT, bool GATED>
-__global__ __launch_bounds__(DOT_WAVES * 64) void k_dot(SkinnyArgs g) {
+__device__ __forceinline__ void dot_block(const SkinnyArgs& g, int block) {
   constexpr int CH = 16 / sizeof(T), BK = 64 * CH;
   const int lane = threadIdx.x & 63;
-  const int id = blockIdx.x * DOT_WAVES + wave_id();
+  const int id = block * DOT_WAVES + wave_id();
   const int n0 = GATED ? id : 2 * id;
   if (n0 >= g.fwd.out) return;
   const bool both = GATED || n0 + 1 < g.fwd.out;
@@ -123,6 +123,11 @@ __global__ __launch_bounds__(DOT_WAVES * 64) void k_dot(SkinnyArgs g) {
   }
 }
 
+template <class T, int NT, bool GATED>
+__global__ __launch_bounds__(DOT_WAVES * 64) void k_dot(SkinnyArgs g) {
+  dot_block<T, NT, GATED>(g, blockIdx.x);
+}
+
 // A block makes 16 columns of Y (gated: the 16 rows of both projections) for
 // up to 16 NT tokens: its SK_WAVES waves take K in turns of one tile of 128
 // bytes a row, with weights and tokens loaded straight into the registers of
@@ -131,12 +136,12 @@ __global__ __launch_bounds__(DOT_WAVES * 64) void k_dot(SkinnyArgs g) {
 constexpr int SK_WAVES = 8;
 
 template <class T, int NT, bool GATED>
-__global__ __launch_bounds__(SK_WAVES * 64) void k_skinny(SkinnyArgs g) {
+__device__ __forceinline__ void skinny_block(const SkinnyArgs& g, int block) {
   constexpr int ES = sizeof(T), CH = 16 / ES, BK = kRowBytes / ES, NW = GATED ? 2 : 1;
   __shared__ f32x4_t sums[SK_WAVES][NW * NT][64];
   const int wave = wave_id(), lane = threadIdx.x & 63;
   const int i = lane & 15, q = lane >> 4;
-  const int n0 = blockIdx.x * 16;
+  const int n0 = block * 16;
   const int row = min(n0 + i, g.fwd.out - 1);
   const T* w[NW];
   w[0] = (const T*)g.W + (int64_t)row * g.ldw + q * CH;
@@ -221,6 +226,11 @@ __global__ __launch_bounds__(SK_WAVES * 64) void k_skinny(SkinnyArgs g) {
   }
 }
 
+template <class T, int NT, bool GATED>
+__global__ __launch_bounds__(SK_WAVES * 64) void k_skinny(SkinnyArgs g) {
+  skinny_block<T, NT, GATED>(g, blockIdx.x);
+}
+
 // ----------------------------------------------------------------------------
 // before the products: the gradient at the pre-activation, aligned operands
 // ----------------------------------------------------------------------------
@@ -261,14 +271,12 @@ __device__ __forceinline__ void st_planes(uint16_t* p, int64_t plane, f32x4_t v,
   }
 }
 
+// Rows r0 .. r1 - 1 of the bx-th block of columns; their bias sums are strip `by`.
 template <class T, bool GATED>
-__device__ __forceinline__ void dz_block(const DzArgs& g, int block) {
+__device__ __forceinline__ void dz_rows(const DzArgs& g, int bx, int by, int64_t r0, int64_t r1) {
   __shared__ f32x4_t part[GATED ? 2 : 1][DZ_ROWS][DZ_LANES];
   const int cx = threadIdx.x & (DZ_LANES - 1), ry = threadIdx.x / DZ_LANES;
-  const int by = block / g.across, bx = block - by * g.across;
   const int n = (bx * DZ_LANES + cx) * 4, left = g.out - n;
-  const int64_t r0 = (int64_t)by * g.strip;
-  const int64_t r1 = min(r0 + g.strip, (int64_t)g.tokens);
   f32x4_t s0 = {}, s1 = {};
   if (left > 0) {
     for (int64_t m = r0 + ry; m < r1; m += DZ_ROWS) {
@@ -318,6 +326,13 @@ __device__ __forceinline__ void dz_block(const DzArgs& g, int block) {
     const int64_t width = GATED ? 2 * (int64_t)g.out : g.out;
     st_quad(g.bias_part + by * width + ry * (int64_t)g.out + n, s, left);
   }
+}
+
+template <class T, bool GATED>
+__device__ __forceinline__ void dz_block(const DzArgs& g, int block) {
+  const int by = block / g.across;
+  const int64_t r0 = (int64_t)by * g.strip;
+  dz_rows<T, GATED>(g, block - by * g.across, by, r0, min(r0 + g.strip, (int64_t)g.tokens));
 }
 
 // Copy of an operand with rows on 16 bytes, whole pieces and zeros behind

@@ -1,4 +1,5 @@
-// liboptcc C ABI of the stage operators: linear and gated layers, AdamW.
+// liboptcc C ABI of the stage operators: linear and gated layers, AdamW; at the
+// end, in headers of their own, the layers of experts and the loss.
 // Argument validation and launch sequencing, on the host (plan_layers.hpp: the
 // layers' forms, tiles and workspaces).
 #include <hip/hip_runtime.h>
@@ -613,3 +614,8 @@ occ_status_t occ_adamw_step(const occ_param_t* params, int count, const occ_adam
 }
 
 }  // extern "C"
+
+// the layers of experts and the loss
+#include "experts_ops.hpp"
+#include "route_ops.hpp"
+#include "distill_ops.hpp"

@@ -17,6 +17,7 @@ import contextlib
 import ctypes
 import os
 import re
+from typing import Any, NamedTuple
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "liboptcc.so")
@@ -33,6 +34,7 @@ OCC_MAX_ITERS = 64
 OCC_ACT_NONE, OCC_ACT_RELU, OCC_ACT_GELU, OCC_ACT_GELU_TANH, OCC_ACT_SILU = range(5)
 OCC_GRAD_ACCUMULATE = 1
 OCC_SCALE_RUN = 256   # columns that share one scale of an 8-bit moment
+OCC_MAX_EXPERTS, OCC_MAX_CHOICES, OCC_MAX_TEACHER = 1024, 32, 1024
 
 STATUS_NAMES = {
     0: "OCC_OK", 1: "OCC_E_NULL", 2: "OCC_E_SHAPE", 3: "OCC_E_RANK", 4: "OCC_E_ITERS",
@@ -131,6 +133,86 @@ class occ_linear_grad_t(ctypes.Structure):
     ]
 
 
+class occ_experts_t(ctypes.Structure):
+    _fields_ = [
+        ("l", occ_linear_t),
+        ("experts", ctypes.c_int64),
+        ("stride_w", ctypes.c_int64),
+        ("offsets", ctypes.c_void_p),
+        ("flags", ctypes.c_void_p),
+    ]
+
+
+class occ_experts_grad_t(ctypes.Structure):
+    _fields_ = [
+        ("l", occ_linear_grad_t),
+        ("experts", ctypes.c_int64),
+        ("stride_w", ctypes.c_int64),
+        ("stride_dw", ctypes.c_int64),
+        ("offsets", ctypes.c_void_p),
+        ("flags", ctypes.c_void_p),
+    ]
+
+
+class occ_route_t(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("k", ctypes.c_int32),
+        ("renorm", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("tokens", ctypes.c_int64),
+        ("experts", ctypes.c_int64),
+        ("logits", ctypes.c_void_p),
+        ("ldl", ctypes.c_int64),
+        ("index", ctypes.c_void_p),
+        ("weights", ctypes.c_void_p),
+        ("offsets", ctypes.c_void_p),
+        ("order", ctypes.c_void_p),
+        ("slots", ctypes.c_void_p),
+    ]
+
+
+class occ_exchange_t(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("k", ctypes.c_int32),
+        ("tokens", ctypes.c_int64),
+        ("experts", ctypes.c_int64),
+        ("rows", ctypes.c_int64),
+        ("width", ctypes.c_int64),
+        ("offsets", ctypes.c_void_p),
+        ("order", ctypes.c_void_p),
+        ("slots", ctypes.c_void_p),
+        ("flags", ctypes.c_void_p),
+    ]
+
+
+class occ_distill_t(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("t_dtype", ctypes.c_int32),
+        ("tokens", ctypes.c_int64),
+        ("vocab", ctypes.c_int64),
+        ("S", ctypes.c_void_p),
+        ("lds", ctypes.c_int64),
+        ("k", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("index", ctypes.c_void_p),
+        ("ldi", ctypes.c_int64),
+        ("teacher", ctypes.c_void_p),
+        ("ldt", ctypes.c_int64),
+        ("labels", ctypes.c_void_p),
+        ("scale", ctypes.c_void_p),
+        ("temperature", ctypes.c_float),
+        ("alpha", ctypes.c_float),
+        ("loss", ctypes.c_void_p),
+        ("lse", ctypes.c_void_p),
+        ("dS", ctypes.c_void_p),
+        ("ldds", ctypes.c_int64),
+        ("flags", ctypes.c_void_p),
+    ]
+
+
 class occ_param_t(ctypes.Structure):
     _fields_ = [
         ("rows", ctypes.c_int64),
@@ -224,6 +306,33 @@ _SIGS = {
                                       ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     "occ_gated_bwd": (ctypes.c_int, [ctypes.POINTER(occ_linear_grad_t), ctypes.c_uint,
                                      ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    **{f"occ_experts_{n}_{d}_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(t)])
+       for n in ("linear", "gated") for d, t in (("fwd", occ_experts_t),
+                                                 ("bwd", occ_experts_grad_t))},
+    **{f"occ_experts_{n}_fwd": (ctypes.c_int, [ctypes.POINTER(occ_experts_t), ctypes.c_void_p,
+                                               ctypes.c_size_t, ctypes.c_void_p])
+       for n in ("linear", "gated")},
+    **{f"occ_experts_{n}_bwd": (ctypes.c_int, [ctypes.POINTER(occ_experts_grad_t), ctypes.c_uint,
+                                               ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p])
+       for n in ("linear", "gated")},
+    "occ_route_fwd_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(occ_route_t)]),
+    "occ_route_fwd": (ctypes.c_int, [ctypes.POINTER(occ_route_t), ctypes.c_void_p,
+                                     ctypes.c_size_t, ctypes.c_void_p]),
+    "occ_route_bwd": (ctypes.c_int, [ctypes.POINTER(occ_route_t), ctypes.c_void_p,
+                                     ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]),
+    "occ_dispatch": (ctypes.c_int, [ctypes.POINTER(occ_exchange_t), ctypes.c_void_p,
+                                    ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
+                                    ctypes.c_void_p]),
+    "occ_combine": (ctypes.c_int, [ctypes.POINTER(occ_exchange_t), ctypes.c_void_p,
+                                   ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                   ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
+                                   ctypes.c_void_p]),
+    "occ_combine_bwd": (ctypes.c_int, [ctypes.POINTER(occ_exchange_t), ctypes.c_void_p,
+                                       ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                       ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
+                                       ctypes.c_void_p, ctypes.c_void_p]),
+    "occ_distill_fwd": (ctypes.c_int, [ctypes.POINTER(occ_distill_t), ctypes.c_void_p]),
+    "occ_distill_bwd": (ctypes.c_int, [ctypes.POINTER(occ_distill_t), ctypes.c_void_p]),
     "occ_adamw_step": (ctypes.c_int, [ctypes.POINTER(occ_param_t), ctypes.c_int,
                                       ctypes.POINTER(occ_adamw_t), ctypes.c_void_p]),
     "occ_profile_begin": (ctypes.c_int, []),
@@ -597,8 +706,15 @@ def _layers():
         from . import _layers as module
         names = [n + e for e in ("", "_workspace_bytes")
                  for n in ("occ_linear_fwd", "occ_gated_fwd", "occ_linear_bwd", "occ_gated_bwd")]
-        module.setup(*(ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in names),
-                     torch._C._cuda_getCurrentRawStream)
+        def address(name):
+            return ctypes.cast(getattr(L, name), ctypes.c_void_p).value
+
+        module.setup(*map(address, names), torch._C._cuda_getCurrentRawStream)
+        experts = [f"occ_experts_{n}_{d}{e}" for e in ("", "_workspace_bytes")
+                   for d in ("fwd", "bwd") for n in ("linear", "gated")]
+        module.setup_experts(*map(address, experts + [
+            "occ_route_fwd", "occ_route_fwd_workspace_bytes", "occ_route_bwd", "occ_dispatch",
+            "occ_combine", "occ_combine_bwd", "occ_distill_fwd", "occ_distill_bwd"]))
         _layers_module = module
     return _layers_module
 
@@ -669,6 +785,166 @@ def occ_gated_bwd(dY, X=None, W=None, Z=None, act: int = OCC_ACT_SILU, dX=None, 
     if stream is not None:
         return _on(stream, occ_gated_bwd, dY, X, W, Z, act, dX, dW, dbias, accumulate, ws)
     _layer_bwd("occ_gated_bwd", True, dY, X, W, Z, act, dX, dW, dbias, accumulate, ws)
+
+
+# ----------------------------------------------------------------------------
+# layers of experts
+# ----------------------------------------------------------------------------
+class Route(NamedTuple):
+    """The experts of every token and the plan of their rows (occ_route_fwd)."""
+    index: Any     # tokens x k int32: the experts chosen, -1: none
+    weights: Any   # tokens x k float32
+    offsets: Any   # experts + 1 int32: where each expert's rows begin, and their number
+    order: Any     # tokens k int32: the entries (token k + j), expert by expert
+    slots: Any     # tokens x k int32: each entry's place in order, -1: none
+
+
+def _made(name: str, result):
+    """What a native call made, its status checked."""
+    if result[0]:
+        raise OccError(name, result[0])
+    return result[1:]
+
+
+def occ_route_fwd(logits, k: int, renorm: bool = True, route=None, ws=None, stream=None) -> Route:
+    """The k largest logits of each token (tokens x experts, float32 or bfloat16),
+    their softmax weights (renorm: among the chosen; else over all the experts)
+    and the plan of the experts' rows.  route: the tensors to write to."""
+    if stream is not None:
+        return _on(stream, occ_route_fwd, logits, k, renorm, route, ws)
+    out = (None,) * 5 if route is None else route
+    return Route(*_made("occ_route_fwd", (_layers_module or _layers()).route_forward(
+        logits, k, bool(renorm), *out, ws)))
+
+
+def occ_route_bwd(dweights, logits, route, renorm: bool = True, dlogits=None, stream=None):
+    """Gradient of the logits from that of the weights (float32, tokens x k);
+    dlogits may be logits itself."""
+    if stream is not None:
+        return _on(stream, occ_route_bwd, dweights, logits, route, renorm, dlogits)
+    return _made("occ_route_bwd", (_layers_module or _layers()).route_backward(
+        dweights, logits, route.index, route.weights, bool(renorm), dlogits))[0]
+
+
+def occ_dispatch(X, route, Xs=None, flags=None, stream=None):
+    """Xs: the tokens' rows of X in the order of the experts (route.order).  Rows
+    behind the last expert's are left alone.  Its gradient is occ_combine of dXs
+    without weights."""
+    if stream is not None:
+        return _on(stream, occ_dispatch, X, route, Xs, flags)
+    return _made("occ_dispatch", (_layers_module or _layers()).dispatch(
+        X, route.offsets, route.order, route.slots, Xs, flags))[0]
+
+
+def occ_combine(Ys, route, weights=None, R=None, Y=None, flags=None, stream=None):
+    """Y: for each token the sum of its experts' rows of Ys, times `weights`
+    (float32, tokens x k) if given, and R.  R may be Y."""
+    if stream is not None:
+        return _on(stream, occ_combine, Ys, route, weights, R, Y, flags)
+    return _made("occ_combine", (_layers_module or _layers()).combine(
+        Ys, route.slots, weights, R, Y, flags))[0]
+
+
+def occ_combine_bwd(dY, Ys, route, weights=None, dYs=None, dweights=None, flags=None, stream=None):
+    """(dYs, dweights) of occ_combine; Ys None: dYs alone.  The gradient of R is
+    dY itself."""
+    if stream is not None:
+        return _on(stream, occ_combine_bwd, dY, Ys, route, weights, dYs, dweights, flags)
+    return _made("occ_combine_bwd", (_layers_module or _layers()).combine_backward(
+        dY, Ys, route.order, route.slots, weights, dYs, dweights, flags))
+
+
+def _experts_fwd(name: str, gated: bool, X, W, offsets, bias, act, R, Y, Z, flags, ws):
+    if Y is None:
+        if X.dim() != 2 or W.dim() != 3:
+            raise ValueError("X must be 2-D and W 3-D")
+        Y = X.new_empty((X.shape[0], W.shape[1] // 2 if gated else W.shape[1]))
+    status = (_layers_module or _layers()).experts_forward(gated, X, W, offsets, bias, act, R, Y,
+                                                           Z, flags, ws)
+    if status:
+        raise OccError(name, status)
+    return Y
+
+
+def occ_experts_linear_fwd(X, W, offsets, bias=None, act: int = OCC_ACT_NONE, R=None, Y=None,
+                           Z=None, flags=None, ws=None, stream=None):
+    """occ_linear_fwd with a weight (experts x out x in) and bias (experts x out) of
+    each expert, whose rows of X, R, Y and Z offsets bounds (int32, experts + 1,
+    on the GPU).  flags: an int32 word that takes OCC_F_BAD_ROWS where offsets
+    fit no plan.  Rows that belong to no expert are left alone.  Returns Y."""
+    if stream is not None:
+        return _on(stream, occ_experts_linear_fwd, X, W, offsets, bias, act, R, Y, Z, flags, ws)
+    return _experts_fwd("occ_experts_linear_fwd", False, X, W, offsets, bias, act, R, Y, Z, flags,
+                        ws)
+
+
+def occ_experts_gated_fwd(X, W, offsets, bias=None, act: int = OCC_ACT_SILU, R=None, Y=None,
+                          Z=None, flags=None, ws=None, stream=None):
+    """occ_gated_fwd with a weight (experts x 2 out x in) of each expert; as
+    occ_experts_linear_fwd."""
+    if stream is not None:
+        return _on(stream, occ_experts_gated_fwd, X, W, offsets, bias, act, R, Y, Z, flags, ws)
+    return _experts_fwd("occ_experts_gated_fwd", True, X, W, offsets, bias, act, R, Y, Z, flags, ws)
+
+
+def _experts_bwd(name: str, gated: bool, dY, offsets, X, W, Z, act, dX, dW, dbias, accumulate,
+                 flags, ws):
+    status = (_layers_module or _layers()).experts_backward(
+        gated, dY, X, W, offsets, Z, act, dX, dW, dbias, bool(accumulate), flags, ws)
+    if status:
+        raise OccError(name, status)
+
+
+def occ_experts_linear_bwd(dY, offsets, X=None, W=None, Z=None, act: int = OCC_ACT_NONE, dX=None,
+                           dW=None, dbias=None, accumulate: bool = False, flags=None, ws=None,
+                           stream=None) -> None:
+    """Gradients of occ_experts_linear_fwd, each made if a tensor is given for it;
+    as occ_linear_bwd.  An expert without rows has zeros in dW and dbias."""
+    if stream is not None:
+        return _on(stream, occ_experts_linear_bwd, dY, offsets, X, W, Z, act, dX, dW, dbias,
+                   accumulate, flags, ws)
+    _experts_bwd("occ_experts_linear_bwd", False, dY, offsets, X, W, Z, act, dX, dW, dbias,
+                 accumulate, flags, ws)
+
+
+def occ_experts_gated_bwd(dY, offsets, X=None, W=None, Z=None, act: int = OCC_ACT_SILU, dX=None,
+                          dW=None, dbias=None, accumulate: bool = False, flags=None, ws=None,
+                          stream=None) -> None:
+    """Gradients of occ_experts_gated_fwd; as occ_gated_bwd."""
+    if stream is not None:
+        return _on(stream, occ_experts_gated_bwd, dY, offsets, X, W, Z, act, dX, dW, dbias,
+                   accumulate, flags, ws)
+    _experts_bwd("occ_experts_gated_bwd", True, dY, offsets, X, W, Z, act, dX, dW, dbias,
+                 accumulate, flags, ws)
+
+
+# ----------------------------------------------------------------------------
+# loss
+# ----------------------------------------------------------------------------
+def occ_distill_fwd(S, index, teacher, temperature: float = 1.0, alpha: float = 1.0, labels=None,
+                    scale=None, loss=None, lse=None, dS=None, flags=None, stream=None):
+    """The loss (float32, one value a token) of logits S (tokens x vocab, float32 or
+    bfloat16) against the teacher's top logits (tokens x k, float32 or bfloat16)
+    at columns `index` (int32; a negative one is masked), alpha of it, and against
+    labels (int32; a negative one is none), 1 - alpha.  scale: a factor for each
+    token.  dS, if given, receives the gradient of the sum of the losses in the
+    same pass (it may be S); lse (float32, tokens x 2) what occ_distill_bwd needs."""
+    if stream is not None:
+        return _on(stream, occ_distill_fwd, S, index, teacher, temperature, alpha, labels, scale,
+                   loss, lse, dS, flags)
+    return _made("occ_distill_fwd", (_layers_module or _layers()).distill(
+        False, S, index, teacher, labels, scale, temperature, alpha, loss, lse, dS, flags))[0]
+
+
+def occ_distill_bwd(S, index, teacher, lse, temperature: float = 1.0, alpha: float = 1.0,
+                    labels=None, scale=None, dS=None, flags=None, stream=None):
+    """The gradient dS of occ_distill_fwd's losses from the lse that it stored.
+    scale: the forward's, times the gradient of each loss.  dS may be S."""
+    if stream is not None:
+        return _on(stream, occ_distill_bwd, S, index, teacher, lse, temperature, alpha, labels,
+                   scale, dS, flags)
+    return _made("occ_distill_bwd", (_layers_module or _layers()).distill(
+        True, S, index, teacher, labels, scale, temperature, alpha, None, lse, dS, flags))[1]
 
 
 def make_param(W, m, v, G=None, P=None, Q=None, W16=None, m_scale=None, v_scale=None,
