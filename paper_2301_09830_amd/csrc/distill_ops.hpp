@@ -102,23 +102,23 @@ occ_status_t start_distill(const occ_distill_t& d, const DistillArgs& all, hipSt
 // to fill the chip with fours.
 constexpr int64_t kDistillTokens = 512;
 
+template <class T, int NW>
+occ_status_t distill_steps(const occ_distill_t& d, const DistillArgs& a, int64_t whole, hipStream_t s) {
+  if (whole <= 2) return start_distill<T, NW, 2>(d, a, s);
+  if (whole <= 4) return start_distill<T, NW, 4>(d, a, s);
+  if (whole <= 8) return start_distill<T, NW, 8>(d, a, s);
+  return start_distill<T, NW, 16>(d, a, s);
+}
+
 template <class T>
 occ_status_t run_distill(const occ_distill_t& d, hipStream_t s) {
   const DistillArgs a = distill_args(d);
-  const int64_t pieces = div_up(d.vocab, 16 / (int64_t)sizeof(T));
-  const int64_t four = div_up(pieces, 256), sixteen = div_up(pieces, 1024);
+  const int64_t four = d.vocab / (256 * (16 / (int64_t)sizeof(T)));   // whole steps of four waves
   if (d.tokens >= kDistillTokens || four <= 2) {
-    if (four <= 2) return start_distill<T, 4, 2>(d, a, s);
-    if (four <= 4) return start_distill<T, 4, 4>(d, a, s);
-    if (four <= 8) return start_distill<T, 4, 8>(d, a, s);
-    if (four <= 16) return start_distill<T, 4, 16>(d, a, s);
-    if (four <= 26) return start_distill<T, 4, 26>(d, a, s);
-    if (four <= 52) return start_distill<T, 8, 26>(d, a, s);
+    if (four <= 16) return distill_steps<T, 4>(d, a, four, s);
+    if (four / 2 <= 16) return distill_steps<T, 8>(d, a, four / 2, s);
   }
-  if (sixteen <= 2) return start_distill<T, 16, 2>(d, a, s);
-  if (sixteen <= 4) return start_distill<T, 16, 4>(d, a, s);
-  if (sixteen <= 8) return start_distill<T, 16, 8>(d, a, s);
-  if (sixteen <= 26) return start_distill<T, 16, 26>(d, a, s);
+  if (four / 4 <= 16) return distill_steps<T, 16>(d, a, four / 4, s);
   return by_tokens(d, a, 1024, [&](const DistillArgs& b, dim3 grid) {
     return launch("distill", s, [&] { hipLaunchKernelGGL((k_distill_long<T>), grid, dim3(1024), 0, s, b); });
   });

@@ -283,8 +283,42 @@ __device__ __forceinline__ void ignored_token(const DistillArgs& g, int64_t toke
   if (g.dS) zero_row<T, NW>(g, token);
 }
 
-// A token a block, its row in the registers of NW waves, VPT pieces of 16 bytes
-// a thread: one pass over memory.
+// A token a block, its row in the registers of NW waves: one pass over memory.
+// A step is a piece of 16 bytes a thread; of a row's steps at most VPT are
+// whole, and one more may be partial.  A piece is widened anew in each pass
+// over the registers (`fresh`): kept from one to the next, bf16 rows would take
+// twice the registers that they are loaded into.  The array has nine
+// pieces or more: the compiler makes one vector of up to 32 registers, which a
+// conditional load of a piece copies as a whole, and spills it.
+__device__ __forceinline__ f32x4_t fresh(f32x4_t& v) {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+template <class T>
+__device__ __forceinline__ float piece_max(f32x4_t v, float m) {
+  constexpr int CH = 16 / sizeof(T);
+  float f[CH];
+  widen<T>(v, f);
+#pragma unroll
+  for (int i = 0; i < CH; ++i) m = fmaxf(m, f[i]);
+  return m;
+}
+
+template <class T>
+__device__ __forceinline__ void piece_sums(f32x4_t v, const DistillExp& x, float& z, float& z1) {
+  constexpr int CH = 16 / sizeof(T);
+  float f[CH];
+  widen<T>(v, f);
+  if (x.two) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) z1 += x.b(f[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < CH; ++i) z += x.a(f[i]);
+}
+
 template <class T, int NW, int VPT, bool NT>
 __global__ __launch_bounds__(NW * 64, 4) void k_distill(DistillArgs g) {
   constexpr int CH = 16 / sizeof(T), STEP = NW * 64 * CH;
@@ -292,36 +326,27 @@ __global__ __launch_bounds__(NW * 64, 4) void k_distill(DistillArgs g) {
   __shared__ float lds[NW];
   const int64_t token = blockIdx.x;
   const T* const row = (const T*)g.S + token * g.lds;
-  const int c0 = threadIdx.x * CH;
-  f32x4_t v[VPT];
+  const int c0 = threadIdx.x * CH, whole = g.vocab / STEP, c1 = c0 + whole * STEP;
+  f32x4_t v[VPT < 9 ? 9 : VPT], last;
   if (!g.scale || g.scale[token] != 0.0f) {   // on its way while the entries are read
 #pragma unroll
-    for (int p = 0; p < VPT; ++p) v[p] = row_piece<T>(row, c0 + p * STEP, g.vocab);
+    for (int p = 0; p < VPT; ++p)
+      if (p < whole) v[p] = ld_piece<T>(row + c0 + p * STEP, CH);
+    last = row_piece<T>(row, c1, g.vocab);
   }
   const DistillRow r = distill_entries<T, NW>(g, token, e, lds);
   if (!r.soft && !r.hard) return ignored_token<T, NW>(g, token);
-  float m = -INFINITY;
+  float m = piece_max<T>(fresh(last), -INFINITY);
 #pragma unroll
-  for (int p = 0; p < VPT; ++p) {
-    float f[CH];
-    widen<T>(v[p], f);
-#pragma unroll
-    for (int i = 0; i < CH; ++i) m = fmaxf(m, f[i]);
-  }
+  for (int p = 0; p < VPT; ++p)
+    if (p < whole) m = piece_max<T>(fresh(v[p]), m);
   m = block_reduce<NW>(m, lds, [](float a, float b) { return fmaxf(a, b); });
   const DistillExp x(g, r, m);
   float z = 0.0f, z1 = 0.0f;
 #pragma unroll
-  for (int p = 0; p < VPT; ++p) {
-    float f[CH];
-    widen<T>(v[p], f);
-    if (x.two) {
-#pragma unroll
-      for (int i = 0; i < CH; ++i) z1 += x.b(f[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < CH; ++i) z += x.a(f[i]);
-  }
+  for (int p = 0; p < VPT; ++p)
+    if (p < whole) piece_sums<T>(fresh(v[p]), x, z, z1);
+  piece_sums<T>(fresh(last), x, z, z1);
   z = block_sum<NW>(z, lds);
   z1 = x.two ? block_sum<NW>(z1, lds) : z;
   distill_loss<NW>(g, token, r, e, m, z, z1, lds);
@@ -329,10 +354,9 @@ __global__ __launch_bounds__(NW * 64, 4) void k_distill(DistillArgs g) {
   const DistillGrad d(g, r, x.two, z, z1);
   T* const out = (T*)g.dS + token * g.ldd;
 #pragma unroll
-  for (int p = 0; p < VPT; ++p) {
-    const int c = c0 + p * STEP;
-    if (c < g.vocab) st_row_piece<T, NT>(out + c, grad_piece<T>(v[p], x, d), g.vocab - c);
-  }
+  for (int p = 0; p < VPT; ++p)
+    if (p < whole) st_row_piece<T, NT>(out + c0 + p * STEP, grad_piece<T>(fresh(v[p]), x, d), CH);
+  if (c1 < g.vocab) st_row_piece<T, NT>(out + c1, grad_piece<T>(fresh(last), x, d), g.vocab - c1);
   store_entries<T, NW>(g, token, r, e, x, d);
 }
 
