@@ -191,25 +191,6 @@ struct DistillGrad {
   }
 };
 
-// A piece of a row, -inf behind its end.
-template <class T>
-__device__ __forceinline__ f32x4_t row_piece(const T* row, int c, int vocab) {
-  constexpr int CH = 16 / sizeof(T);
-  if (c + CH <= vocab) return ld_piece<T>(row + c, CH);
-  const uint32_t low = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
-  f32x4_t v;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(low);
-  if (c >= vocab) return v;
-  T e[CH];
-  __builtin_memcpy(e, &v, 16);
-#pragma unroll
-  for (int i = 0; i < CH; ++i)
-    if (c + i < vocab) e[i] = row[c + i];
-  __builtin_memcpy(&v, e, 16);
-  return v;
-}
-
 template <class T>
 __device__ __forceinline__ f32x4_t grad_piece(f32x4_t v, const DistillExp& x, const DistillGrad& d) {
   constexpr int CH = 16 / sizeof(T);

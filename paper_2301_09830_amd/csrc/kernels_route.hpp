@@ -6,6 +6,64 @@
 
 namespace occ {
 
+template <class T>
+__device__ __forceinline__ void st_piece(T* p, f32x4_t v, int left) {
+  constexpr int CH = 16 / sizeof(T);
+  if (left >= CH) {
+    if constexpr (sizeof(T) == 4) *(f4u_t*)p = f4u_t{v[0], v[1], v[2], v[3]};
+    else *(u4h_t*)p = __builtin_bit_cast(u4h_t, v);
+    return;
+  }
+  T e[CH];
+  __builtin_memcpy(e, &v, 16);
+#pragma unroll
+  for (int i = 0; i < CH; ++i)
+    if (i < left) p[i] = e[i];
+}
+
+// A piece of a row, -inf behind its end.
+template <class T>
+__device__ __forceinline__ f32x4_t row_piece(const T* row, int c, int vocab) {
+  constexpr int CH = 16 / sizeof(T);
+  if (c + CH <= vocab) return ld_piece<T>(row + c, CH);
+  const uint32_t low = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+  f32x4_t v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(low);
+  if (c >= vocab) return v;
+  T e[CH];
+  __builtin_memcpy(e, &v, 16);
+#pragma unroll
+  for (int i = 0; i < CH; ++i)
+    if (c + i < vocab) e[i] = row[c + i];
+  __builtin_memcpy(&v, e, 16);
+  return v;
+}
+
+// The elements of a piece as fp32, and back.
+template <class T>
+__device__ __forceinline__ void widen(f32x4_t v, float* e) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e[i] = v[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      e[2 * i] = bf16_lo(__float_as_uint(v[i]));
+      e[2 * i + 1] = bf16_hi(__float_as_uint(v[i]));
+    }
+  }
+}
+
+template <class T>
+__device__ __forceinline__ f32x4_t narrow(const float* e) {
+  if constexpr (sizeof(T) == 4) return f32x4_t{e[0], e[1], e[2], e[3]};
+  f32x4_t v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(bf16_pack2(e[2 * i], e[2 * i + 1]));
+  return v;
+}
+
 // ----------------------------------------------------------------------------
 // choice of the experts
 // ----------------------------------------------------------------------------
@@ -86,14 +144,186 @@ __device__ __forceinline__ void load_logits(const void* p, int64_t ld, int64_t t
   }
 }
 
-// The k largest logits of a token, the lower index first among equals: lane j
-// of the L that share it ends with the j-th choice (index -1, weight 0: there
-// is none).  One pick a round: the largest of the lanes' largest; in bf16 the
-// value and the index fit one word, in fp32 they take two.  Bound by these
-// rounds' instructions: 4 tokens a wave at up to 256 experts.
-template <class T, int L, int Q>
-__device__ __forceinline__ void choose(const RouteArgs& g, int64_t token, int lane, int& index, float& weight) {
-  constexpr int V = 4 * Q;
+// Choices of a token: index -1 and weight 0 where there is none.  The lower
+// index comes first among equals, so a logit and its column are one key: in
+// bf16 they fit one word; in fp32 they take 42 bits of a double's fraction,
+// whose maximum and minimum are one instruction too.
+template <class T> struct RouteKey;
+
+// What is never chosen has the rank of -inf, the lowest.
+constexpr uint32_t kLowestRank = 0x007fffffu;
+
+__device__ __forceinline__ uint32_t rank_or_lowest(float x) {
+  const uint32_t u = __float_as_uint(fmaxf(x + 0.0f, -INFINITY));   // -0 is 0, NaN -inf
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+
+template <> struct RouteKey<uint16_t> {
+  using type = uint32_t;
+  static __device__ __forceinline__ type make(float x, int column) {
+    return (rank_or_lowest(x) & 0xffff0000u) | (0xffffu - column);
+  }
+  static __device__ __forceinline__ bool some(type k) { return k > kLowestRank; }
+  static __device__ __forceinline__ int column(type k) { return (int)(0xffffu - (k & 0xffffu)); }
+  // the low bits of a negative value's rank are ones
+  static __device__ __forceinline__ float value(type k) { return value_of(k & 0x80000000u ? k & 0xffff0000u : k | 0xffffu); }
+  static __device__ __forceinline__ type larger(type a, type b) { return max(a, b); }
+  static __device__ __forceinline__ type smaller(type a, type b) { return min(a, b); }
+  template <class F>
+  static __device__ __forceinline__ type moved(type k, F&& f) { return f(k); }
+};
+
+template <> struct RouteKey<float> {
+  using type = double;
+  static __device__ __forceinline__ uint64_t bits(type k) { return __builtin_bit_cast(uint64_t, k); }
+  static __device__ __forceinline__ type make(float x, int column) {   // 1.0 and up: no denormal, infinity or NaN
+    const uint32_t r = rank_or_lowest(x);
+    return __builtin_bit_cast(double, (uint64_t)(0x3ff00000u | r >> 22) << 32 | (r << 10 | (uint32_t)(1023 - column)));
+  }
+  static __device__ __forceinline__ uint32_t rank(type k) { return (uint32_t)(bits(k) >> 10); }
+  static __device__ __forceinline__ bool some(type k) { return rank(k) > kLowestRank; }
+  static __device__ __forceinline__ int column(type k) { return 1023 - (int)(bits(k) & 1023); }
+  static __device__ __forceinline__ float value(type k) { return value_of(rank(k)); }
+  static __device__ __forceinline__ type larger(type a, type b) { return __builtin_fmax(a, b); }
+  static __device__ __forceinline__ type smaller(type a, type b) { return __builtin_fmin(a, b); }
+  template <class F>
+  static __device__ __forceinline__ type moved(type k, F&& f) {
+    const uint64_t u = bits(k);
+    return __builtin_bit_cast(double, (uint64_t)f((uint32_t)(u >> 32)) << 32 | f((uint32_t)u));
+  }
+};
+
+// Value of a lane of the other half of 2 D lanes (D up to 8: of lane ^ D, or of
+// the mirrored one), for lists that are the same in all D lanes of a half.
+template <int D>
+__device__ __forceinline__ uint32_t other_half(uint32_t x) {
+  if constexpr (D == 1) return row_turn<0xb1>(x);
+  else if constexpr (D == 2) return row_turn<0x4e>(x);
+  else if constexpr (D == 4) return row_turn<0x141>(x);
+  else if constexpr (D == 8) return row_turn<0x140>(x);
+  else return (uint32_t)__shfl_xor((int)x, D);
+}
+
+constexpr int RT_LIST = 8;   // keys of a list
+
+template <class K>
+__device__ __forceinline__ void in_order(typename K::type& a, typename K::type& b) {
+  const auto x = a;
+  a = K::larger(x, b);
+  b = K::smaller(x, b);
+}
+
+// Falling order, by Batcher's network for eight (19 exchanges).
+template <class K>
+__device__ __forceinline__ void sort_list(typename K::type* k) {
+  constexpr int at[19][2] = {{0, 1}, {2, 3}, {4, 5}, {6, 7}, {0, 2}, {1, 3}, {4, 6}, {5, 7}, {1, 2}, {5, 6},
+                             {0, 4}, {1, 5}, {2, 6}, {3, 7}, {2, 4}, {3, 5}, {1, 2}, {3, 4}, {5, 6}};
+#pragma unroll
+  for (int i = 0; i < 19; ++i) in_order<K>(k[at[i][0]], k[at[i][1]]);
+}
+
+// The eight largest of two sorted lists: of a falling and a rising one the
+// larger at each place, which rise and fall once and are sorted in three steps.
+template <class K>
+__device__ __forceinline__ void merge_list(typename K::type* k, const typename K::type* o) {
+#pragma unroll
+  for (int i = 0; i < RT_LIST; ++i) k[i] = K::larger(k[i], o[RT_LIST - 1 - i]);
+#pragma unroll
+  for (int d = RT_LIST / 2; d; d >>= 1)
+#pragma unroll
+    for (int i = 0; i < RT_LIST; ++i)
+      if (!(i & d)) in_order<K>(k[i], k[i + d]);
+}
+
+template <class K, int D>
+__device__ __forceinline__ void merge_lanes(typename K::type* k) {
+  typename K::type o[RT_LIST];
+#pragma unroll
+  for (int i = 0; i < RT_LIST; ++i) o[i] = K::moved(k[i], [](uint32_t x) { return other_half<D>(x); });
+  merge_list<K>(k, o);
+}
+
+template <int L>
+__device__ __forceinline__ float sum_halves(float x) {
+  auto add = [&](uint32_t y) { x += __uint_as_float(y); };
+  add(other_half<1>(__float_as_uint(x)));
+  add(other_half<2>(__float_as_uint(x)));
+  if constexpr (L > 4) add(other_half<4>(__float_as_uint(x)));
+  if constexpr (L > 8) add(other_half<8>(__float_as_uint(x)));
+  if constexpr (L > 16) add(other_half<16>(__float_as_uint(x)));
+  return x;
+}
+
+// Up to RT_LIST choices, of L lanes (4 to 32) that hold V (8 to 32) logits
+// each: every lane sorts its keys by eights and keeps the largest, then the
+// lanes' lists are merged.  Lane l ends with the choices l, l + L, ...: PER of
+// them.  Bound by the exchanges, two instructions each: 128 logits are 20 a
+// token of 16 in a wave (four lanes; 17 in one lane, which leaves three of four
+// waves out; a pick a round, 112).
+template <int L> constexpr int route_per() { return L < RT_LIST ? RT_LIST / L : 1; }
+
+template <class T, int L, int V>
+__device__ __forceinline__ void choose(const RouteArgs& g, int64_t token, int lane, int* index, float* weight) {
+  using K = RouteKey<T>;
+  constexpr int CH = 16 / sizeof(T), PER = route_per<L>();
+  const T* const row = (const T*)g.logits + token * g.ldl;
+  float x[V];
+#pragma unroll
+  for (int v = 0; v < V; v += CH) {
+    widen<T>(row_piece<T>(row, (v / CH * L + lane) * CH, g.experts), x + v);
+  }
+  typename K::type best[RT_LIST];
+  uint32_t largest = 0;   // magnitude: above infinity's, a NaN
+#pragma unroll
+  for (int v = 0; v < V; v += RT_LIST) {
+    typename K::type k[RT_LIST];
+#pragma unroll
+    for (int i = 0; i < RT_LIST; ++i) {
+      const int u = v + i;
+      largest = max(largest, __float_as_uint(x[u]) & 0x7fffffffu);
+      k[i] = K::make(x[u], (u / CH * L + lane) * CH + u % CH);
+    }
+    sort_list<K>(k);
+    if (v) {
+      merge_list<K>(best, k);
+    } else {
+#pragma unroll
+      for (int i = 0; i < RT_LIST; ++i) best[i] = k[i];
+    }
+  }
+  merge_lanes<K, 1>(best);
+  merge_lanes<K, 2>(best);
+  if constexpr (L > 4) merge_lanes<K, 4>(best);
+  if constexpr (L > 8) merge_lanes<K, 8>(best);
+  if constexpr (L > 16) merge_lanes<K, 16>(best);
+  const float first = K::value(best[0]);
+  float e[PER], part = 0.0f;
+#pragma unroll
+  for (int p = 0; p < PER; ++p) {
+    auto mine = best[p * L];
+#pragma unroll
+    for (int i = 1; i < L && i < RT_LIST; ++i) mine = lane == i ? best[p * L + i] : mine;
+    const int j = p * L + lane;
+    const bool some = j < g.k && j < RT_LIST && K::some(mine);
+    index[p] = some ? K::column(mine) : -1;
+    e[p] = some ? exp_f(K::value(mine) - first) : 0.0f;
+    part += e[p];
+  }
+  if (!g.renorm) {
+    part = 0.0f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) part += exp_f(x[v] - first);
+  }
+  const float sum = sum_halves<L>(largest > 0x7f800000u ? NAN : part);
+#pragma unroll
+  for (int p = 0; p < PER; ++p) weight[p] = index[p] >= 0 ? e[p] / sum : 0.0f;
+}
+
+// More than RT_LIST choices: lane j of the L that share a token ends with the
+// j-th.  One pick a round: the largest of the lanes' largest.
+template <class T, int L>
+__device__ __forceinline__ void choose_many(const RouteArgs& g, int64_t token, int lane, int& index, float& weight) {
+  constexpr int Q = 4, V = 4 * Q;
   constexpr bool PACK = sizeof(T) == 2;
   float x[V];
   uint32_t r[V];
@@ -150,6 +380,33 @@ __device__ __forceinline__ void choose(const RouteArgs& g, int64_t token, int la
   weight = index >= 0 ? e / sum : 0.0f;
 }
 
+// The lanes of a token, and each one's choices: f(choice, index, weight).
+template <class T, int L, int V>
+struct ChooseFew {
+  static constexpr int lanes = L;
+  template <class F>
+  static __device__ __forceinline__ void run(const RouteArgs& g, int64_t token, int lane, F&& f) {
+    int index[route_per<L>()];
+    float weight[route_per<L>()];
+    choose<T, L, V>(g, token, lane, index, weight);
+#pragma unroll
+    for (int p = 0; p < route_per<L>(); ++p)
+      if (p * L + lane < g.k) f(p * L + lane, index[p], weight[p]);
+  }
+};
+
+template <class T, int L>
+struct ChooseMany {
+  static constexpr int lanes = L;
+  template <class F>
+  static __device__ __forceinline__ void run(const RouteArgs& g, int64_t token, int lane, F&& f) {
+    int index;
+    float weight;
+    choose_many<T, L>(g, token, lane, index, weight);
+    if (lane < g.k) f(lane, index, weight);
+  }
+};
+
 // ----------------------------------------------------------------------------
 // places of the entries: a stable sort by expert without a race
 // ----------------------------------------------------------------------------
@@ -190,8 +447,9 @@ __device__ __forceinline__ int mask_rank(const uint32_t* m, int bit) {
 }
 
 // Up to RT_CHUNK tokens: all of it in one block and one launch.
-template <class T, int L, int Q>
+template <class C>
 __global__ __launch_bounds__(1024) void k_route_small(RouteArgs g) {
+  constexpr int L = C::lanes;
   extern __shared__ uint32_t route_lds[];
   uint32_t* const mask = route_lds;                      // experts x RT_WORDS
   int* const base = (int*)(mask + g.experts * RT_WORDS);   // experts
@@ -200,16 +458,13 @@ __global__ __launch_bounds__(1024) void k_route_small(RouteArgs g) {
   __syncthreads();
   const int lane = threadIdx.x % L;
   for (int t = threadIdx.x / L; t < g.tokens; t += 1024 / L) {
-    int index;
-    float weight;
-    choose<T, L, Q>(g, t, lane, index, weight);
-    if (lane < g.k) {
-      const int i = t * g.k + lane;
+    C::run(g, t, lane, [&](int j, int index, float weight) {
+      const int i = t * g.k + j;
       g.index[i] = index;
       g.weights[i] = weight;
       picks[i] = index;
       if (index >= 0) atomicOr(&mask[index * RT_WORDS + t / 32], 1u << (t & 31));
-    }
+    });
   }
   __syncthreads();
   for (int e = threadIdx.x; e < g.experts; e += 1024) base[e] = mask_count(mask + e * RT_WORDS);
@@ -233,48 +488,51 @@ __global__ __launch_bounds__(1024) void k_route_small(RouteArgs g) {
 }
 
 // More tokens, first launch: the choices, and how many of a block's tokens
-// chose each expert.
-template <class T, int L, int Q>
-__global__ __launch_bounds__(256) void k_route_choose(RouteArgs g) {
+// chose each expert (rows of whole 16 bytes).
+__device__ __forceinline__ int count_row(const RouteArgs& g) { return (g.experts + 3) & ~3; }
+
+template <class C>
+__global__ __launch_bounds__(1024) void k_route_choose(RouteArgs g) {
+  constexpr int L = C::lanes;
   __shared__ int count[RT_EXPERTS];
-  for (int e = threadIdx.x; e < g.experts; e += 256) count[e] = 0;
+  const int row = count_row(g);
+  for (int e = threadIdx.x; e < row; e += 1024) count[e] = 0;
   __syncthreads();
   const int lane = threadIdx.x % L;
   const int64_t t0 = (int64_t)blockIdx.x * g.per, t1 = min(t0 + g.per, g.tokens);
-  for (int64_t t = t0 + threadIdx.x / L; t < t1; t += 256 / L) {
-    int index;
-    float weight;
-    choose<T, L, Q>(g, t, lane, index, weight);
-    if (lane < g.k) {
-      g.index[t * g.k + lane] = index;
-      g.weights[t * g.k + lane] = weight;
+  for (int64_t t = t0 + threadIdx.x / L; t < t1; t += 1024 / L)
+    C::run(g, t, lane, [&](int j, int index, float weight) {
+      g.index[t * g.k + j] = index;
+      g.weights[t * g.k + j] = weight;
       if (index >= 0) atomicAdd(&count[index], 1);
-    }
-  }
+    });
   __syncthreads();
-  for (int e = threadIdx.x; e < g.experts; e += 256) g.counts[(int64_t)blockIdx.x * g.experts + e] = count[e];
+  for (int e = threadIdx.x; e < row; e += 1024) g.counts[(int64_t)blockIdx.x * row + e] = count[e];
 }
 
-// Second launch: every block adds up the counts before its own.
-__global__ __launch_bounds__(256) void k_route_place(RouteArgs g) {
+// Second launch: every block adds up the counts before its own.  Bound by the
+// latency of its few steps, so all loads of a step are in flight together: four
+// experts a thread, the blocks' rows dealt to groups of threads.
+__global__ __launch_bounds__(1024) void k_route_place(RouteArgs g) {
   __shared__ uint32_t mask[RT_EXPERTS * RT_WORDS];
   __shared__ int total[RT_EXPERTS], prior[RT_EXPERTS];
-  const int blocks = gridDim.x, me = blockIdx.x;
-  for (int e = threadIdx.x; e < g.experts; e += 256) total[e] = prior[e] = 0;
+  const int blocks = gridDim.x, me = blockIdx.x, row = count_row(g);
+  for (int e = threadIdx.x; e < row; e += 1024) total[e] = prior[e] = 0;
   __syncthreads();
-  // whole runs of experts side by side, the blocks' rows dealt to the groups
-  const int lanes = min(256, (g.experts + 63) & ~63), groups = 256 / lanes, group = threadIdx.x / lanes;
+  const int quads = row / 4, groups = 1024 / quads, group = threadIdx.x / quads;
   if (group < groups) {
-    for (int e = threadIdx.x - group * lanes; e < g.experts; e += lanes) {
-      int all = 0, before = 0;
+    const int q = threadIdx.x - group * quads;
+    i32x4_t all = {}, before = {};
 #pragma unroll 8
-      for (int b = group; b < blocks; b += groups) {
-        const int n = g.counts[(int64_t)b * g.experts + e];
-        all += n;
-        before += b < me ? n : 0;
-      }
-      atomicAdd(&total[e], all);
-      atomicAdd(&prior[e], before);
+    for (int b = group; b < blocks; b += groups) {
+      const i32x4_t n = *(const i32x4_t*)(g.counts + (int64_t)b * row + 4 * q);
+      all += n;
+      if (b < me) before += n;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      atomicAdd(&total[4 * q + i], all[i]);
+      atomicAdd(&prior[4 * q + i], before[i]);
     }
   }
   __syncthreads();
@@ -283,7 +541,7 @@ __global__ __launch_bounds__(256) void k_route_place(RouteArgs g) {
     if (me == 0 && threadIdx.x == 0) g.offsets[g.experts] = all;
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < g.experts; e += 256) {
+  for (int e = threadIdx.x; e < g.experts; e += 1024) {
     if (me == 0) g.offsets[e] = total[e];
     prior[e] += total[e];
   }
@@ -291,14 +549,14 @@ __global__ __launch_bounds__(256) void k_route_place(RouteArgs g) {
   for (int64_t c = t0; c < t1; c += RT_CHUNK) {
     const int n = (int)min((int64_t)RT_CHUNK, t1 - c) * g.k;
     const int64_t i0 = c * g.k;
-    for (int i = threadIdx.x; i < g.experts * RT_WORDS; i += 256) mask[i] = 0;
+    for (int i = threadIdx.x; i < g.experts * RT_WORDS; i += 1024) mask[i] = 0;
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += 256) {
+    for (int i = threadIdx.x; i < n; i += 1024) {
       const int e = g.index[i0 + i], t = i / g.k;
       if (e >= 0) atomicOr(&mask[e * RT_WORDS + t / 32], 1u << (t & 31));
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += 256) {
+    for (int i = threadIdx.x; i < n; i += 1024) {
       const int e = g.index[i0 + i];
       int slot = -1;
       if (e >= 0) {
@@ -308,7 +566,7 @@ __global__ __launch_bounds__(256) void k_route_place(RouteArgs g) {
       g.slots[i0 + i] = slot;
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < g.experts; e += 256) prior[e] += mask_count(mask + e * RT_WORDS);
+    for (int e = threadIdx.x; e < g.experts; e += 1024) prior[e] += mask_count(mask + e * RT_WORDS);
     __syncthreads();
   }
 }
@@ -328,6 +586,12 @@ struct RouteGradArgs {
   int64_t ldl, ldd, tokens;
   int32_t experts, k, renorm;
 };
+
+// The compiler keeps memory accesses on their side of this.
+__device__ __forceinline__ void wave_step() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
 
 template <class T, int L, int Q>
 __global__ __launch_bounds__(256) void k_route_bwd(RouteGradArgs g) {
@@ -370,13 +634,20 @@ __global__ __launch_bounds__(256) void k_route_bwd(RouteGradArgs g) {
 #pragma unroll
     for (int v = 0; v < V; ++v) x[v] = 0.0f;
   }
-  const int first = (threadIdx.x & 63) / L * L;
-  for (int j = 0; j < g.k; ++j) {
-    const int at = __shfl(index, first + j);
-    const float dj = __shfl(d, first + j);
+  // the chosen ones through LDS, a row of the token's own; its lanes are of one
+  // wave, whose LDS instructions stay in order
+  __shared__ __attribute__((aligned(16))) float chosen[256 / L][4 * L * Q];
+  float* const mine = chosen[threadIdx.x / L];
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-      if (at == ((v >> 2) * L + lane) * 4 + (v & 3)) x[v] += dj;
+  for (int q = 0; q < Q; ++q) *(f32x4_t*)(mine + (q * L + lane) * 4) = f32x4_t{};
+  wave_step();
+  if (index >= 0 && index < g.experts) atomicAdd(&mine[index], d);
+  wave_step();
+#pragma unroll
+  for (int q = 0; q < Q; ++q) {
+    const f32x4_t c = *(const f32x4_t*)(mine + (q * L + lane) * 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[4 * q + i] += c[i];
   }
   if (!in) return;
 #pragma unroll
@@ -416,45 +687,6 @@ __device__ __forceinline__ int64_t row_of_unit(int64_t unit, int64_t total, int 
   const int64_t row = total >> 32 ? unit / parts : (int64_t)((uint32_t)unit / (uint32_t)parts);
   part = (int)(unit - row * parts);
   return row;
-}
-
-template <class T>
-__device__ __forceinline__ void st_piece(T* p, f32x4_t v, int left) {
-  constexpr int CH = 16 / sizeof(T);
-  if (left >= CH) {
-    if constexpr (sizeof(T) == 4) *(f4u_t*)p = f4u_t{v[0], v[1], v[2], v[3]};
-    else *(u4h_t*)p = __builtin_bit_cast(u4h_t, v);
-    return;
-  }
-  T e[CH];
-  __builtin_memcpy(e, &v, 16);
-#pragma unroll
-  for (int i = 0; i < CH; ++i)
-    if (i < left) p[i] = e[i];
-}
-
-// The elements of a piece as fp32, and back.
-template <class T>
-__device__ __forceinline__ void widen(f32x4_t v, float* e) {
-  if constexpr (sizeof(T) == 4) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) e[i] = v[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      e[2 * i] = bf16_lo(__float_as_uint(v[i]));
-      e[2 * i + 1] = bf16_hi(__float_as_uint(v[i]));
-    }
-  }
-}
-
-template <class T>
-__device__ __forceinline__ f32x4_t narrow(const float* e) {
-  if constexpr (sizeof(T) == 4) return f32x4_t{e[0], e[1], e[2], e[3]};
-  f32x4_t v;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(bf16_pack2(e[2 * i], e[2 * i + 1]));
-  return v;
 }
 
 __device__ __forceinline__ void raise_rows(uint32_t* flags) {

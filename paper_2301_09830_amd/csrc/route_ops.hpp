@@ -36,11 +36,11 @@ int64_t route_per(const occ_route_t& r) { return up(div_up(r.tokens, 256), RT_CH
 size_t route_bytes(const occ_route_t& r) {
   if (!r.tokens || route_small(r)) return 0;
   Carve c;
-  c.take((size_t)div_up(r.tokens, route_per(r)) * r.experts * 4);
+  c.take((size_t)div_up(r.tokens, route_per(r)) * up(r.experts, 4) * 4);
   return c.total();
 }
 
-// f(L, quads) for the lanes that share a token and what each holds of it
+// f(lanes that share a token, quads that each holds of it)
 template <class F>
 occ_status_t by_experts(const occ_route_t& r, F&& f) {
   using std::integral_constant;
@@ -48,6 +48,20 @@ occ_status_t by_experts(const occ_route_t& r, F&& f) {
   if (r.experts > 128) return f(integral_constant<int, 16>{}, integral_constant<int, 4>{});
   if (r.experts > 64) return f(integral_constant<int, 16>{}, integral_constant<int, 2>{});
   return f(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+}
+
+// f(the way of choosing)
+template <class T, class F>
+occ_status_t by_choices(const occ_route_t& r, F&& f) {
+  if (r.k > 16 || (r.k > RT_LIST && r.experts > 256)) return f(ChooseMany<T, 64>{});
+  if (r.k > RT_LIST) return f(ChooseMany<T, 16>{});
+  constexpr int V = sizeof(T) == 2 ? 32 : 16;   // fp32 keys take two registers
+  if (r.experts <= 32) return f(ChooseFew<T, 4, 8>{});
+  if (r.experts <= 64) return f(ChooseFew<T, 4, 16>{});
+  if (r.experts <= 128) return f(ChooseFew<T, 128 / V, V>{});
+  if (r.experts <= 256) return f(ChooseFew<T, 256 / V, V>{});
+  if (r.experts <= 512) return f(ChooseFew<T, 512 / V, V>{});
+  return f(ChooseFew<T, 32, 32>{});
 }
 
 template <class T>
@@ -67,18 +81,18 @@ occ_status_t run_route(const occ_route_t& r, char* ws, hipStream_t s) {
   a.slots = r.slots;
   a.counts = (int32_t*)(ws + kWsHeader);
   if (route_small(r))
-    return by_experts(r, [&](auto lanes, auto quads) {
+    return by_choices<T>(r, [&](auto c) {
       return launch("route", s, [&] {
-        hipLaunchKernelGGL((k_route_small<T, lanes, quads>), dim3(1), dim3(1024), route_small_lds(r), s, a);
+        hipLaunchKernelGGL((k_route_small<decltype(c)>), dim3(1), dim3(1024), route_small_lds(r), s, a);
       });
     });
   const dim3 grid((unsigned)div_up(r.tokens, a.per));
-  OCC_TRY(by_experts(r, [&](auto lanes, auto quads) {
+  OCC_TRY(by_choices<T>(r, [&](auto c) {
     return launch("route_choose", s, [&] {
-      hipLaunchKernelGGL((k_route_choose<T, lanes, quads>), grid, dim3(256), 0, s, a);
+      hipLaunchKernelGGL((k_route_choose<decltype(c)>), grid, dim3(1024), 0, s, a);
     });
   }));
-  return launch("route_place", s, [&] { hipLaunchKernelGGL(k_route_place, grid, dim3(256), 0, s, a); });
+  return launch("route_place", s, [&] { hipLaunchKernelGGL(k_route_place, grid, dim3(1024), 0, s, a); });
 }
 
 template <class T>
