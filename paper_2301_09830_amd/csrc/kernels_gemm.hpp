@@ -736,6 +736,7 @@ struct Form {
 using Form256 = Form<2, 4, 8, 4, 2>;
 using Form128 = Form<2, 4, 4, 2, 4>;
 using Form64 = Form<4, 2, 1, 2, 4>;
+using Form128x256 = Form<2, 4, 4, 4, 2>;   // half of the first, for the last rows
 using FormDirect = Form<4, 2, 1, 2, 2, true>;
 
 // Tile (tm, tn) of a product: all of its K, or part `split` of it.  T: type
