@@ -45,8 +45,9 @@ struct DistillToken {
 // Sum (or maximum) over a block of NW waves, in every thread.
 template <int NW, class F>
 __device__ __forceinline__ float block_reduce(float x, float* lds, F&& f) {
-#pragma unroll
-  for (int s = 32; s; s >>= 1) x = f(x, __shfl_xor(x, s));
+  x = __uint_as_float(over_lanes<64>(__float_as_uint(x), [&](uint32_t a, uint32_t b) {
+    return __float_as_uint(f(__uint_as_float(a), __uint_as_float(b)));
+  }));
   if constexpr (NW == 1) return x;
   __syncthreads();   // the last use of lds has ended
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
@@ -98,12 +99,9 @@ __device__ __forceinline__ DistillRow distill_entries(const DistillArgs& g, int6
       const int i = g.index[token * g.ldi + j];
       const bool in = i >= 0 && i < g.vocab;
       bad |= i >= g.vocab;
-      float t = -INFINITY;
-      if (in) {   // what stands at a masked entry is not looked at
-        t = g.teacher_bf16 ? ld_elem<uint16_t>((const uint16_t*)g.teacher + token * g.ldt + j)
-                           : ((const float*)g.teacher)[token * g.ldt + j];
-        t *= inv;
-      }
+      float t = g.teacher_bf16 ? ld_elem<uint16_t>((const uint16_t*)g.teacher + token * g.ldt + j)
+                               : ((const float*)g.teacher)[token * g.ldt + j];
+      t = in ? t * inv : -INFINITY;   // what stands at a masked entry is not looked at
       const bool live = in && t != -INFINITY;
       e.index[j] = live ? i : -1;
       e.p[j] = t;
