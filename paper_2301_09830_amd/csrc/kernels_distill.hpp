@@ -34,12 +34,13 @@ struct DistillArgs {
   int32_t stream;         // dS bypasses the caches
 };
 
-// One token's entries, in LDS.  Those out of the vocabulary are masked, and
-// those that name a column for the second time are added to its first entry.
+// One token's entries, in LDS; the label's is behind the teacher's.  Entries of
+// one column are taken together in the gradient: the first of them (column)
+// has what all of them take off it (off).
 template <int N>
 struct DistillToken {
-  int32_t index[N + 1];   // the label's entry is behind the teacher's
-  float p[N + 1], s[N + 1];
+  int32_t index[N + 1], column[N + 1];   // -1: masked
+  float p[N + 1], s[N + 1], off[N + 1];
 };
 
 // Sum (or maximum) over a block of NW waves, in every thread.
@@ -93,41 +94,68 @@ __device__ __forceinline__ DistillRow distill_entries(const DistillArgs& g, int6
   if (r.scale == 0.0f) return r;
   const T* const row = (const T*)g.S + token * g.lds;
   const float inv = 1.0f / g.temperature;
-  float top = -INFINITY;
-  if (g.alpha != 0.0f)
-    for (int j = threadIdx.x; j < g.k; j += NT) {
-      const int i = g.index[token * g.ldi + j];
-      const bool in = i >= 0 && i < g.vocab;
-      bad |= i >= g.vocab;
-      float t = g.teacher_bf16 ? ld_elem<uint16_t>((const uint16_t*)g.teacher + token * g.ldt + j)
-                               : ((const float*)g.teacher)[token * g.ldt + j];
-      t = in ? t * inv : -INFINITY;   // what stands at a masked entry is not looked at
-      const bool live = in && t != -INFINITY;
-      e.index[j] = live ? i : -1;
-      e.p[j] = t;
-      e.s[j] = live ? ld_elem<T>(row + i) : 0.0f;
-      top = max_nan(top, t);
-    }
+  const int k = g.alpha != 0.0f ? g.k : 0;
+  for (int j = threadIdx.x; j < k; j += NT) {
+    const int i = g.index[token * g.ldi + j];
+    const bool in = i >= 0 && i < g.vocab;
+    bad |= i >= g.vocab;
+    float t = g.teacher_bf16 ? ld_elem<uint16_t>((const uint16_t*)g.teacher + token * g.ldt + j)
+                             : ((const float*)g.teacher)[token * g.ldt + j];
+    t = in ? t * inv : -INFINITY;   // what stands at a masked entry is not looked at
+    const bool live = in && t != -INFINITY;
+    e.index[j] = live ? i : -1;
+    e.p[j] = t;
+    e.s[j] = live ? ld_elem<T>(row + i) : 0.0f;
+  }
   if (threadIdx.x == 0) {
     e.index[g.k] = r.hard ? label : -1;
     e.s[g.k] = r.hard ? ld_elem<T>(row + label) : 0.0f;
   }
   if (__ballot(bad) && (threadIdx.x & 63) == 0 && g.flags) atomicOr(g.flags, kBadRows);
-  top = block_max<NW>(top, lds);
-  r.soft = g.k && g.alpha != 0.0f && top != -INFINITY;
-  if (r.soft) {
-    float sum = 0.0f, plog = 0.0f;
-    for (int j = threadIdx.x; j < g.k; j += NT) sum += exp_f(e.p[j] - top);
-    sum = block_sum<NW>(sum, lds);
-    const float log_sum = logf(sum), part = 1.0f / sum;
-    for (int j = threadIdx.x; j < g.k; j += NT) {
-      const float d = e.p[j] - top, p = exp_f(d) * part;
-      plog += p > 0.0f || p != p ? p * (d - log_sum) : 0.0f;
-      e.p[j] = p;
+  __syncthreads();
+  // the teacher's softmax by one wave, while the row is on its way to the others
+  if (threadIdx.x < 64) {
+    float top = -INFINITY, sum = 0.0f, plog = 0.0f;
+    for (int j = threadIdx.x; j < k; j += 64) top = max_nan(top, e.p[j]);
+    top = block_max<1>(top, lds);
+    if (top != -INFINITY) {
+      for (int j = threadIdx.x; j < k; j += 64) sum += exp_f(e.p[j] - top);
+      sum = block_sum<1>(sum, lds);
+      const float log_sum = logf(sum), part = 1.0f / sum;
+      for (int j = threadIdx.x; j < k; j += 64) {
+        const float d = e.p[j] - top, p = exp_f(d) * part;
+        plog += p > 0.0f || p != p ? p * (d - log_sum) : 0.0f;
+        e.p[j] = p;
+      }
+      plog = block_sum<1>(plog, lds);
     }
-    r.entropy = block_sum<NW>(plog, lds);
+    if (threadIdx.x == 0) {
+      lds[0] = top;
+      lds[1] = plog;
+    }
   }
   __syncthreads();
+  r.soft = lds[0] != -INFINITY;
+  r.entropy = lds[1];
+  if (g.dS) {
+    const float soft = r.scale * g.alpha * g.temperature, hard = r.scale * (1.0f - g.alpha);
+    for (int j = threadIdx.x; j <= g.k; j += NT) {
+      const int at = j == g.k || r.soft ? e.index[j] : -1;
+      float off = 0.0f;
+      bool first = at >= 0;
+      if (first && r.soft)
+        for (int i = 0; i < k; ++i) {
+          if (e.index[i] != at) continue;
+          first = first && i >= j;
+          off += e.p[i];
+        }
+      off *= soft;
+      if (r.hard && e.index[g.k] == at) off += hard;
+      e.column[j] = first ? at : -1;
+      e.off[j] = off;
+    }
+    __syncthreads();
+  }
   return r;
 }
 
@@ -137,14 +165,15 @@ template <int NW>
 __device__ __forceinline__ void distill_loss(const DistillArgs& g, int64_t token, const DistillRow& r,
                                              const DistillToken<DL_ENTRIES>& e, float m, float z, float z1,
                                              float* lds) {
+  if (threadIdx.x >= 64) return;   // one wave
   const float inv = 1.0f / g.temperature, log_z = logf(z), log_1 = logf(z1);
   float cross = 0.0f;   // -sum p log q
   if (r.soft) {
-    for (int j = threadIdx.x; j < g.k; j += NW * 64) {
+    for (int j = threadIdx.x; j < g.k; j += 64) {
       const float p = e.p[j];
       if (p > 0.0f || p != p) cross += p * (log_z - (e.s[j] - m) * inv);
     }
-    cross = block_sum<NW>(cross, lds);
+    cross = block_sum<1>(cross, lds);
   }
   if (threadIdx.x) return;
   float loss = 0.0f;
@@ -213,35 +242,22 @@ __device__ __forceinline__ void st_row_piece(T* p, f32x4_t v, int left) {
   st_piece<T>(p, v, left);
 }
 
-// The columns of the entries, once the rest of the row is stored: the first
-// entry of a column takes off what all of the same column hold.
+// The columns of the entries, over what the rest of the row stored there: each
+// by the wave that stored it, whose stores to one place stay in order.
 template <class T, int NW>
 __device__ __forceinline__ void store_entries(const DistillArgs& g, int64_t token, const DistillRow& r,
                                               const DistillToken<DL_ENTRIES>& e, const DistillExp& x,
                                               const DistillGrad& d) {
-  // another thread has stored to the same place: its store has to be done
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
-  const float soft = r.scale * g.alpha * g.temperature, hard = r.scale * (1.0f - g.alpha);
-  const int n = g.k + 1;
-  for (int j = threadIdx.x; j < n; j += NW * 64) {
-    const int at = e.index[j];
-    if (at < 0 || (j < g.k && !r.soft)) continue;
-    float off = 0.0f;
-    bool first = true;
-    if (r.soft)
-      for (int i = 0; i < g.k; ++i) {
-        if (e.index[i] != at) continue;
-        first = first && i >= j;
-        off += e.p[i];
-      }
-    if (!first) continue;
-    off *= soft;
-    if (r.hard && e.index[g.k] == at) off += hard;
+  constexpr int CH = 16 / sizeof(T);
+  wave_step();
+  const int wave = wave_id();
+  for (int j = threadIdx.x & 63; j <= g.k; j += 64) {
+    const int at = e.column[j];
+    if (at < 0 || (int)((uint32_t)at / (64 * CH) % NW) != wave) continue;
     const float s = e.s[j];
     float v = d.fa * x.a(s);
     if (x.two) v = __builtin_fmaf(d.fb, x.b(s), v);
-    st_elem((T*)g.dS + token * g.ldd + at, v - off);
+    st_elem((T*)g.dS + token * g.ldd + at, v - e.off[j]);
   }
 }
 
@@ -307,7 +323,8 @@ __global__ __launch_bounds__(NW * 64, 4) void k_distill(DistillArgs g) {
   const T* const row = (const T*)g.S + token * g.lds;
   const int c0 = threadIdx.x * CH, whole = g.vocab / STEP, c1 = c0 + whole * STEP;
   f32x4_t v[VPT < 9 ? 9 : VPT], last;
-  if (!g.scale || g.scale[token] != 0.0f) {   // on its way while the entries are read
+  // on its way while the entries are read; of few tokens without a look at the scale
+  if (NW == 16 || !g.scale || g.scale[token] != 0.0f) {
 #pragma unroll
     for (int p = 0; p < VPT; ++p)
       if (p < whole) v[p] = ld_piece<T>(row + c0 + p * STEP, CH);
