@@ -106,6 +106,9 @@ template <class T, int NW>
 occ_status_t distill_steps(const occ_distill_t& d, const DistillArgs& a, int64_t whole, hipStream_t s) {
   if (whole <= 2) return start_distill<T, NW, 2>(d, a, s);
   if (whole <= 4) return start_distill<T, NW, 4>(d, a, s);
+  if constexpr (NW == 16) {
+    if (whole <= 6) return start_distill<T, NW, 6>(d, a, s);
+  }
   if (whole <= 8) return start_distill<T, NW, 8>(d, a, s);
   return start_distill<T, NW, 16>(d, a, s);
 }

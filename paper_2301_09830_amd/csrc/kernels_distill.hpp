@@ -143,12 +143,15 @@ __device__ __forceinline__ DistillRow distill_entries(const DistillArgs& g, int6
       const int at = j == g.k || r.soft ? e.index[j] : -1;
       float off = 0.0f;
       bool first = at >= 0;
-      if (first && r.soft)
-        for (int i = 0; i < k; ++i) {
-          if (e.index[i] != at) continue;
-          first = first && i >= j;
-          off += e.p[i];
+      if (first && r.soft) {
+#pragma unroll 8
+        for (int i = 0; i < k; ++i) {   // without branches: the reads are in flight together
+          const bool same = e.index[i] == at;
+          const float p = e.p[i];
+          first &= !same | (i >= j);
+          off += same ? p : 0.0f;
         }
+      }
       off *= soft;
       if (r.hard && e.index[g.k] == at) off += hard;
       e.column[j] = first ? at : -1;
@@ -301,8 +304,9 @@ __device__ __forceinline__ float piece_max(f32x4_t v, float m) {
   return m;
 }
 
+// keep, if not null, receives the exponentials (unless there are two of each).
 template <class T>
-__device__ __forceinline__ void piece_sums(f32x4_t v, const DistillExp& x, float& z, float& z1) {
+__device__ __forceinline__ void piece_sums(f32x4_t v, const DistillExp& x, float& z, float& z1, float* keep = nullptr) {
   constexpr int CH = 16 / sizeof(T);
   float f[CH];
   widen<T>(v, f);
@@ -311,7 +315,11 @@ __device__ __forceinline__ void piece_sums(f32x4_t v, const DistillExp& x, float
     for (int i = 0; i < CH; ++i) z1 += x.b(f[i]);
   }
 #pragma unroll
-  for (int i = 0; i < CH; ++i) z += x.a(f[i]);
+  for (int i = 0; i < CH; ++i) {
+    const float a = x.a(f[i]);
+    if (keep) keep[i] = a;
+    z += a;
+  }
 }
 
 template <class T, int NW, int VPT, bool NT>
@@ -338,17 +346,33 @@ __global__ __launch_bounds__(NW * 64, 4) void k_distill(DistillArgs g) {
     if (p < whole) m = piece_max<T>(fresh(v[p]), m);
   m = block_reduce<NW>(m, lds, [](float a, float b) { return fmaxf(a, b); });
   const DistillExp x(g, r, m);
-  float z = 0.0f, z1 = 0.0f;
+  // sixteen waves take few tokens, a CU each, and are bound by instructions: the
+  // exponentials stay in registers
+  constexpr bool KEEP = NW == 16 && VPT * CH <= 48;   // of 128 registers
+  float z = 0.0f, z1 = 0.0f, kept[KEEP ? (VPT + 1) * CH : 1];
 #pragma unroll
   for (int p = 0; p < VPT; ++p)
-    if (p < whole) piece_sums<T>(fresh(v[p]), x, z, z1);
-  piece_sums<T>(fresh(last), x, z, z1);
+    if (p < whole) piece_sums<T>(fresh(v[p]), x, z, z1, KEEP ? kept + p * CH : nullptr);
+  piece_sums<T>(fresh(last), x, z, z1, KEEP ? kept + VPT * CH : nullptr);
   z = block_sum<NW>(z, lds);
   z1 = x.two ? block_sum<NW>(z1, lds) : z;
   distill_loss<NW>(g, token, r, e, m, z, z1, lds);
   if (!g.dS) return;
   const DistillGrad d(g, r, x.two, z, z1);
   T* const out = (T*)g.dS + token * g.ldd;
+  if (KEEP && !x.two) {
+    auto scaled = [&](const float* a) {
+      float f[CH];
+#pragma unroll
+      for (int i = 0; i < CH; ++i) f[i] = d.fa * a[i];
+      return narrow<T>(f);
+    };
+#pragma unroll
+    for (int p = 0; p < VPT; ++p)
+      if (p < whole) st_row_piece<T, NT>(out + c0 + p * STEP, scaled(kept + p * CH), CH);
+    if (c1 < g.vocab) st_row_piece<T, NT>(out + c1, scaled(kept + VPT * CH), g.vocab - c1);
+    return store_entries<T, NW>(g, token, r, e, x, d);
+  }
 #pragma unroll
   for (int p = 0; p < VPT; ++p)
     if (p < whole) st_row_piece<T, NT>(out + c0 + p * STEP, grad_piece<T>(fresh(v[p]), x, d), CH);
