@@ -64,7 +64,7 @@ occ_status_t run_experts_fwd(const occ_experts_t& p, const ExpertsFwdPlan& f, ch
     a.of = of;
     a.w_step = p.stride_w * (int64_t)sizeof(T);
     a.wide = (int32_t)wide;
-    a.across = (int32_t)(f.few == 1 ? div_up(GATED ? l.out : div_up(l.out, 2), DOT_WAVES) : div_up(l.out, 16));
+    a.across = (int32_t)few_across(f.few, l.out, GATED);
     return launch(GATED ? "experts_gated_few" : "experts_linear_few", s, [&] {
       const dim3 waves(DOT_WAVES * 64), block(SK_WAVES * 64);
       if (f.few == 1) hipLaunchKernelGGL((k_experts_dot<T, GATED>), grid, waves, 0, s, a);

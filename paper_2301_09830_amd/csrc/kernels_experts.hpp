@@ -318,6 +318,19 @@ __device__ __forceinline__ void shift_dz(DzSource& d, int64_t row, int es) {
   if (d.Z) d.Z = (const char*)d.Z + row * d.ldz * es;
 }
 
+// A tile of zeros, for an expert without rows.
+template <class TE, class F>
+__device__ __forceinline__ void zero_tile(const GemmArgs& g, int tm, int tn) {
+  constexpr int QPR = F::BN / 4;
+  for (int i = threadIdx.x; i < F::BM * QPR; i += F::NW * 64) {
+    const int m = tm * F::BM + i / QPR, n = tn * F::BN + i % QPR * 4, left = g.N - n;
+    if (m >= g.M || left <= 0) continue;
+    const int64_t at = (int64_t)m * g.ldc + n;
+    if (sizeof(TE) == 4 || g.c_f32) st_quad((float*)g.C + at, f32x4_t{}, left);
+    else st_quad((uint16_t*)g.C + at, f32x4_t{}, left);
+  }
+}
+
 // dW of an expert is a product over its rows.  Experts' lengths differ, so the
 // tiles of every expert are dealt to all XCDs, a contiguous run to each.
 template <class T, class TE, class F>
@@ -351,6 +364,7 @@ __device__ __forceinline__ void experts_dw(const ExpertsBackwardArgs& a, int b, 
   g.k_per_split = g.tiles_k;
   int tm, tn;
   band_tile(in, g.tiles_m, g.tiles_n, tm, tn);
+  if (!x.count) return zero_tile<TE, F>(g, tm, tn);
   ragged_tile<T, TE, F, true, true, EP_STORE>(g, tm, tn, lds);
 }
 

@@ -14,10 +14,11 @@ constexpr int64_t kMaxExperts = OCC_MAX_EXPERTS;
 // `run` rows or fewer each.
 inline int64_t most_runs(int64_t rows, int64_t experts, int64_t run) { return rows / run + std::min(rows, experts); }
 
-// The same at the mean length.
+// The same as expected: experts differ, so that some have a run more than the
+// mean's.
 inline double mean_runs(int64_t rows, int64_t experts, int64_t run) {
   const double n = (double)std::min(rows, experts), mean = (double)rows / n;
-  return n * std::max(1.0, mean / (double)run + 0.5);
+  return n * std::max(1.0, mean / (double)run + (experts > 1 ? 0.6 : 0.5));
 }
 
 // A matrix of every expert: rows x cols, ld apart, and `stride` to the next.
@@ -26,10 +27,11 @@ inline bool experts_ok(int64_t experts, int64_t rows, int64_t cols, int64_t ld, 
   return experts == 1 || (stride >= (rows - 1) * ld + cols && stride < ((int64_t)1 << 44) / experts);
 }
 
-// us of `blocks` blocks on `slots` places: whole rounds while there are few.
-inline double rounds_us(double blocks, int64_t slots, double block_us) {
+// us of `blocks` blocks on `slots` places: whole rounds while there are few and
+// their number is known, which it is not where lengths are near a run's.
+inline double rounds_us(double blocks, int64_t slots, double block_us, bool known) {
   const double r = blocks / (double)slots;
-  return (r < 4.0 ? std::ceil(r) : r) * block_us;
+  return (r <= 0.7 ? 1.0 : known ? r < 4.0 ? std::ceil(r) : r : r + 0.5) * block_us;
 }
 
 struct ExpertsTile {
@@ -43,6 +45,34 @@ inline double tile_us(const TileTimes& t, size_t es, double k_tiles) {
 }
 
 inline int64_t tile_slots(const TileTimes& t, size_t es) { return (int64_t)kCUs * (es == 4 ? 1 : t.resident); }
+
+// Forms that stream the weights, for few rows of an expert: rows of a run, and
+// ns of the whole chip that a block takes, fixed and for each 2 KiB of K
+// (linear, gated).  Measured at 64 rows of each of 8 and 64 experts, in 512 to
+// 4096; bf16 rows off 16 bytes take 1.5 times as long along K, twice through
+// the matrix instructions.  With two rows an expert or fewer they are ahead of
+// the tiles (8 experts, 4096 x 4096, gated, 16 rows 78 against 89 us; 3 experts, 1408 x
+// 3008, 6 rows 7.4 and 9.3), from some eight on behind (8 experts, 1408 x 3008, 64
+// rows 20.1 and 13.5, 512 rows 57 and 18.5; fp32 64 rows 41 and 55, 512 rows 118 and 85).
+struct FewTimes {
+  int form, run;
+  double fixed[2], k[2];
+};
+constexpr FewTimes kFewForms[4] = {{1, 4, {2.35, 2.35}, {1.35, 1.35}},
+                                   {16, 16, {5.1, 8.0}, {6.45, 9.6}},
+                                   {32, 32, {3.0, 5.0}, {8.5, 13.0}},
+                                   {64, 64, {9.0, 9.5}, {14.5, 18.6}}};
+
+inline int64_t few_across(int form, int64_t out, bool gated) {
+  return form == 1 ? div_up(gated ? out : div_up(out, 2), 4) : div_up(out, 16);
+}
+
+inline double few_experts_us(const occ_experts_t& p, bool gated, const FewTimes& t, size_t es) {
+  const double blocks = mean_runs(p.l.tokens, p.experts, t.run) * (double)few_across(t.form, p.l.out, gated);
+  const bool off = es == 2 && needs_copy(p.l.W, p.l.ldw, p.l.in, es);
+  const double k = (double)p.l.in * (double)es / 2048.0;
+  return 3.0 + blocks * (t.fixed[gated] + t.k[gated] * k) * 1e-3 * (off ? t.form == 1 ? 1.5 : 2.0 : 1.0);
+}
 
 struct ExpertsFwdPlan {
   int few = 0;           // 1: along K; 16, 32, 64: rows through the matrix instructions
@@ -68,7 +98,13 @@ inline bool experts_copy(const void* p, int64_t ld, int64_t cols, int64_t stride
 inline double fwd_tile_us(const occ_experts_t& p, bool gated, const TileTimes& t, size_t es, bool planes) {
   const int64_t tiles_n = gated ? div_up(p.l.out, t.side / 2) : div_up(p.l.out, t.side);
   const double k = (double)div_up(p.l.in, kRowBytes / (int64_t)es) * (planes ? kPairs : 1);
-  return rounds_us(mean_runs(p.l.tokens, p.experts, t.side) * (double)tiles_n, tile_slots(t, es), tile_us(t, es, k));
+  const double blocks = mean_runs(p.l.tokens, p.experts, t.side) * (double)tiles_n;
+  const double mean = (double)p.l.tokens / (double)std::min(p.l.tokens, p.experts) / t.side;
+  const bool known = p.experts == 1 || mean < 0.33 || mean > 2.0;
+  double block = tile_us(t, es, k);
+  // one resident block alone does not share its CU (0.27 us a K tile of 64 x 64)
+  if (es == 2 && t.resident > 1 && blocks <= (double)kCUs) block = k * 0.65 * t.k_bf16 + t.fixed;
+  return rounds_us(blocks, tile_slots(t, es), block, known);
 }
 
 inline ExpertsTile best_fwd(const occ_experts_t& p, bool gated, size_t es, bool planes) {
@@ -86,12 +122,6 @@ inline occ_status_t plan_experts_fwd(const occ_experts_t& p, bool gated, Experts
   const size_t es = elem_size(l.dtype);
   const int64_t wide = gated ? 2 * l.out : l.out, used = std::min(l.tokens, p.experts);
   const double mean = (double)l.tokens / (double)used;
-  if (mean <= (double)kFewTokens) {
-    f.few = mean <= 2.0 ? 1 : mean <= 12.0 ? 16 : mean <= 24.0 ? 32 : 64;
-    const int64_t across = f.few == 1 ? div_up(gated ? l.out : div_up(l.out, 2), 4) : div_up(l.out, 16);
-    f.blocks = most_runs(l.tokens, p.experts, f.few == 1 ? 4 : f.few) * across;
-    return f.blocks <= kMaxBlocks ? OCC_OK : OCC_E_SHAPE;
-  }
   f.copy_x = needs_copy(l.X, l.ldx, l.in, es);
   f.copy_w = experts_copy(l.W, l.ldw, l.in, p.stride_w, p.experts, es);
   ExpertsTile best = best_fwd(p, gated, es, false);
@@ -115,6 +145,22 @@ inline occ_status_t plan_experts_fwd(const occ_experts_t& p, bool gated, Experts
       f.direct = false;
       f.planes = f.copy_x = f.copy_w = true;
     }
+  }
+  // the weights of the experts that have rows are read in any form
+  const double weights = (double)used * (double)wide * (double)l.in * (double)es / 5.5e6;
+  us = std::max(us + 2.0, weights);
+  if (mean <= (double)kFewTokens)
+    for (const FewTimes& t : kFewForms) {
+      const double few = std::max(few_experts_us(p, gated, t, es), weights);
+      if (few > us || (f.few && few == us)) continue;
+      us = few;
+      f.few = t.form;
+    }
+  if (f.few) {
+    f.copy_x = f.copy_w = f.planes = f.direct = false;
+    const int run = f.few == 1 ? 4 : f.few;
+    f.blocks = most_runs(l.tokens, p.experts, run) * few_across(f.few, l.out, gated);
+    return f.blocks <= kMaxBlocks ? OCC_OK : OCC_E_SHAPE;
   }
   f.tile = best.tile;
   const int side = f.direct ? 64 : kTiles[f.tile].side;
@@ -163,8 +209,10 @@ inline double bwd_tile_us(const occ_experts_grad_t& p, int64_t wide, const TileT
   const double xus = tile_us(t, es, (double)div_up(wide, bk) * pairs);
   const double w = l.dW ? (double)p.experts * (double)div_up(wide, t.side) * (double)tiles_n : 0.0;
   const double wus = tile_us(t, es, ((double)l.tokens / (double)(p.experts * bk) + 0.5) * pairs);
+  // the longest expert has twice the mean's rows, and its tiles of dW may end last
+  const double longest = p.experts > 1 ? 2.0 * wus - t.fixed : wus;
   const double slots = (double)tile_slots(t, es), sum = (x * xus + w * wus) / slots;
-  return std::max({sum, x > 0.0 ? xus : 0.0, w > 0.0 ? wus : 0.0});
+  return std::max({sum, x > 0.0 ? xus : 0.0, w > 0.0 ? longest : 0.0});
 }
 
 inline ExpertsTile best_bwd(const occ_experts_grad_t& p, int64_t wide, size_t es, bool planes, int first) {
