@@ -70,7 +70,7 @@ occ_status_t run_experts_fwd(const occ_experts_t& p, const ExpertsFwdPlan& f, ch
       if (f.few == 1) hipLaunchKernelGGL((k_experts_dot<T, GATED>), grid, waves, 0, s, a);
       else if (f.few == 16) hipLaunchKernelGGL((k_experts_skinny<T, 1, GATED>), grid, block, 0, s, a);
       else if (f.few == 32) hipLaunchKernelGGL((k_experts_skinny<T, 2, GATED>), grid, block, 0, s, a);
-      else hipLaunchKernelGGL((k_experts_skinny<T, 4, GATED>), grid, block, 0, s, a);
+      else if constexpr (GATED) hipLaunchKernelGGL((k_experts_skinny<T, 4, GATED>), grid, block, 0, s, a);
     });
   }
   ExpertsArgs a{};

@@ -61,7 +61,7 @@ struct FewTimes {
 constexpr FewTimes kFewForms[4] = {{1, 4, {2.35, 2.35}, {1.35, 1.35}},
                                    {16, 16, {5.1, 8.0}, {6.45, 9.6}},
                                    {32, 32, {3.0, 5.0}, {8.5, 13.0}},
-                                   {64, 64, {9.0, 9.5}, {14.5, 18.6}}};
+                                   {64, 64, {0.0, 9.5}, {0.0, 18.6}}};
 
 inline int64_t few_across(int form, int64_t out, bool gated) {
   return form == 1 ? div_up(gated ? out : div_up(out, 2), 4) : div_up(out, 16);
@@ -151,6 +151,7 @@ inline occ_status_t plan_experts_fwd(const occ_experts_t& p, bool gated, Experts
   us = std::max(us + 2.0, weights);
   if (mean <= (double)kFewTokens)
     for (const FewTimes& t : kFewForms) {
+      if (t.form == 64 && !gated) continue;   // never ahead of two runs of 32
       const double few = std::max(few_experts_us(p, gated, t, es), weights);
       if (few > us || (f.few && few == us)) continue;
       us = few;
