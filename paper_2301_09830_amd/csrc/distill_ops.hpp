@@ -104,8 +104,10 @@ constexpr int64_t kDistillTokens = 512;
 
 template <class T, int NW>
 occ_status_t distill_steps(const occ_distill_t& d, const DistillArgs& a, int64_t whole, hipStream_t s) {
-  if (whole <= 2) return start_distill<T, NW, 2>(d, a, s);
-  if (whole <= 4) return start_distill<T, NW, 4>(d, a, s);
+  if constexpr (NW != 8) {   // eight waves: more than sixteen steps of four
+    if (whole <= 2) return start_distill<T, NW, 2>(d, a, s);
+    if (whole <= 4) return start_distill<T, NW, 4>(d, a, s);
+  }
   if constexpr (NW == 16) {
     if (whole <= 6) return start_distill<T, NW, 6>(d, a, s);
   }
