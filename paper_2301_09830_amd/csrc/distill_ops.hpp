@@ -98,9 +98,11 @@ occ_status_t start_distill(const occ_distill_t& d, const DistillArgs& all, hipSt
 }
 
 // Waves of a block: four, which leaves other blocks of a CU to load while one
-// computes, as long as they hold a row; sixteen where there are too few tokens
-// to fill the chip with fours.
-constexpr int64_t kDistillTokens = 512;
+// computes, or eight where four do not hold a row; sixteen, and the exponentials
+// kept, up to a token a CU.  us with sixteen and with four or eight, 511 and 512
+// tokens: bf16 8000 columns 11.5 and 8.0, 51200 29.3 and 24.2; fp32 8000 12.5 and
+// 9.3, 51200 41.7 and 41.8; with sixteen, 256 tokens take half of these.
+constexpr int64_t kDistillTokens = 256;
 
 template <class T, int NW>
 occ_status_t distill_steps(const occ_distill_t& d, const DistillArgs& a, int64_t whole, hipStream_t s) {
@@ -119,7 +121,7 @@ template <class T>
 occ_status_t run_distill(const occ_distill_t& d, hipStream_t s) {
   const DistillArgs a = distill_args(d);
   const int64_t four = d.vocab / (256 * (16 / (int64_t)sizeof(T)));   // whole steps of four waves
-  if (d.tokens >= kDistillTokens || four <= 2) {
+  if (d.tokens > kDistillTokens || four <= 2) {
     if (four <= 16) return distill_steps<T, 4>(d, a, four, s);
     if (four / 2 <= 16) return distill_steps<T, 8>(d, a, four / 2, s);
   }
@@ -132,7 +134,7 @@ occ_status_t run_distill(const occ_distill_t& d, hipStream_t s) {
 template <class T>
 occ_status_t run_distill_bwd(const occ_distill_t& d, hipStream_t s) {
   const DistillArgs all = distill_args(d);
-  const bool wide = d.tokens < kDistillTokens;
+  const bool wide = d.tokens <= kDistillTokens;
   return by_tokens(d, all, wide ? 1024 : 256, [&](const DistillArgs& a, dim3 grid) {
     return launch("distill_bwd", s, [&] {
       if (wide) hipLaunchKernelGGL((k_distill_bwd<T, 16, false>), grid, dim3(1024), 0, s, a);

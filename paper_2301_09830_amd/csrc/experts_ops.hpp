@@ -319,9 +319,12 @@ occ_status_t experts_backward_call(const occ_experts_grad_t* pp, unsigned flags,
   hipStream_t s = (hipStream_t)stream;
   if (l.tokens == 0) {
     if (accumulate) return OCC_OK;
-    for (int64_t e = 0; l.dW && e < p.experts; ++e) {
+    // one launch where the experts' rows follow each other
+    const bool whole = p.experts == 1 || p.stride_dw == wide * l.lddw;
+    const int64_t calls = whole ? 1 : p.experts, rows = whole ? p.experts * wide : wide;
+    for (int64_t e = 0; l.dW && e < calls; ++e) {
       char* const w = (char*)l.dW + e * p.stride_dw * (int64_t)ws_es;
-      OCC_TRY(ws_es == 2 ? zero_rows<uint16_t>(w, wide, l.in, l.lddw, s) : zero_rows<float>(w, wide, l.in, l.lddw, s));
+      OCC_TRY(ws_es == 2 ? zero_rows<uint16_t>(w, rows, l.in, l.lddw, s) : zero_rows<float>(w, rows, l.in, l.lddw, s));
     }
     return l.dbias ? zero_rows<float>(l.dbias, 1, p.experts * wide, p.experts * wide, s) : OCC_OK;
   }

@@ -42,3 +42,20 @@ def test_experts_without_rows_have_zeros(gated):
         for dtype in ("bf16", "f32"):
             run_backward(sizes, n_in, out, dtype, 4, gated, pad=4, gap=8)
             run_backward(sizes, n_in, out, dtype, 4, gated, dw_f32=True)
+
+
+def test_no_rows_at_all_have_zeros_in_every_expert():
+    """With the experts' gradients next to each other, and apart."""
+    import torch
+    from paper_2301_09830_amd import optcc
+
+    at = torch.zeros(6, dtype=torch.int32, device="cuda")
+    for dt in (torch.bfloat16, torch.float32):
+        for gap in (0, 3):
+            dW = torch.ones(5, 12 + gap, 40, dtype=dt, device="cuda")
+            db = torch.ones(5, 12, device="cuda")
+            optcc.occ_experts_gated_bwd(torch.empty(0, 6, dtype=dt, device="cuda"), at,
+                                        X=torch.empty(0, 40, dtype=dt, device="cuda"),
+                                        Z=torch.empty(0, 12, dtype=dt, device="cuda"),
+                                        dW=dW[:, :12], dbias=db)
+            assert not dW[:, :12].any() and (dW[:, 12:] == 1).all() and not db.any()
