@@ -497,8 +497,8 @@ occ_status_t occ_route_fwd(const occ_route_t* r, void* ws, size_t ws_bytes, occ_
  * them.  With s the sum of w dw over a token's choices:
  *   renorm 1   w (dw - s) at the chosen, 0 elsewhere (logits may be NULL)
  *   renorm 0   -p s at every expert, p their softmax, and w dw more at the chosen
- * dweights of a choice that is none are not looked at.  dlogits may be the
- * logits. */
+ * dweights of a choice that is none are not looked at; choices of one expert (a
+ * plan of the caller's) are added up in their order.  dlogits may be the logits. */
 occ_status_t occ_route_bwd(const occ_route_t* r, const float* dweights, void* dlogits, int64_t ldd,
                            occ_stream_t stream);
 

@@ -5,6 +5,11 @@
 // a block has.  The host does not know the runs' lengths: it launches as many
 // blocks as any lengths may need, and a block that finds no tile ends.
 //
+// Bound as the layers' products are: 16384 rows of 8 experts, gated 4096 x 8192 bf16
+// 1901 us (1157 TFLOP/s of the rows that there are), backward 4096 x 4096 2101 with dZ;
+// 32768 rows of 128 experts, 2048 x 1024, backward 541: dW has four K tiles an
+// expert, beside which the first loads and the results take most of a block's time.
+//
 // A block finds its tile from the offsets themselves: a wave counts the tiles
 // of 64 experts at a time and adds them up across its lanes, so that no launch
 // and no table stands before the products.
@@ -196,7 +201,8 @@ __global__ __launch_bounds__(512, 4) void k_experts_direct(ExpertsArgs a) {
 }
 
 // Few rows an expert: its weights are streamed, once for every 4 rows (along
-// K) or every 16 NT (through the matrix instructions).
+// K) or every 16 NT (through the matrix instructions).  16 gated rows over 64
+// experts, 2048 x 1024 bf16: 17 us, 5.4 TB/s of weights.
 struct ExpertsFewArgs {
   SkinnyArgs g;
   Groups of;

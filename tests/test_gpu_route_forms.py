@@ -8,6 +8,8 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from paper_2301_09830_amd import optcc  # noqa: E402
+from experts_ref import route_bwd64  # noqa: E402
+from stage_ref import within  # noqa: E402
 from test_gpu_route import check_route, gen, rand  # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -72,3 +74,21 @@ def test_every_token_chooses_the_same_experts():
     x[:, 7], x[:, 30] = 2.0, 1.0
     r = check_route(x, 2, True)
     assert r.offsets[8] - r.offsets[7] == 3000 and r.offsets[31] - r.offsets[30] == 3000
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("e,k", [(10, 2), (10, 7), (200, 16), (700, 32)])
+def test_gradient_of_an_expert_chosen_twice(e, k, dtype):
+    """A plan of the caller's own: the parts of equal choices add up, in order."""
+    x = rand(gen(e), 70, e, DT[dtype])
+    r = optcc.occ_route_fwd(x, k)
+    index = r.index.clone()
+    index[::3, 1] = index[::3, 0]
+    index[5] = 3
+    index[6, k // 2:] = -1
+    r = r._replace(index=index)
+    dw = torch.randn(70, k, generator=gen(k), device="cuda")
+    for renorm in (True, False):
+        got = optcc.occ_route_bwd(dw, x, r, renorm=renorm)
+        within(got, *route_bwd64(x, index, r.weights, dw, renorm), "dlogits")
+        assert torch.equal(got, optcc.occ_route_bwd(dw, x, r, renorm=renorm))
