@@ -21,6 +21,14 @@ inline double mean_runs(int64_t rows, int64_t experts, int64_t run) {
   return n * std::max(1.0, mean / (double)run + (experts > 1 ? 0.6 : 0.5));
 }
 
+// Lanes that share a token in the router's gradient, and the tokens of one of
+// its launches: a launch holds fewer than 2^32 threads, in whole blocks of 256.
+inline int route_lanes(int64_t experts, int k) { return k > 16 || experts > 256 ? 64 : 16; }
+
+inline int64_t route_bwd_part(int64_t experts, int k) {
+  return (((int64_t)1 << 32) - 1) / 256 * (256 / route_lanes(experts, k));
+}
+
 // A matrix of every expert: rows x cols, ld apart, and `stride` to the next.
 inline bool experts_ok(int64_t experts, int64_t rows, int64_t cols, int64_t ld, int64_t stride) {
   if (!ld_ok(cols, ld)) return false;

@@ -3,6 +3,7 @@
 #pragma once
 
 #include "kernels_route.hpp"
+#include "plan_experts.hpp"
 
 namespace {
 
@@ -44,7 +45,7 @@ size_t route_bytes(const occ_route_t& r) {
 template <class F>
 occ_status_t by_experts(const occ_route_t& r, F&& f) {
   using std::integral_constant;
-  if (r.k > 16 || r.experts > 256) return f(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+  if (route_lanes(r.experts, r.k) == 64) return f(integral_constant<int, 64>{}, integral_constant<int, 4>{});
   if (r.experts > 128) return f(integral_constant<int, 16>{}, integral_constant<int, 4>{});
   if (r.experts > 64) return f(integral_constant<int, 16>{}, integral_constant<int, 2>{});
   return f(integral_constant<int, 16>{}, integral_constant<int, 1>{});
@@ -97,23 +98,33 @@ occ_status_t run_route(const occ_route_t& r, char* ws, hipStream_t s) {
 
 template <class T>
 occ_status_t run_route_bwd(const occ_route_t& r, const float* dweights, void* dlogits, int64_t ldd, hipStream_t s) {
-  RouteGradArgs a{};
-  a.logits = r.logits;
-  a.dlogits = dlogits;
-  a.index = r.index;
-  a.weights = r.weights;
-  a.dweights = dweights;
-  a.ldl = r.ldl;
-  a.ldd = ldd;
-  a.tokens = r.tokens;
-  a.experts = (int32_t)r.experts;
-  a.k = r.k;
-  a.renorm = r.renorm;
+  RouteGradArgs all{};
+  all.logits = r.logits;
+  all.dlogits = dlogits;
+  all.index = r.index;
+  all.weights = r.weights;
+  all.dweights = dweights;
+  all.ldl = r.ldl;
+  all.ldd = ldd;
+  all.experts = (int32_t)r.experts;
+  all.k = r.k;
+  all.renorm = r.renorm;
+  const int64_t part = route_bwd_part(r.experts, r.k);
   return by_experts(r, [&](auto lanes, auto quads) {
-    return launch("route_bwd", s, [&] {
-      hipLaunchKernelGGL((k_route_bwd<T, lanes, quads>), dim3((unsigned)div_up(r.tokens, 256 / lanes)), dim3(256), 0, s,
-                         a);
-    });
+    for (int64_t t = 0; t < r.tokens; t += part) {
+      RouteGradArgs a = all;
+      a.tokens = std::min(part, r.tokens - t);
+      if (a.logits) a.logits = (const T*)a.logits + t * a.ldl;
+      a.dlogits = (T*)a.dlogits + t * a.ldd;
+      a.index += t * a.k;
+      a.weights += t * a.k;
+      a.dweights += t * a.k;
+      OCC_TRY(launch("route_bwd", s, [&] {
+        hipLaunchKernelGGL((k_route_bwd<T, lanes, quads>), dim3((unsigned)div_up(a.tokens, 256 / lanes)), dim3(256), 0,
+                           s, a);
+      }));
+    }
+    return OCC_OK;
   });
 }
 
