@@ -515,21 +515,24 @@ typedef struct {
 } occ_exchange_t;
 
 /* Xs[s] = X[order[s] / k] for s < offsets[experts]; rows behind are left alone.
+ * A last offset out of 0 .. rows is taken as the nearer end; it and an entry that
+ * is none of the tokens' raise OCC_F_BAD_ROWS, and such an entry's row is left.
  * Its gradient is occ_combine of dXs without weights. */
 occ_status_t occ_dispatch(const occ_exchange_t* x, const void* X, int64_t ldx, void* Xs, int64_t ldxs,
                           occ_stream_t stream);
 
 /* Y[t] = sum over j of weights[t][j] Ys[slots[t][j]] + R[t], summed in fp32 in
  * the order of j, rounded once.  weights (fp32) NULL: ones; R may be NULL, or Y.
- * A slot of -1 adds nothing, whatever its weight; one of `rows` or more raises
- * OCC_F_BAD_ROWS and adds nothing. */
+ * A slot of -1 adds nothing, whatever its weight; any other outside 0 .. rows - 1
+ * adds nothing either and raises OCC_F_BAD_ROWS. */
 occ_status_t occ_combine(const occ_exchange_t* x, const float* weights, const void* Ys, int64_t ldys, const void* R,
                          int64_t ldr, void* Y, int64_t ldy, occ_stream_t stream);
 
 /* dYs[slots[t][j]] = weights[t][j] dY[t] and dweights[t][j] = <dY[t],
  * Ys[slots[t][j]]> (fp32); either may be NULL.  An entry without a row has
- * dweights 0; rows of dYs that no entry has are left alone.  An entry whose
- * place in order does not name it raises OCC_F_BAD_ROWS and counts as without. */
+ * dweights 0; rows of dYs that no entry has are left alone.  A slot outside -1 ..
+ * rows - 1 raises OCC_F_BAD_ROWS, as does an entry whose place in order does not
+ * name it; both count as without. */
 occ_status_t occ_combine_bwd(const occ_exchange_t* x, const float* weights, const void* dY, int64_t lddy,
                              const void* Ys, int64_t ldys, void* dYs, int64_t lddys, float* dweights,
                              occ_stream_t stream);

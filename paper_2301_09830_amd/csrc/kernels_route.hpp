@@ -713,7 +713,8 @@ __device__ __forceinline__ void raise_rows(uint32_t* flags) {
 template <class T>
 __global__ __launch_bounds__(EX_WAVES * 64) void k_dispatch(ExchangeArgs g) {
   constexpr int CH = 16 / sizeof(T);
-  const int64_t total = min((int64_t)max(g.offsets[g.experts], 0), g.rows) * g.parts;
+  const int64_t last = g.offsets[g.experts], rows = min(max(last, (int64_t)0), g.rows), total = rows * g.parts;
+  if (last != rows && blockIdx.x == 0 && wave_id() == 0) raise_rows(g.flags);
   for (int64_t unit = (int64_t)blockIdx.x * EX_WAVES + wave_id(); unit < total; unit += (int64_t)gridDim.x * EX_WAVES) {
     int part;
     const int64_t s = row_of_unit(unit, total, g.parts, part);
@@ -762,7 +763,7 @@ __device__ __forceinline__ void combine_part(const ExchangeArgs& g, int64_t t, i
       have[u] = false;
       if (j0 + u >= g.k) continue;
       const int64_t s = g.slots[t * g.k + j0 + u];
-      if (s >= g.rows) raise_rows(g.flags);
+      if (s < -1 || s >= g.rows) raise_rows(g.flags);
       if (s < 0 || s >= g.rows) continue;
       have[u] = true;
       w[u] = g.weights ? g.weights[t * g.k + j0 + u] : 1.0f;
@@ -815,7 +816,7 @@ __device__ __forceinline__ void combine_entry(const ExchangeArgs& g, int64_t ent
   const int lane = threadIdx.x & 63;
   const int64_t s = g.slots[entry];
   const bool in = s >= 0 && s < g.rows, have = in && g.order[s] == entry;
-  if (s >= g.rows || in != have) raise_rows(g.flags);
+  if (s < -1 || s >= g.rows || in != have) raise_rows(g.flags);
   if (!have) {
     if (g.dweights && lane == 0) g.dweights[entry] = 0.0f;
     return;
