@@ -585,8 +585,8 @@ occ_status_t occ_experts_gated_bwd(const occ_experts_grad_t* l, unsigned flags, 
  * first part, one whose label is negative (or labels NULL) no second.  With
  * neither, or with scale 0, the loss is 0 and the gradient a row of zeros, and the
  * token's logits are not looked at.  An index or label of `vocab` or more counts
- * as masked and raises OCC_F_BAD_ROWS.  alpha 1 leaves labels, alpha 0 the list
- * out of account.
+ * as masked and raises OCC_F_BAD_ROWS, also of a token whose scale is 0.  alpha 1
+ * leaves labels, alpha 0 the list out of account.
  *   occ_distill_fwd   loss (fp32, a token each); lse, if given, receives the
  *                     logarithms of the two softmaxes' sums (tokens x 2: at T, at
  *                     1; 0 for a part that a token has not); dS, if given, the

@@ -94,10 +94,18 @@ __device__ __forceinline__ DistillRow distill_entries(const DistillArgs& g, int6
   r.soft = false;
   r.entropy = 0.0f;
   bool bad = label >= g.vocab;
-  if (r.scale == 0.0f) return r;
+  const int k = g.alpha != 0.0f ? g.k : 0;
+  auto raise = [&] {
+    if (__ballot(bad) && (threadIdx.x & 63) == 0 && g.flags) atomicOr(g.flags, kBadRows);
+  };
+  if (r.scale == 0.0f) {   // no part in the loss; its columns are checked all the same
+    if (!g.flags) return r;
+    for (int j = threadIdx.x; j < k; j += NT) bad |= g.index[token * g.ldi + j] >= g.vocab;
+    raise();
+    return r;
+  }
   const T* const row = (const T*)g.S + token * g.lds;
   const float inv = 1.0f / g.temperature;
-  const int k = g.alpha != 0.0f ? g.k : 0;
   for (int j = threadIdx.x; j < k; j += NT) {
     const int i = g.index[token * g.ldi + j];
     const bool in = i >= 0 && i < g.vocab;
@@ -114,7 +122,7 @@ __device__ __forceinline__ DistillRow distill_entries(const DistillArgs& g, int6
     e.index[g.k] = r.hard ? label : -1;
     e.s[g.k] = r.hard ? ld_elem<T>(row + label) : 0.0f;
   }
-  if (__ballot(bad) && (threadIdx.x & 63) == 0 && g.flags) atomicOr(g.flags, kBadRows);
+  raise();
   __syncthreads();
   // the teacher's softmax by one wave, while the row is on its way to the others
   if (threadIdx.x < 64) {
