@@ -112,8 +112,8 @@ __device__ __forceinline__ DistillRow distill_entries(const DistillArgs& g, int6
     bad |= i >= g.vocab;
     float t = g.teacher_bf16 ? ld_elem<uint16_t>((const uint16_t*)g.teacher + token * g.ldt + j)
                              : ((const float*)g.teacher)[token * g.ldt + j];
-    t = in ? t * inv : -INFINITY;   // what stands at a masked entry is not looked at
-    const bool live = in && t != -INFINITY;
+    t = in ? t : -INFINITY;   // what stands at a masked entry is not looked at
+    const bool live = t != -INFINITY;
     e.index[j] = live ? i : -1;
     e.p[j] = t;
     e.s[j] = live ? ld_elem<T>(row + i) : 0.0f;
@@ -124,17 +124,18 @@ __device__ __forceinline__ DistillRow distill_entries(const DistillArgs& g, int6
   }
   raise();
   __syncthreads();
-  // the teacher's softmax by one wave, while the row is on its way to the others
+  // the teacher's softmax by one wave, while the row is on its way to the others;
+  // the maximum is subtracted before the division by T, as in the row's
   if (threadIdx.x < 64) {
     float top = -INFINITY, sum = 0.0f, plog = 0.0f;
     for (int j = threadIdx.x; j < k; j += 64) top = max_nan(top, e.p[j]);
     top = block_max<1>(top, lds);
     if (top != -INFINITY) {
-      for (int j = threadIdx.x; j < k; j += 64) sum += exp_f(e.p[j] - top);
+      for (int j = threadIdx.x; j < k; j += 64) sum += exp_f((e.p[j] - top) * inv);
       sum = block_sum<1>(sum, lds);
       const float log_sum = logf(sum), part = 1.0f / sum;
       for (int j = threadIdx.x; j < k; j += 64) {
-        const float d = e.p[j] - top, p = exp_f(d) * part;
+        const float d = (e.p[j] - top) * inv, p = exp_f(d) * part;
         plog += p > 0.0f || p != p ? p * (d - log_sum) : 0.0f;
         e.p[j] = p;
       }
