@@ -593,8 +593,9 @@ occ_status_t occ_experts_gated_bwd(const occ_experts_grad_t* l, unsigned flags, 
  *                     gradient of the sum of the losses, in the same pass
  *   occ_distill_bwd   dS from lse (loss is not looked at); scale carries the
  *                     gradient of each loss: the forward's scale times it
- * dS has the type of S and may be S.  Sums are held in fp32, dS is rounded once;
- * from lse, itself rounded to fp32, it is |lse| 2^-24 less exact. */
+ * dS has the type of S and may be S.  Sums are held in fp32, dS is rounded once.
+ * From lse, itself rounded to fp32, a softmax is off by a few 2^-24 of |lse| + |s| / T
+ * more; tokens whose lse is beyond +-1024 are summed anew from S. */
 typedef struct {
   int32_t dtype;   /* occ_dtype_t of S and dS */
   int32_t t_dtype; /* occ_dtype_t of the teacher's logits */

@@ -206,20 +206,44 @@ constexpr float kLog2e = 1.4426950408889634f;
 // Exponentials of a row: e^((s - m) / T), or e^(s - m) for the labels alone or
 // at T = 1, and both where a token has entries and a label at another
 // temperature (`two`).  m is the row's maximum, subtracted before anything is
-// multiplied, so that rows of the type's lowest values stay exact; from stored
-// logarithms m is 0 and oa, ob hold them, in powers of two.
+// multiplied, so that rows of the type's lowest values stay exact.
 struct DistillExp {
-  float m, ka, kb, oa, ob;
+  float m, ka, kb;
   bool two;
   __device__ __forceinline__ DistillExp(const DistillArgs& g, const DistillRow& r, float top) {
     m = top;
     ka = r.soft ? kLog2e / g.temperature : kLog2e;
     kb = kLog2e;
-    oa = ob = 0.0f;
     two = r.soft && r.hard && g.temperature != 1.0f;
   }
-  __device__ __forceinline__ float a(float s) const { return __builtin_amdgcn_exp2f(__builtin_fmaf(s - m, ka, -oa)); }
-  __device__ __forceinline__ float b(float s) const { return __builtin_amdgcn_exp2f(__builtin_fmaf(s - m, kb, -ob)); }
+  __device__ __forceinline__ float a(float s) const { return __builtin_amdgcn_exp2f((s - m) * ka); }
+  __device__ __forceinline__ float b(float s) const { return __builtin_amdgcn_exp2f((s - m) * kb); }
+};
+
+// The same over their sums, from stored logarithms of these: e^(s / T - lse).
+// The logarithm is subtracted before anything is rounded but it and 1 / T, so an
+// exponent is off by a few 2^-24 of |lse| + |s| / T.  That is too much for rows
+// whose logarithm is beyond kFarLse (6e-4 of the softmax there; all of it for a
+// row of the type's lowest values): they are summed anew, and use the maximum.
+constexpr float kFarLse = 1024.0f;
+
+struct DistillLse {
+  float ia, oa, ob, ka;
+  bool two;
+  __device__ __forceinline__ DistillLse(const DistillArgs& g, const DistillRow& r, float soft, float hard) {
+    ia = r.soft ? 1.0f / g.temperature : 1.0f;
+    oa = r.soft ? soft : hard;
+    ob = hard;
+    ka = kLog2e;
+    two = r.soft && r.hard && g.temperature != 1.0f;
+  }
+  __device__ __forceinline__ void from_maximum(const DistillExp& x) {
+    ia = 1.0f;
+    oa = ob = x.m;
+    ka = x.ka;
+  }
+  __device__ __forceinline__ float a(float s) const { return __builtin_amdgcn_exp2f(__builtin_fmaf(s, ia, -oa) * ka); }
+  __device__ __forceinline__ float b(float s) const { return __builtin_amdgcn_exp2f((s - ob) * kLog2e); }
 };
 
 // Factors of the exponentials in the gradient.
@@ -233,8 +257,8 @@ struct DistillGrad {
   }
 };
 
-template <class T>
-__device__ __forceinline__ f32x4_t grad_piece(f32x4_t v, const DistillExp& x, const DistillGrad& d) {
+template <class T, class X>
+__device__ __forceinline__ f32x4_t grad_piece(f32x4_t v, const X& x, const DistillGrad& d) {
   constexpr int CH = 16 / sizeof(T);
   float e[CH];
   widen<T>(v, e);
@@ -259,10 +283,9 @@ __device__ __forceinline__ void st_row_piece(T* p, f32x4_t v, int left) {
 
 // The columns of the entries, over what the rest of the row stored there: each
 // by the wave that stored it, whose stores to one place stay in order.
-template <class T, int NW>
-__device__ __forceinline__ void store_entries(const DistillArgs& g, int64_t token, const DistillRow& r,
-                                              const DistillToken<DL_ENTRIES>& e, const DistillExp& x,
-                                              const DistillGrad& d) {
+template <class T, int NW, class X>
+__device__ __forceinline__ void store_entries(const DistillArgs& g, int64_t token, const DistillToken<DL_ENTRIES>& e,
+                                              const X& x, const DistillGrad& d) {
   constexpr int CH = 16 / sizeof(T);
   wave_step();
   const int wave = wave_id();
@@ -383,34 +406,30 @@ __global__ __launch_bounds__(NW * 64, 4) void k_distill(DistillArgs g) {
     for (int p = 0; p < VPT; ++p)
       if (p < whole) st_row_piece<T, NT>(out + c0 + p * STEP, scaled(kept + p * CH), CH);
     if (c1 < g.vocab) st_row_piece<T, NT>(out + c1, scaled(kept + VPT * CH), g.vocab - c1);
-    return store_entries<T, NW>(g, token, r, e, x, d);
+    return store_entries<T, NW>(g, token, e, x, d);
   }
 #pragma unroll
   for (int p = 0; p < VPT; ++p)
     if (p < whole) st_row_piece<T, NT>(out + c0 + p * STEP, grad_piece<T>(fresh(v[p]), x, d), CH);
   if (c1 < g.vocab) st_row_piece<T, NT>(out + c1, grad_piece<T>(fresh(last), x, d), g.vocab - c1);
-  store_entries<T, NW>(g, token, r, e, x, d);
+  store_entries<T, NW>(g, token, e, x, d);
 }
 
-// Rows that the registers of a block do not hold: the maximum and the sums in
-// one pass, kept together, then the gradient from a second one, which finds
-// the row in the memory-side cache.
-template <class T>
-__global__ __launch_bounds__(1024) void k_distill_long(DistillArgs g) {
-  constexpr int NW = 16, CH = 16 / sizeof(T), STEP = NW * 64 * CH, U = 4;
-  __shared__ DistillToken<DL_ENTRIES> e;
-  __shared__ float lds[NW];
-  const int64_t token = blockIdx.x;
-  const DistillRow r = distill_entries<T, NW>(g, token, e, lds);
-  if (!r.soft && !r.hard) return ignored_token<T, NW>(g, token);
-  const T* const row = (const T*)g.S + token * g.lds;
-  const DistillExp unit(g, r, 0.0f);   // its factors alone
+// A row's maximum, and the sums of its exponentials, kept together in one pass
+// of U pieces at a time.  unit: an exponential's factors (its m is not used).
+struct DistillSums {
+  float m, z, z1;
+};
+
+template <class T, int NW, int U>
+__device__ __forceinline__ DistillSums row_sums(const T* row, int vocab, const DistillExp& unit, float* lds) {
+  constexpr int CH = 16 / sizeof(T), STEP = NW * 64 * CH;
   float m = -INFINITY, z = 0.0f, z1 = 0.0f;
-  for (int c0 = threadIdx.x * CH; c0 < g.vocab; c0 += U * STEP) {
+  for (int c0 = threadIdx.x * CH; c0 < vocab; c0 += U * STEP) {
     f32x4_t v[U];
     float f[U][CH], top = m;
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = row_piece<T>(row, c0 + u * STEP, g.vocab);
+    for (int u = 0; u < U; ++u) v[u] = row_piece<T>(row, c0 + u * STEP, vocab);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       widen<T>(v[u], f[u]);
@@ -429,15 +448,32 @@ __global__ __launch_bounds__(1024) void k_distill_long(DistillArgs g) {
       }
     m = top;
   }
-  const float all = block_reduce<NW>(m, lds, [](float a, float b) { return fmaxf(a, b); });
-  const float own = m == -INFINITY && z == 0.0f ? 0.0f : m - all;   // a thread without a column has nothing to add
-  z = block_sum<NW>(z * __builtin_amdgcn_exp2f(unit.ka * own), lds);
-  z1 = unit.two ? block_sum<NW>(z1 * __builtin_amdgcn_exp2f(unit.kb * own), lds) : z;
-  if (all == -INFINITY) z = z1 = NAN;
-  distill_loss<NW>(g, token, r, e, all, z, z1, lds);
+  DistillSums r;
+  r.m = block_reduce<NW>(m, lds, [](float a, float b) { return fmaxf(a, b); });
+  const float own = m == -INFINITY && z == 0.0f ? 0.0f : m - r.m;   // a thread without a column has nothing to add
+  r.z = block_sum<NW>(z * __builtin_amdgcn_exp2f(unit.ka * own), lds);
+  r.z1 = unit.two ? block_sum<NW>(z1 * __builtin_amdgcn_exp2f(unit.kb * own), lds) : r.z;
+  if (r.m == -INFINITY) r.z = r.z1 = NAN;
+  return r;
+}
+
+// Rows that the registers of a block do not hold: the maximum and the sums in
+// one pass, then the gradient from a second one, which finds the row in the
+// memory-side cache.
+template <class T>
+__global__ __launch_bounds__(1024) void k_distill_long(DistillArgs g) {
+  constexpr int NW = 16, CH = 16 / sizeof(T), STEP = NW * 64 * CH, U = 4;
+  __shared__ DistillToken<DL_ENTRIES> e;
+  __shared__ float lds[NW];
+  const int64_t token = blockIdx.x;
+  const DistillRow r = distill_entries<T, NW>(g, token, e, lds);
+  if (!r.soft && !r.hard) return ignored_token<T, NW>(g, token);
+  const T* const row = (const T*)g.S + token * g.lds;
+  const DistillSums sums = row_sums<T, NW, U>(row, g.vocab, DistillExp(g, r, 0.0f), lds);
+  distill_loss<NW>(g, token, r, e, sums.m, sums.z, sums.z1, lds);
   if (!g.dS) return;
-  const DistillExp x(g, r, all);
-  const DistillGrad d(g, r, x.two, z, z1);
+  const DistillExp x(g, r, sums.m);
+  const DistillGrad d(g, r, x.two, sums.z, sums.z1);
   T* const out = (T*)g.dS + token * g.ldd;
   for (int c0 = threadIdx.x * CH; c0 < g.vocab; c0 += U * STEP) {
     f32x4_t v[U];
@@ -449,7 +485,7 @@ __global__ __launch_bounds__(1024) void k_distill_long(DistillArgs g) {
       if (c < g.vocab) st_piece<T>(out + c, grad_piece<T>(v[u], x, d), g.vocab - c);
     }
   }
-  store_entries<T, NW>(g, token, r, e, x, d);
+  store_entries<T, NW>(g, token, e, x, d);
 }
 
 // The gradient from the stored logarithms of the sums.
@@ -462,11 +498,17 @@ __global__ __launch_bounds__(NW * 64) void k_distill_bwd(DistillArgs g) {
   const float soft = g.lse[2 * token], hard = g.lse[2 * token + 1];
   const DistillRow r = distill_entries<T, NW>(g, token, e, lds);
   if (!r.soft && !r.hard) return zero_row<T, NW>(g, token);
-  DistillExp x(g, r, 0.0f);
-  x.oa = kLog2e * (r.soft ? soft : hard);
-  x.ob = kLog2e * hard;
-  const DistillGrad d(g, r, x.two, 1.0f, 1.0f);
+  DistillLse x(g, r, soft, hard);
   const T* const row = (const T*)g.S + token * g.lds;
+  float z = 1.0f, z1 = 1.0f;
+  if ((r.soft && !(fabsf(soft) <= kFarLse)) || (r.hard && !(fabsf(hard) <= kFarLse))) {
+    const DistillExp unit(g, r, 0.0f);
+    const DistillSums sums = row_sums<T, NW, 1>(row, g.vocab, unit, lds);   // all read before a column is written
+    x.from_maximum(DistillExp(g, r, sums.m));
+    z = sums.z;
+    z1 = sums.z1;
+  }
+  const DistillGrad d(g, r, x.two, z, z1);
   T* const out = (T*)g.dS + token * g.ldd;
   for (int c0 = threadIdx.x * CH; c0 < g.vocab; c0 += U * STEP) {
     f32x4_t v[U];
@@ -478,7 +520,7 @@ __global__ __launch_bounds__(NW * 64) void k_distill_bwd(DistillArgs g) {
       if (c < g.vocab) st_row_piece<T, NT>(out + c, grad_piece<T>(v[u], x, d), g.vocab - c);
     }
   }
-  store_entries<T, NW>(g, token, r, e, x, d);
+  store_entries<T, NW>(g, token, e, x, d);
 }
 
 }  // namespace occ

@@ -47,3 +47,70 @@ def test_teachers_of_extreme_values(T, dtype):
         within(lse, *want["lse"], "lse")
         within(optcc.occ_distill_bwd(S, index, teacher, lse, T, alpha, labels), *want["dS_lse"],
                "dS from lse")
+
+
+def rows_far_from_zero(dtype, v):
+    """Rows whose logarithm of the sum is near the type's ends, or some thousands."""
+    dt, low, high = DT[dtype], torch.finfo(DT[dtype]).min, torch.finfo(DT[dtype]).max
+    S = torch.randn(12, v, generator=gen(5), device="cuda")
+    S[3] += 3000.0
+    S[4] -= 3000.0
+    S[5] = S[5] * 0.01 + 1021.0            # within the stored logarithms, or just not
+    S[6] = S[6] * 0.01 - 1030.0
+    S = S.to(dt)
+    S[0], S[1] = low, high
+    S[2, v // 2:] = low
+    S[7, 1:] = low
+    S[8, :-1], S[8, -1] = -math.inf, low
+    S[9, ::2] = -math.inf
+    S[9, 1::2] = low
+    S[10] = low
+    S[10, v // 3] = low / 2
+    return S
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("v", [64, 5003, 230000])
+@pytest.mark.parametrize("T", [0.5, 1.0, 3.0])
+def test_gradient_from_logarithms_far_from_zero(T, v, dtype):
+    """As exact as from the same pass where the logarithm is beyond 1024, and even for a
+    row of the type's lowest value."""
+    S = rows_far_from_zero(dtype, v)
+    t, k = S.shape[0], 5
+    index = torch.rand(t, v, generator=gen(6), device="cuda").argsort(1)[:, :k].to(torch.int32)
+    index = index.contiguous()
+    teacher = torch.randn(t, k, generator=gen(7), device="cuda")
+    labels = torch.randint(0, v, (t,), generator=gen(8), device="cuda", dtype=torch.int32)
+    labels[::3] = -1
+    for alpha in (1.0, 0.5, 0.0):
+        lse, dS = torch.empty(t, 2, device="cuda"), torch.empty_like(S)
+        optcc.occ_distill_fwd(S, index, teacher, T, alpha, labels, lse=lse, dS=dS)
+        # the forward's own gradient, and from the logarithms alone or in place
+        want = distill64(S, index, teacher, T, alpha, labels, None)
+        got = optcc.occ_distill_bwd(S, index, teacher, lse, T, alpha, labels)
+        far = ~(lse.abs() <= 1024.0).all(1)
+        assert far.any() and not far.all()
+        d, b = want["dS"]
+        within(dS, d, b, "dS")
+        within(got[far], d[far], b[far], "dS from far logarithms")
+        d, b = want["dS_lse"]
+        within(got[~far], d[~far], b[~far], "dS from lse")
+        s = S.clone()
+        optcc.occ_distill_bwd(s, index, teacher, lse, T, alpha, labels, dS=s)
+        assert torch.equal(s, got)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_that_are_no_distribution(dtype):
+    """NaN, +inf or nothing but -inf in a row: its gradient is NaN from the logarithms
+    too, and the other rows' are not touched."""
+    S = torch.randn(5, 700, generator=gen(9), device="cuda").to(DT[dtype])
+    S[1, 3], S[2, 699], S[3] = float("nan"), math.inf, -math.inf
+    index = torch.tensor([[1, 2]] * 5, dtype=torch.int32, device="cuda")
+    teacher, lse = torch.zeros(5, 2, device="cuda"), torch.empty(5, 2, device="cuda")
+    dS = torch.empty_like(S)
+    optcc.occ_distill_fwd(S, index, teacher, lse=lse, dS=dS)
+    got = optcc.occ_distill_bwd(S, index, teacher, lse)
+    for d in (dS, got):
+        assert torch.isnan(d[[1, 3]]).all() and torch.isnan(d[2, 699])
+        assert torch.isfinite(d[[0, 4]]).all()
