@@ -610,7 +610,7 @@ typedef struct {
   int64_t ldt;
   const int32_t* labels; /* a token each, or NULL */
   const float* scale;    /* a token each, or NULL: ones */
-  float temperature, alpha; /* T > 0; alpha 0 .. 1 */
+  float temperature, alpha; /* T > 0, its square a normal number; alpha 0 .. 1 */
   float* loss;
   float* lse;
   void* dS;

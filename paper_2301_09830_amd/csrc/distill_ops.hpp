@@ -12,7 +12,9 @@ occ_status_t check_distill(const occ_distill_t* d) {
   if (!d) return OCC_E_NULL;
   if ((d->dtype != OCC_F32 && d->dtype != OCC_BF16) || (d->t_dtype != OCC_F32 && d->t_dtype != OCC_BF16))
     return OCC_E_DTYPE;
-  if (!(d->temperature > 0.0f) || !std::isfinite(d->temperature) || !(d->alpha >= 0.0f && d->alpha <= 1.0f))
+  // T^2 and 1 / T are factors, and neither may overflow or be lost
+  if (!(d->temperature > 0.0f) || !std::isnormal(d->temperature * d->temperature) ||
+      !(d->alpha >= 0.0f && d->alpha <= 1.0f))
     return OCC_E_VALUE;
   if (d->tokens < 0 || d->tokens >= kMaxTokens || d->vocab < 1 || d->vocab > kMaxVocab || d->k < 0 ||
       d->k > OCC_MAX_TEACHER || !ld_ok(d->vocab, d->lds) || (d->dS && !ld_ok(d->vocab, d->ldds)))

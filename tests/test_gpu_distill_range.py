@@ -114,3 +114,29 @@ def test_rows_that_are_no_distribution(dtype):
     for d in (dS, got):
         assert torch.isnan(d[[1, 3]]).all() and torch.isnan(d[2, 699])
         assert torch.isfinite(d[[0, 4]]).all()
+
+
+@pytest.mark.parametrize("T", [2.0 ** -63, 1e-3, 1e4, 2.0 ** 63])
+def test_extreme_temperatures(T):
+    """The gradient at the ends of the temperatures that are taken, and the loss there: the
+    difference to the largest logit at one, the size of the list and the vocabulary at the
+    other."""
+    t, v, k = 6, 300, 4
+    S = torch.randn(t, v, generator=gen(10), device="cuda")
+    index = torch.rand(t, v, generator=gen(11), device="cuda").argsort(1)[:, :k].to(torch.int32)
+    index = index.contiguous()
+    teacher = torch.randn(t, k, generator=gen(12), device="cuda")
+    lse, dS = torch.empty(t, 2, device="cuda"), torch.empty_like(S)
+    loss = optcc.occ_distill_fwd(S, index, teacher, T, lse=lse, dS=dS)
+    assert not torch.isnan(loss).any() and torch.isfinite(dS).all()
+    T = torch.tensor(T, dtype=torch.float32).item()
+    want = distill64(S, index, teacher, T, 1.0, None, None)
+    # T^2 log(300 / 4), the loss of even distributions, is 4.3 2^126 at 2^63: more than fp32 holds
+    d, b = want["loss"]
+    over = d.abs() > torch.finfo(torch.float32).max
+    assert over.all() if T == 2.0 ** 63 else not over.any()
+    assert (loss[over] == math.inf).all()
+    within(loss[~over], d[~over], b[~over], "loss")
+    within(dS, *want["dS"], "dS")
+    got = optcc.occ_distill_bwd(S, index, teacher, lse, T)
+    within(got, *want["dS_lse"], "dS from lse")
