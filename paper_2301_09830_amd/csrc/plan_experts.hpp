@@ -183,6 +183,10 @@ inline occ_status_t plan_experts_fwd(const occ_experts_t& p, bool gated, Experts
   return OCC_OK;
 }
 
+// Before the products: blocks of 256 threads in a launch of fewer than 2^32,
+// beside those of the copies.
+constexpr int64_t kMaxPrepBlocks = (((int64_t)1 << 32) - 1) / 256 - 3 * kMaxCopyBlocks;
+
 struct ExpertsBwdPlan {
   bool has_dz = false, planes = false, direct = false;
   bool copy_dy = false, copy_x = false, copy_w = false;
@@ -296,7 +300,7 @@ inline occ_status_t plan_experts_bwd(const occ_experts_grad_t& p, bool gated, Ex
     const int64_t down = std::max<int64_t>(1, std::min<int64_t>(div_up(most, f.across), div_up(l.tokens, DZ_ROWS)));
     f.strip = up(div_up(l.tokens, down), DZ_ROWS);
     f.strips = most_runs(l.tokens, p.experts, f.strip);
-    if (f.across * f.strips >= ((int64_t)1 << 30)) return OCC_E_SHAPE;
+    if (f.across * f.strips > kMaxPrepBlocks) return OCC_E_SHAPE;
     if (l.dbias) f.bias_off = c.take((size_t)f.strips * wide * 4);
   }
   if (f.copy_w) f.w_off = c.take((size_t)(p.experts * wide) * piece_ld(l.in, os) * os * np);

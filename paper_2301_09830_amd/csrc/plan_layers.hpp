@@ -72,6 +72,7 @@ constexpr double kMaxPartBytes = 512e6;
 // A launch holds fewer than 2^32 threads: of blocks of 512, those of the
 // products and, beside them, of the bias gradient (16 columns or more each).
 constexpr int64_t kMaxBlocks = (((int64_t)1 << 32) - 1) / 512 - kMaxWidth / 16;
+constexpr int64_t kMaxCopyBlocks = 8192;   // of one operand's copy
 
 // One product of m x width results over k: its blocks with a tile and a split.
 struct Product {

@@ -68,7 +68,7 @@ CopyArgs copy_operand(const void* src, int64_t ld, int64_t rows, int64_t cols, c
   const size_t es = planes ? 2 : sizeof(T);
   c.pieces = (int32_t)(piece_ld(cols, es) * (int64_t)es / 16);
   c.plane = planes ? rows * piece_ld(cols, es) : 0;
-  c.blocks = (int32_t)std::min<int64_t>(div_up(rows * c.pieces, 256), 8192);
+  c.blocks = (int32_t)std::min<int64_t>(div_up(rows * c.pieces, 256), kMaxCopyBlocks);
   return c;
 }
 
