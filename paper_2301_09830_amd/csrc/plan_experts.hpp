@@ -288,7 +288,9 @@ inline occ_status_t plan_experts_bwd(const occ_experts_grad_t& p, bool gated, Ex
     if (l.dW) f.dw_blocks = dw_blocks_of(wide, l.in, p.experts, side);
     if (f.dx_blocks + f.dw_blocks > kMaxBlocks || p.experts * wide >= ((int64_t)1 << 31)) return OCC_E_SHAPE;
   }
-  if (l.dbias && p.experts * div_up(wide, 64) > kMaxBlocks / 2) return OCC_E_SHAPE;
+  const int64_t bias_blocks = l.dbias ? p.experts * div_up(wide, 64) : 0;   // of the products' launch
+  if (bias_blocks > kMaxBlocks / 2 || f.dx_blocks + f.dw_blocks + bias_blocks > (((int64_t)1 << 32) - 1) / 512)
+    return OCC_E_SHAPE;
   const size_t os = f.planes ? 2 : es, np = f.planes ? kPlanes : 1;   // of operands in the workspace
   f.ldd = piece_ld(wide, os);
   Carve c;

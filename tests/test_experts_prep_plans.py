@@ -7,7 +7,9 @@ import subprocess
 
 import pytest
 
+from experts_plans import case, compile_plans
 from layer_plans import AVAILABLE, HIP_INCLUDE, ROOT
+from layer_plans import plans as plans_of
 
 pytestmark = pytest.mark.skipif(not AVAILABLE, reason="g++ or the HIP headers not available")
 
@@ -71,3 +73,25 @@ def test_launches_stay_within_the_largest_grid(tmp_path):
     assert len(plans) == len(cases) and sum(not p[0] for p in plans) > 200
     for c, (status, blocks, copies) in zip(cases, plans):
         assert status or (blocks + copies * COPY_BLOCKS) * 256 < 1 << 32, (c, blocks, copies)
+
+
+def test_products_beside_bias_sums_stay_within_the_largest_grid(tmp_path):
+    """The products' blocks and those of the bias gradient are one launch, 512 threads each."""
+    exe = compile_plans(tmp_path)
+    # some 3.6 million bias blocks beside 7.3 million tiles of 64, off 16 bytes
+    cases = [dict(kind="bwd", dtype="bf16", experts=e, rows=e, n_in=128, out=wide // e, shift=1, pad=1,
+                  act=0, dx=False) for e in (14, 100, 512) for wide in (200 << 20, 224 << 20)]
+    rng = random.Random(6)
+    for _ in range(3000):
+        e = rng.choice((1, 16, 64, 500, 1024))
+        gated = rng.random() < 0.3
+        out = rng.randint(1, (224 << 20) // e // (2 if gated else 1))
+        cases.append(dict(kind="bwd", dtype=rng.choice(("bf16", "f32")), experts=e, gated=gated,
+                          rows=rng.choice((1, 300, 1 << 20, rng.randint(1, 1 << 29))), shift=rng.choice((0, 1)),
+                          n_in=rng.randint(1, 600), out=min(out, 1 << 24), act=4 if gated else rng.randint(0, 4),
+                          dx=rng.random() < 0.5, db=rng.random() < 0.8))
+    taken = 0
+    for c, p in zip(cases, plans_of(exe, [case(**c) for c in cases])):
+        taken += not p["status"]
+        assert p["status"] or p["blocks"] * 512 < 1 << 32, (c, p)
+    assert taken > 300
