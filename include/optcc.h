@@ -545,8 +545,9 @@ occ_status_t occ_combine_bwd(const occ_exchange_t* x, const float* weights, cons
  * experts x 2 out), contiguous.  An expert may have no rows: its dW and dbias
  * are zero (or left, when accumulating).  Offsets out of 0 .. l.tokens are taken as
  * the nearer end, and one that falls as the largest before it; either raises
- * OCC_F_BAD_ROWS.  All else is as in occ_linear_fwd and its companions; the order
- * of a sum depends on the number of rows and experts, and of dbias on offsets. */
+ * OCC_F_BAD_ROWS (without any rows the offsets are not looked at).  All else is as
+ * in occ_linear_fwd and its companions; the order of a sum depends on the number of
+ * rows and experts, and of dbias on offsets. */
 typedef struct {
   occ_linear_t l;
   int64_t experts; /* 1 .. OCC_MAX_EXPERTS */

@@ -511,8 +511,10 @@ __global__ __launch_bounds__(1024) void k_route_choose(RouteArgs g) {
 }
 
 // Second launch: every block adds up the counts before its own.  Bound by the
-// latency of its few steps (8.5 us for 65536 tokens, k 8; 18.5 with 256 threads), so all loads of a step are in flight together: four
-// experts a thread, the blocks' rows dealt to groups of threads.
+// latency of its few steps (8.5 us for 65536 tokens, k 8; 18.5 with 256 threads),
+// so all loads of a step are in flight together: four experts a thread, the
+// blocks' rows dealt to groups of threads.  Some 1.6 us of it are conflicts of
+// LDS banks: the same word of random experts' masks lies in an eighth of them.
 __global__ __launch_bounds__(1024) void k_route_place(RouteArgs g) {
   __shared__ uint32_t mask[RT_EXPERTS * RT_WORDS];
   __shared__ int total[RT_EXPERTS], prior[RT_EXPERTS];
@@ -574,10 +576,12 @@ __global__ __launch_bounds__(1024) void k_route_place(RouteArgs g) {
 // ----------------------------------------------------------------------------
 // gradient of the logits
 // ----------------------------------------------------------------------------
-// Bound by memory and its few dependent steps (65536 x 128 bf16, softmax over
-// all experts: 34 MB in 11 us).  With s = sum of w dw over the choices: renormalised weights give the chosen
-// logits w (dw - s); weights of the softmax over all experts give -p s at every
-// expert and w dw more at the chosen ones.
+// Bound by memory and its few dependent steps (65536 x 128 bf16, k 8, softmax
+// over all experts: 39.8 MB in 11 to 13 us; renormalised, without the logits,
+// 23.1 MB in 5.9 where they lie in the caches).  With s = sum of w dw over the
+// choices: renormalised weights give the chosen logits w (dw - s); weights of the
+// softmax over all experts give -p s at every expert and w dw more at the chosen
+// ones.
 struct RouteGradArgs {
   const void* logits;
   void* dlogits;

@@ -829,7 +829,8 @@ def occ_route_bwd(dweights, logits, route, renorm: bool = True, dlogits=None, st
 def occ_dispatch(X, route, Xs=None, flags=None, stream=None):
     """Xs: the tokens' rows of X in the order of the experts (route.order).  Rows
     behind the last expert's are left alone.  Its gradient is occ_combine of dXs
-    without weights."""
+    without weights.  flags, here and in occ_combine and its backward pass: an int32
+    word that takes OCC_F_BAD_ROWS where an entry or a place is out of range."""
     if stream is not None:
         return _on(stream, occ_dispatch, X, route, Xs, flags)
     return _made("occ_dispatch", (_layers_module or _layers()).dispatch(
@@ -928,7 +929,9 @@ def occ_distill_fwd(S, index, teacher, temperature: float = 1.0, alpha: float = 
     at columns `index` (int32; a negative one is masked), alpha of it, and against
     labels (int32; a negative one is none), 1 - alpha.  scale: a factor for each
     token.  dS, if given, receives the gradient of the sum of the losses in the
-    same pass (it may be S); lse (float32, tokens x 2) what occ_distill_bwd needs."""
+    same pass (it may be S); lse (float32, tokens x 2) what occ_distill_bwd needs.
+    flags: an int32 word that takes OCC_F_BAD_ROWS where a column is none of S's.
+    temperature: above 0, its square a normal float32."""
     if stream is not None:
         return _on(stream, occ_distill_fwd, S, index, teacher, temperature, alpha, labels, scale,
                    loss, lse, dS, flags)
